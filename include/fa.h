@@ -529,8 +529,95 @@ int fa_kvcache_fwd(const void* Q, const void* Kcache, const void* Vcache, const 
                    float scale, int causal, int num_splits, void* stream);
 
 /*
+ * Decoding a batch whose sequences share a long prefix (a system prompt, several answers to one question): the queries of all
+ * sequences attend to the prefix, which is read once for the batch instead of once per sequence, and each to the keys its own
+ * sequence holds: O = softmax(scale * Q [Kprefix ; Kcache_b]^T) [Vprefix ; Vcache_b], what fa_kvcache_fwd gives for caches that
+ * begin with the prefix. (Not in the paper; softmax over the two parts is joined by the identity section 3.1.1 uses between blocks.)
+ *   Q, O [B, Nq, Hq, d], LSE [B, Hq, Nq] (of all keys a row sees). Every query sees the whole prefix; the causal rule holds
+ *   among a sequence's own keys, query r at position r + seqlens_k[b] - Nq of them. Own keys, seqlens_k (of the own keys
+ *   alone), block_table, page_size, pages_per_seq: as fa_kvcache_fwd.
+ *   Kprefix, Vprefix: prefix_table == nullptr: [Np, Hkv, d]; else pools of pages [pages, page_size, Hkv, d] (they may be the pools of
+ *   the caches) and prefix_table a DEVICE array of prefix_pages int32 page numbers, prefix_pages * page_size >= Np.
+ * Np = 0 (Kprefix, Vprefix may then be NULL) and own lengths of 0 are allowed; a row that sees no key at all gets O = 0, LSE = -inf.
+ * bfloat16, d in {64, 128}. How the keys are cut over workgroups goes by the sizes alone, so results are the same bits in every
+ * run; `workspace` (partial results, float32) needs fa_prefix_fwd_workspace_bytes() bytes, undefined on entry and return.
+ * Forward only, as fa_kvcache_fwd.
+ */
+size_t fa_prefix_fwd_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int d);
+int fa_prefix_fwd(const void* Q, const void* Kprefix, const void* Vprefix, const int32_t* prefix_table,
+                  const void* Kcache, const void* Vcache, const int32_t* seqlens_k, const int32_t* block_table,
+                  void* O, float* LSE, void* workspace, size_t workspace_bytes,
+                  int B, int Hq, int Hkv, int Nq, int Np, int Nk, int d, int page_size, int prefix_pages,
+                  int pages_per_seq, float scale, int causal, void* stream);
+
+/*
+ * New keys and values into a cache. Row i of Knew, Vnew [B, Nq, Hkv, d] goes to slot seqlens_k[b] - Nq + i of sequence b: seqlens_k
+ * counts the new keys already, as it does in the fa_kvcache_fwd call that follows (nullptr: Nk). Caches, block_table, page_size and
+ * pages_per_seq as fa_kvcache_fwd; Nk is the number of slots of a sequence. Rows whose slot lies outside 0 .. Nk - 1 are dropped.
+ * weights (float32) and positions (int32), each [B, Hkv, Nk] or NULL: what fa_cache_weights and fa_cache_evict keep beside every
+ * slot; a new slot gets weight 0 and position first_position[b] + i (first_position NULL: the slot's number). 16-bit elements of
+ * either type; d a multiple of 8 up to 256.
+ */
+int fa_cache_append(const void* Knew, const void* Vnew, void* Kcache, void* Vcache, const int32_t* seqlens_k,
+                    const int32_t* block_table, float* weights, int32_t* positions, const int32_t* first_position,
+                    int B, int Hkv, int Nq, int Nk, int d, int page_size, int pages_per_seq, void* stream);
+
+/*
+ * Attention weight that every cached key has drawn, added up over calls:
+ *     weights[b, g, c] += sum over the query heads h of group g, the queries r that see key c:  exp(scale * q_r . k_c - LSE[b, h, r])
+ * with the LSE that the attention over these keys left (fa_kvcache_fwd, fa_fwd; fa_prefix_fwd, whose LSE counts the prefix too).
+ * weights: float32 [B, Hkv, Nk]; slots past seqlens_k[b] are not touched. queries (DEVICE int32 [B] or NULL): only the first queries[b]
+ * (clamped into 0 .. Nq) of sequence b count, the others being drafts that were rejected; positions are those of all Nq. Rows with
+ * LSE = -inf add nothing. Q [B, Nq, Hq, d]; Kcache, seqlens_k, block_table, causal rule and limits as fa_kvcache_fwd
+ * (bfloat16, d in {64, 128}). No workspace, no atomics: the same bits in every run.
+ */
+int fa_cache_weights(const void* Q, const void* Kcache, const float* LSE, const int32_t* seqlens_k, const int32_t* block_table,
+                     const int32_t* queries, float* weights, int B, int Hq, int Hkv, int Nq, int Nk, int d, int page_size,
+                     int pages_per_seq, float scale, int causal, void* stream);
+
+/*
+ * Caches cut to `budget` keys by accumulated attention weight. Every (sequence, key/value head) with n = seqlens_k[b] > budget keeps
+ * budget of its slots: the protected ones first (position < sinks, or among the `recent` newest positions: position > newest -
+ * recent), then those of the largest weight; among equals the lower slot stays, a NaN counts as less than any number. Kept slots past
+ * the budget move, in ascending order, into the free ones below it, in ascending order; slots that stay where they are do so,
+ * so that as few rows move as can (attention does not ask in which order keys are kept; positions says which token a slot holds).
+ * K and V rows move in place. weights and positions [B, Hkv, Nk] are read; the first min(n, budget) slots of weights_out,
+ * positions_out and min(n, budget) itself as seqlens_out[b] are written. Each may be the array that it comes from. Nothing moves where
+ * n <= budget. seqlens_k NULL: Nk. 1 <= budget, 0 <= sinks, 0 <= recent, sinks + recent <= budget. Caches as fa_cache_append (every page
+ * that a sequence's slots lie in is its own). `workspace` needs fa_cache_evict_workspace_bytes() bytes.
+ */
+size_t fa_cache_evict_workspace_bytes(int B, int Hkv, int Nk, int budget);
+int fa_cache_evict(void* Kcache, void* Vcache, const float* weights, const int32_t* positions, const int32_t* seqlens_k,
+                   const int32_t* block_table, float* weights_out, int32_t* positions_out, int32_t* seqlens_out,
+                   void* workspace, size_t workspace_bytes, int B, int Hkv, int Nk, int d, int budget, int sinks, int recent,
+                   int page_size, int pages_per_seq, void* stream);
+
+/*
+ * Verification of drafted tokens. draft_tokens [B, k] int32 were drawn from draft_probs [B, k, V] (rows draft_stride elements apart;
+ * NULL: the drafts are certain, their probability 1); target [B, k + 1, V] (rows target_stride apart) holds the target's
+ * probabilities, or with target_is_logits its logits: p = softmax(inv_temperature * logits). uniform [B, k + 1] float32 in [0, 1).
+ * Draft i is accepted iff all before it are and uniform[b, i] * q_i(x_i) < p_i(x_i) (both probabilities of the drafted token).
+ * The token after the last accepted one is drawn: where a draft was rejected from max(p_i - q_i, 0) (from p_i where that is 0
+ * everywhere), after all k from p_k: the lowest token whose running sum exceeds uniform[b, k] times the whole sum (else the last one
+ * of weight above 0). A drafted token outside 0 .. V - 1 ends the drafts there and the next token is drawn from p_i. tokens
+ * [B, k + 1]: the accepted ones, the drawn one (-1 where all weights are 0), then -1; accepted [B]: how many drafts were. Sums that
+ * decide which token is drawn are float64. Logits of -inf are probabilities of 0. k >= 0 (k = 0: draft_tokens may be NULL, a
+ * draw from the target). Types: FA_TYPE_*. 1 <= V <= FA_VERIFY_MAX_VOCAB, strides >= V, inv_temperature > 0 and finite.
+ * Pointers aligned to their elements; workspace (8-byte aligned) of fa_verify_drafts_workspace_bytes() bytes.
+ */
+#define FA_TYPE_F32 0
+#define FA_TYPE_BF16 1
+#define FA_TYPE_F16 2
+#define FA_VERIFY_MAX_VOCAB (1 << 24)
+size_t fa_verify_drafts_workspace_bytes(int B, int k, int V);
+int fa_verify_drafts(const int32_t* draft_tokens, const void* draft_probs, const void* target, const float* uniform,
+                     int32_t* tokens, int32_t* accepted, void* workspace, size_t workspace_bytes, int B, int k, int V,
+                     long long draft_stride, long long target_stride, int draft_type, int target_type, int target_is_logits,
+                     float inv_temperature, void* stream);
+
+/*
  * The packed ragged entry points (one and two lengths, with dropout, with a window), the split-key
- * forward and the key/value cache forward for IEEE half precision (fp16) elements: each is its bfloat16 namesake with every
+ * forward, the key/value cache forward, the shared-prefix forward and the weights of cached keys for IEEE half precision (fp16) elements: each is its bfloat16 namesake with every
  * 16-bit tensor holding fp16, as fa_cross_fwd_f16 / fa_cross_bwd_f16 are to fa_cross_fwd /
  * fa_cross_bwd. LSE, workspaces, offset arrays, lengths, page tables, limits and errors are
  * unchanged.
@@ -582,6 +669,14 @@ int fa_kvcache_fwd_f16(const void* Q, const void* Kcache, const void* Vcache, co
                        void* workspace, size_t workspace_bytes,
                        int B, int Hq, int Hkv, int Nq, int Nk, int d, int page_size, int pages_per_seq,
                        float scale, int causal, int num_splits, void* stream);
+int fa_prefix_fwd_f16(const void* Q, const void* Kprefix, const void* Vprefix, const int32_t* prefix_table,
+                      const void* Kcache, const void* Vcache, const int32_t* seqlens_k, const int32_t* block_table,
+                      void* O, float* LSE, void* workspace, size_t workspace_bytes,
+                      int B, int Hq, int Hkv, int Nq, int Np, int Nk, int d, int page_size, int prefix_pages,
+                      int pages_per_seq, float scale, int causal, void* stream);
+int fa_cache_weights_f16(const void* Q, const void* Kcache, const float* LSE, const int32_t* seqlens_k,
+                         const int32_t* block_table, const int32_t* queries, float* weights, int B, int Hq, int Hkv, int Nq,
+                         int Nk, int d, int page_size, int pages_per_seq, float scale, int causal, void* stream);
 
 /*
  * Measurement aid, not part of either algorithm: a register-resident loop of the bf16 MFMA

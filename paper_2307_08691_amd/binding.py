@@ -103,6 +103,17 @@ SIGNATURES = {
     "fa_splitkv_fwd_f16": (_c_int, [_c_void_p] * 5 + [_c_void_p, _c_size_t] + [_c_int] * 6 + [_c_float, _c_int, _c_int, _c_void_p]),
     "fa_kvcache_fwd": (_c_int, [_c_void_p] * 7 + [_c_void_p, _c_size_t] + [_c_int] * 8 + [_c_float, _c_int, _c_int, _c_void_p]),
     "fa_kvcache_fwd_f16": (_c_int, [_c_void_p] * 7 + [_c_void_p, _c_size_t] + [_c_int] * 8 + [_c_float, _c_int, _c_int, _c_void_p]),
+    "fa_prefix_fwd_workspace_bytes": (_c_size_t, [_c_int] * 7),
+    "fa_prefix_fwd": (_c_int, [_c_void_p] * 10 + [_c_void_p, _c_size_t] + [_c_int] * 10 + [_c_float, _c_int, _c_void_p]),
+    "fa_prefix_fwd_f16": (_c_int, [_c_void_p] * 10 + [_c_void_p, _c_size_t] + [_c_int] * 10 + [_c_float, _c_int, _c_void_p]),
+    "fa_cache_append": (_c_int, [_c_void_p] * 9 + [_c_int] * 7 + [_c_void_p]),
+    "fa_cache_weights": (_c_int, [_c_void_p] * 7 + [_c_int] * 8 + [_c_float, _c_int, _c_void_p]),
+    "fa_cache_weights_f16": (_c_int, [_c_void_p] * 7 + [_c_int] * 8 + [_c_float, _c_int, _c_void_p]),
+    "fa_cache_evict_workspace_bytes": (_c_size_t, [_c_int] * 4),
+    "fa_cache_evict": (_c_int, [_c_void_p] * 9 + [_c_void_p, _c_size_t] + [_c_int] * 9 + [_c_void_p]),
+    "fa_verify_drafts_workspace_bytes": (_c_size_t, [_c_int] * 3),
+    "fa_verify_drafts": (_c_int, [_c_void_p] * 6 + [_c_void_p, _c_size_t] + [_c_int] * 3 + [ctypes.c_longlong] * 2 + [_c_int] * 3 +
+                         [_c_float, _c_void_p]),
     "fa_mfma_probe_scratch_bytes": (_c_size_t, []),
     "fa_mfma_probe": (_c_int, [_c_int, _c_int, _c_void_p, _c_void_p]),
 }
@@ -357,6 +368,50 @@ def fa_kvcache_fwd_raw(Q, Kc, Vc, seqlens_k, block_table, O, LSE, ws, ws_bytes, 
     fn = load().fa_kvcache_fwd_f16 if f16 else load().fa_kvcache_fwd
     return fn(Q, Kc, Vc, seqlens_k, block_table, O, LSE, ws, ws_bytes, B, Hq, Hkv, Nq, Nk, d, page_size,
               pages_per_seq, scale, int(causal), num_splits, stream)
+
+
+def fa_prefix_fwd_workspace_bytes(B, Hq, Hkv, Nq, Np, Nk, d) -> int:
+    return load().fa_prefix_fwd_workspace_bytes(B, Hq, Hkv, Nq, Np, Nk, d)
+
+
+def fa_prefix_fwd_raw(Q, Kp, Vp, prefix_table, Kc, Vc, seqlens_k, block_table, O, LSE, ws, ws_bytes, B, Hq, Hkv, Nq, Np, Nk, d,
+                      page_size, prefix_pages, pages_per_seq, scale, causal, stream=0, f16=False) -> int:
+    fn = load().fa_prefix_fwd_f16 if f16 else load().fa_prefix_fwd
+    return fn(Q, Kp, Vp, prefix_table, Kc, Vc, seqlens_k, block_table, O, LSE, ws, ws_bytes, B, Hq, Hkv, Nq, Np, Nk, d, page_size,
+              prefix_pages, pages_per_seq, scale, int(causal), stream)
+
+
+def fa_cache_append_raw(Knew, Vnew, Kc, Vc, seqlens_k, block_table, weights, positions, first_position, B, Hkv, Nq, Nk, d, page_size,
+                        pages_per_seq, stream=0) -> int:
+    return load().fa_cache_append(Knew, Vnew, Kc, Vc, seqlens_k, block_table, weights, positions, first_position, B, Hkv, Nq, Nk, d,
+                                  page_size, pages_per_seq, stream)
+
+
+def fa_cache_weights_raw(Q, Kc, LSE, seqlens_k, block_table, queries, weights, B, Hq, Hkv, Nq, Nk, d, page_size, pages_per_seq, scale,
+                         causal, stream=0, f16=False) -> int:
+    fn = load().fa_cache_weights_f16 if f16 else load().fa_cache_weights
+    return fn(Q, Kc, LSE, seqlens_k, block_table, queries, weights, B, Hq, Hkv, Nq, Nk, d, page_size, pages_per_seq, scale,
+              int(causal), stream)
+
+
+def fa_cache_evict_workspace_bytes(B, Hkv, Nk, budget) -> int:
+    return load().fa_cache_evict_workspace_bytes(B, Hkv, Nk, budget)
+
+
+def fa_cache_evict_raw(Kc, Vc, weights, positions, seqlens_k, block_table, weights_out, positions_out, seqlens_out, ws, ws_bytes, B,
+                       Hkv, Nk, d, budget, sinks, recent, page_size, pages_per_seq, stream=0) -> int:
+    return load().fa_cache_evict(Kc, Vc, weights, positions, seqlens_k, block_table, weights_out, positions_out, seqlens_out, ws,
+                                 ws_bytes, B, Hkv, Nk, d, budget, sinks, recent, page_size, pages_per_seq, stream)
+
+
+def fa_verify_drafts_workspace_bytes(B, k, V) -> int:
+    return load().fa_verify_drafts_workspace_bytes(B, k, V)
+
+
+def fa_verify_drafts_raw(draft_tokens, draft_probs, target, uniform, tokens, accepted, ws, ws_bytes, B, k, V, draft_stride,
+                         target_stride, draft_type, target_type, logits, inv_temperature, stream=0) -> int:
+    return load().fa_verify_drafts(draft_tokens, draft_probs, target, uniform, tokens, accepted, ws, ws_bytes, B, k, V, draft_stride,
+                                   target_stride, draft_type, target_type, int(logits), inv_temperature, stream)
 
 
 def fa_mfma_probe_scratch_bytes() -> int:
@@ -1030,6 +1085,202 @@ def fa_kvcache_fwd(Q, Kcache, Vcache, scale: float, causal: bool, seqlens_k=None
                               _wsbytes(ws), x.B, x.Hq, x.Hkv, x.Nq, x.Nk, x.d, page_size, pages_per_seq, scale, causal,
                               num_splits, _stream(), et == torch.float16))
     return O, LSE
+
+
+def _cache_slots(K, table, B, Nk, dev):
+    """A cache [B,Nk,Hkv,d], or pools [pages,page_size,Hkv,d] with block_table [B,pages_per_seq] -> (slots of a sequence, page_size,
+    pages_per_seq); Nk (0: all there are) says how many of the slots are meant."""
+    import torch
+    if table is None:
+        if K.shape[0] != B:
+            raise ValueError("a contiguous cache must be [B, Nk, Hkv, d]")
+        if Nk not in (0, K.shape[1]):
+            raise ValueError(f"the slots of a contiguous cache are its {K.shape[1]} rows a sequence, not {Nk}")
+        return K.shape[1], 0, 0
+    _need(table, "block_table", torch.int32, None, dev)
+    if table.dim() != 2 or table.shape[0] != B:
+        raise ValueError("block_table must be [B, pages_per_seq]")
+    slots = K.shape[1] * table.shape[1]
+    if Nk > slots:
+        raise ValueError(f"the pages of block_table hold {slots} slots a sequence, not {Nk}")
+    return Nk or slots, K.shape[1], table.shape[1]
+
+
+def fa_prefix_fwd(Q, Kprefix, Vprefix, Kcache, Vcache, scale: float, causal: bool, seqlens_k=None, block_table=None, prefix_table=None,
+                  prefix_len: int = 0, max_seqlen_k: int = 0, O=None, LSE=None, workspace=None):
+    """Nq new queries per sequence, Q [B,Nq,Hq,d] bf16 or fp16, against a prefix that all sequences share and each sequence's own cache
+    (Kcache, Vcache, seqlens_k, block_table, max_seqlen_k as fa_kvcache_fwd; lengths count the own keys alone). The prefix is read once for
+    the batch: Kprefix, Vprefix [Np,Hkv,d], or with prefix_table (int32 page numbers on the GPU) pools [pages,page_size,Hkv,d], of which
+    the first prefix_len keys are meant. The causal rule holds among own keys. Returns O [B,Nq,Hq,d] and LSE [B,Hq,Nq] fp32 (of all keys)."""
+    import torch
+    et = _elem_type(Q)
+    _need(Q, "Q", et)
+    if Q.dim() != 4 or Kcache.dim() != 4:
+        raise ValueError("Q must be [B, Nq, Hq, d] and the caches [B, Nk, Hkv, d] or [pages, page_size, Hkv, d]")
+    x = _Dims()
+    x.B, x.Nq, x.Hq, x.d = Q.shape
+    x.Hkv, x.et, x.dev = Kcache.shape[2], et, Q.device
+    _need(Kcache, "Kcache", et, None, x.dev)
+    _need(Vcache, "Vcache", et, tuple(Kcache.shape), x.dev)
+    if Kcache.shape[3] != x.d:
+        raise ValueError("the caches must have the head dimension of Q")
+    x.Nk, page_size, pages_per_seq = _cache_slots(Kcache, block_table, x.B, max_seqlen_k if block_table is not None else 0, x.dev)
+    _need(Kprefix, "Kprefix", et, None, x.dev)
+    _need(Vprefix, "Vprefix", et, tuple(Kprefix.shape), x.dev)
+    prefix_pages = 0
+    if prefix_table is None:
+        if Kprefix.dim() != 3 or tuple(Kprefix.shape[1:]) != (x.Hkv, x.d):
+            raise ValueError("the prefix must be [Np, Hkv, d], or pools of pages with a prefix_table")
+        Np = prefix_len or Kprefix.shape[0]
+        if not 0 <= Np <= Kprefix.shape[0]:
+            raise ValueError(f"the prefix holds {Kprefix.shape[0]} keys, not {Np}")
+    else:
+        _need(prefix_table, "prefix_table", torch.int32, None, x.dev)
+        if prefix_table.dim() != 1 or Kprefix.dim() != 4 or tuple(Kprefix.shape[2:]) != (x.Hkv, x.d):
+            raise ValueError("a prefix in pages is pools [pages, page_size, Hkv, d] and a vector prefix_table")
+        if block_table is not None and Kprefix.shape[1] != page_size:
+            raise ValueError("the pages of the prefix and of the caches must be of one size")
+        page_size, prefix_pages, Np = Kprefix.shape[1], prefix_table.numel(), prefix_len
+        if not 0 < Np <= page_size * prefix_pages:
+            raise ValueError("prefix_len must be given with a prefix_table, and lie in its pages")
+    if seqlens_k is not None:
+        _need(seqlens_k, "seqlens_k", torch.int32, (x.B,), x.dev)
+    x.q_shape, x.l_shape = (x.B, x.Nq, x.Hq, x.d), (x.B, x.Hq, x.Nq)
+    O, LSE = _fwd_outputs(x, O, LSE)
+    ws = _workspace(workspace, fa_prefix_fwd_workspace_bytes(x.B, x.Hq, x.Hkv, x.Nq, Np, x.Nk, x.d), x.dev)
+    _check(fa_prefix_fwd_raw(_ptr(Q), _ptr(Kprefix), _ptr(Vprefix), _ptr(prefix_table), _ptr(Kcache), _ptr(Vcache), _ptr(seqlens_k),
+                             _ptr(block_table), _ptr(O), _ptr(LSE), _ptr(ws), _wsbytes(ws), x.B, x.Hq, x.Hkv, x.Nq, Np, x.Nk, x.d,
+                             page_size, prefix_pages, pages_per_seq, scale, causal, _stream(), et == torch.float16))
+    return O, LSE
+
+
+def _beside_slots(t, name, dtype, B, Hkv, dev):
+    """weights or positions [B,Hkv,slots] -> slots"""
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [B, Hkv, slots]")
+    _need(t, name, dtype, (B, Hkv, t.shape[2]), dev)
+    return t.shape[2]
+
+
+def fa_cache_append(Knew, Vnew, Kcache, Vcache, seqlens_k=None, block_table=None, weights=None, positions=None, first_position=None):
+    """New keys and values Knew, Vnew [B,Nq,Hkv,d] (bf16 or fp16) into the slots seqlens_k[b] - Nq .. of every sequence's cache (slabs or
+    pages as fa_kvcache_fwd; seqlens_k counts the new keys already). weights [B,Hkv,slots] fp32 and positions [B,Hkv,slots] int32, where
+    given: weight 0 and position first_position[b] + i (int32 [B]; None: the slot) for the new slots. Returns the caches."""
+    import torch
+    et = _elem_type(Knew)
+    _need(Knew, "Knew", et)
+    if Knew.dim() != 4 or Kcache.dim() != 4:
+        raise ValueError("Knew must be [B, Nq, Hkv, d] and the caches [B, Nk, Hkv, d] or [pages, page_size, Hkv, d]")
+    B, Nq, Hkv, d = Knew.shape
+    dev = Knew.device
+    _need(Vnew, "Vnew", et, (B, Nq, Hkv, d), dev)
+    _need(Kcache, "Kcache", et, (*Kcache.shape[:2], Hkv, d), dev)
+    _need(Vcache, "Vcache", et, tuple(Kcache.shape), dev)
+    slots = [_beside_slots(t, nm, ty, B, Hkv, dev) for t, nm, ty in ((weights, "weights", torch.float32), (positions, "positions", torch.int32))
+             if t is not None]
+    if len(set(slots)) > 1:
+        raise ValueError("weights and positions must have as many slots")
+    Nk, page_size, pages = _cache_slots(Kcache, block_table, B, slots[0] if slots else 0, dev)
+    if seqlens_k is not None:
+        _need(seqlens_k, "seqlens_k", torch.int32, (B,), dev)
+    if first_position is not None:
+        _need(first_position, "first_position", torch.int32, (B,), dev)
+    _check(fa_cache_append_raw(_ptr(Knew), _ptr(Vnew), _ptr(Kcache), _ptr(Vcache), _ptr(seqlens_k), _ptr(block_table), _ptr(weights),
+                               _ptr(positions), _ptr(first_position), B, Hkv, Nq, Nk, d, page_size, pages, _stream()))
+    return Kcache, Vcache
+
+
+def fa_cache_weights(Q, Kcache, LSE, weights, scale: float, causal: bool, seqlens_k=None, block_table=None, queries=None):
+    """weights [B,Hkv,slots] fp32 += the attention weight that each cached key draws from the queries Q [B,Nq,Hq,d] (bf16 or fp16), summed
+    over the queries and the heads of its group: exp(scale q.k - LSE), LSE [B,Hq,Nq] fp32 from the attention over these keys.
+    queries (int32 [B]): only the first of each sequence count (accepted drafts). Cache and lengths as fa_kvcache_fwd. Returns weights."""
+    import torch
+    et = _elem_type(Q)
+    _need(Q, "Q", et)
+    if Q.dim() != 4 or Kcache.dim() != 4:
+        raise ValueError("Q must be [B, Nq, Hq, d] and the cache [B, Nk, Hkv, d] or [pages, page_size, Hkv, d]")
+    B, Nq, Hq, d = Q.shape
+    dev, Hkv = Q.device, Kcache.shape[2]
+    _need(Kcache, "Kcache", et, (*Kcache.shape[:3], d), dev)
+    _need(LSE, "LSE", torch.float32, (B, Hq, Nq), dev)
+    Nk, page_size, pages = _cache_slots(Kcache, block_table, B, _beside_slots(weights, "weights", torch.float32, B, Hkv, dev), dev)
+    for t, nm in ((seqlens_k, "seqlens_k"), (queries, "queries")):
+        if t is not None:
+            _need(t, nm, torch.int32, (B,), dev)
+    _check(fa_cache_weights_raw(_ptr(Q), _ptr(Kcache), _ptr(LSE), _ptr(seqlens_k), _ptr(block_table), _ptr(queries), _ptr(weights), B, Hq,
+                                Hkv, Nq, Nk, d, page_size, pages, scale, causal, _stream(), et == torch.float16))
+    return weights
+
+
+def fa_cache_evict(Kcache, Vcache, weights, positions, seqlens_k, budget: int, sinks: int = 0, recent: int = 0, block_table=None,
+                   weights_out=None, positions_out=None, seqlens_out=None, workspace=None):
+    """Cut every sequence's cache to `budget` keys a head: the keys at positions below `sinks` and the `recent` newest stay, then those
+    of the largest weight; kept rows past the budget move into the free slots below it, in place. weights fp32, positions int32
+    [B,Hkv,slots] and seqlens_k int32 [B] are updated in place, or written to weights_out, positions_out, seqlens_out. Returns those
+    three."""
+    import torch
+    et = _elem_type(Kcache)
+    if Kcache.dim() != 4:
+        raise ValueError("the caches must be [B, Nk, Hkv, d] or [pages, page_size, Hkv, d]")
+    dev, Hkv, d, B = Kcache.device, Kcache.shape[2], Kcache.shape[3], weights.shape[0]
+    _need(Kcache, "Kcache", et)
+    _need(Vcache, "Vcache", et, tuple(Kcache.shape), dev)
+    slots = _beside_slots(weights, "weights", torch.float32, B, Hkv, dev)
+    shape = (B, Hkv, slots)
+    _need(positions, "positions", torch.int32, shape, dev)
+    _need(seqlens_k, "seqlens_k", torch.int32, (B,), dev)
+    Nk, page_size, pages = _cache_slots(Kcache, block_table, B, slots, dev)
+    weights_out = weights if weights_out is None else _out(weights_out, "weights_out", shape, torch.float32, dev)
+    positions_out = positions if positions_out is None else _out(positions_out, "positions_out", shape, torch.int32, dev)
+    seqlens_out = seqlens_k if seqlens_out is None else _out(seqlens_out, "seqlens_out", (B,), torch.int32, dev)
+    ws = _workspace(workspace, fa_cache_evict_workspace_bytes(B, Hkv, Nk, budget), dev)
+    _check(fa_cache_evict_raw(_ptr(Kcache), _ptr(Vcache), _ptr(weights), _ptr(positions), _ptr(seqlens_k), _ptr(block_table),
+                              _ptr(weights_out), _ptr(positions_out), _ptr(seqlens_out), _ptr(ws), _wsbytes(ws), B, Hkv, Nk, d, budget,
+                              sinks, recent, page_size, pages, _stream()))
+    return weights_out, positions_out, seqlens_out
+
+
+FA_TYPE_F32, FA_TYPE_BF16, FA_TYPE_F16 = 0, 1, 2
+
+
+def _vocab_rows(t, name, shape, dev):
+    """Rows of V values, the rows of all sequences evenly spaced -> (type code, elements between rows). (V may be a slice of wider rows.)"""
+    import torch
+    types = {torch.float32: FA_TYPE_F32, torch.bfloat16: FA_TYPE_BF16, torch.float16: FA_TYPE_F16}
+    if t.dtype not in types:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16")
+    if tuple(t.shape) != shape or t.device != dev:
+        raise ValueError(f"{name} must have shape {shape} and be on {dev}, not {tuple(t.shape)} on {t.device}")
+    row = t.stride(1) if shape[1] > 1 else t.stride(0) if shape[0] > 1 else shape[2]
+    if t.stride(2) != 1 or row < shape[2] or (shape[0] > 1 and t.stride(0) != shape[1] * row):
+        raise ValueError(f"the rows of {name} must be dense and evenly spaced")
+    return types[t.dtype], row
+
+
+def fa_verify_drafts(draft_tokens, draft_probs, target, uniform, logits: bool = False, inv_temperature: float = 1.0, tokens=None,
+                     accepted=None, workspace=None):
+    """Verify drafted tokens: draft_tokens [B,k] int32, drawn from draft_probs [B,k,V] (None: certain), against the target's
+    probabilities [B,k+1,V] (logits=True: softmax(inv_temperature * target)), with uniform [B,k+1] fp32 in [0,1): k to accept with, the
+    last to draw the next token with. Values fp32, bf16 or fp16; rows may be slices of wider ones. Returns tokens [B,k+1] int32 (the
+    accepted drafts, the drawn token, then -1) and accepted [B] int32."""
+    import torch
+    dev = target.device
+    if draft_tokens.dim() != 2 or target.dim() != 3:
+        raise ValueError("draft_tokens must be [B, k] and target [B, k + 1, V]")
+    (B, k), V = draft_tokens.shape, target.shape[2]
+    _need(draft_tokens, "draft_tokens", torch.int32, None, dev)
+    target_type, target_stride = _vocab_rows(target, "target", (B, k + 1, V), dev)
+    draft_type, draft_stride = 0, V
+    if draft_probs is not None and k > 0:
+        draft_type, draft_stride = _vocab_rows(draft_probs, "draft_probs", (B, k, V), dev)
+    _need(uniform, "uniform", torch.float32, (B, k + 1), dev)
+    tokens = _out(tokens, "tokens", (B, k + 1), torch.int32, dev)
+    accepted = _out(accepted, "accepted", (B,), torch.int32, dev)
+    ws = _workspace(workspace, fa_verify_drafts_workspace_bytes(B, k, V), dev)
+    _check(fa_verify_drafts_raw(_ptr(draft_tokens), _ptr(draft_probs), _ptr(target), _ptr(uniform), _ptr(tokens), _ptr(accepted), _ptr(ws),
+                                _wsbytes(ws), B, k, V, draft_stride, target_stride, draft_type, target_type, logits, inv_temperature,
+                                _stream()))
+    return tokens, accepted
 
 
 def fa_mfma_probe(iters: int, random_operands: bool):

@@ -1025,6 +1025,224 @@ int fa_kvcache_fwd_f16(const void* Q, const void* Kcache, const void* Vcache, co
                          Nq, Nk, d, page_size, pages_per_seq, scale, causal, num_splits, stream);
 }
 
+// ---- caches that are written, weighed and cut, a prefix that a batch shares, drafts that are verified
+
+static inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+static int launched(hipError_t e) {
+  if (e == hipSuccess) return FA_OK;
+  g_last_hip_error = (int)e;
+  return FA_ERR_LAUNCH;
+}
+
+// The slots of B sequences (Nk each), in slabs or pages
+static int set_cache(fa::CacheView& c, const int32_t* lens, const int32_t* table, int B, int Hkv, int Nk, int d, int page_size, int pages_per_seq) {
+  if (B <= 0 || Hkv <= 0 || Nk <= 0) return FA_ERR_SHAPE;
+  if (B > (1 << 20) || Hkv > (1 << 20) || (long)B * Hkv > (1 << 20)) return FA_ERR_SHAPE;  // (a grid has room for them)
+  c = {lens, table, 0, pages_per_seq, Nk, Hkv, d};
+  if (table) {
+    if (page_size < 64 || (page_size & (page_size - 1))) return FA_ERR_UNSUPPORTED;
+    if (pages_per_seq < 1 || (long)pages_per_seq * page_size < Nk) return FA_ERR_SHAPE;
+    c.page_log2 = __builtin_ctz((unsigned)page_size);
+  }
+  if (!aligned4(lens) || !aligned4(table)) return FA_ERR_ALIGN;
+  return FA_OK;
+}
+
+// Head dimensions of the kernels that only move rows
+static int check_rows(int d) { return d <= 0 ? FA_ERR_SHAPE : (d % 8 || d > 256 ? FA_ERR_UNSUPPORTED : FA_OK); }
+
+size_t fa_prefix_fwd_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int d) {
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || Nq <= 0 || Np < 0 || Nk <= 0 || (d != 64 && d != 128) ||
+      (double)B * Nq * Hq > (1 << 26))
+    return 0;
+  const fa::PrefixPlan p = fa::prefix_plan(B, Hq, Hkv, Nq, Np, Nk, d);
+  return round_up((size_t)(p.prefix_shares + p.own_shares) * B * Nq * Hq * (d + 1) * sizeof(float), 256);
+}
+
+static int prefix_fwd_any(int f16, const void* Q, const void* Kprefix, const void* Vprefix, const int32_t* prefix_table, const void* Kcache,
+                          const void* Vcache, const int32_t* seqlens_k, const int32_t* block_table, void* O, float* LSE, void* workspace,
+                          size_t workspace_bytes, int B, int Hq, int Hkv, int Nq, int Np, int Nk, int d, int page_size,
+                          int prefix_pages, int pages_per_seq, float scale, int causal, void* stream) {
+  if (!Q || !Kcache || !Vcache || !O || !LSE || !workspace || (Np > 0 && (!Kprefix || !Vprefix))) return FA_ERR_NULL;
+  if (Nq <= 0 || Np < 0) return FA_ERR_SHAPE;
+  if (int e = check_common(Hq, Hkv, d, scale, false)) return e;
+  fa::PrefixArgs a;
+  if (int e = set_cache(a.own, seqlens_k, block_table, B, Hkv, Nk, d, page_size, pages_per_seq)) return e;
+  if ((double)B * Nq * Hq > (1 << 26)) return FA_ERR_SHAPE;
+  if (prefix_table && Np > 0) {
+    if (page_size < 64 || (page_size & (page_size - 1))) return FA_ERR_UNSUPPORTED;
+    if (prefix_pages < 1 || (long)prefix_pages * page_size < Np) return FA_ERR_SHAPE;
+    a.own.page_log2 = __builtin_ctz((unsigned)page_size);
+  }
+  if (!aligned16(Q) || !aligned16(Kprefix) || !aligned16(Vprefix) || !aligned16(Kcache) || !aligned16(Vcache) || !aligned16(O) ||
+      !aligned16(LSE) || !aligned16(workspace) || !aligned4(prefix_table))
+    return FA_ERR_ALIGN;
+  if (workspace_bytes < fa_prefix_fwd_workspace_bytes(B, Hq, Hkv, Nq, Np, Nk, d)) return FA_ERR_WORKSPACE;
+  const fa::PrefixPlan p = fa::prefix_plan(B, Hq, Hkv, Nq, Np, Nk, d);
+  a.Q = (const __bf16*)Q;
+  a.Kp = (const __bf16*)Kprefix;
+  a.Vp = (const __bf16*)Vprefix;
+  a.K = (const __bf16*)Kcache;
+  a.V = (const __bf16*)Vcache;
+  a.prefix_table = prefix_table;
+  a.O = (__bf16*)O;
+  a.LSE = LSE;
+  a.Opart = (float*)workspace;
+  a.Lpart = a.Opart + (size_t)(p.prefix_shares + p.own_shares) * B * Nq * Hq * d;
+  a.nseq = B;
+  a.Nq = Nq;
+  a.Np = Np;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.G = Hq / Hkv;
+  a.f16 = f16;
+  a.causal = causal != 0;
+  a.scale = scale;
+  a.scale_log2e = scale * fa::kLog2e;
+  return launched(fa::launch_prefix(a, d, (hipStream_t)stream));
+}
+
+int fa_prefix_fwd(const void* Q, const void* Kprefix, const void* Vprefix, const int32_t* prefix_table, const void* Kcache,
+                  const void* Vcache, const int32_t* seqlens_k, const int32_t* block_table, void* O, float* LSE, void* workspace,
+                  size_t workspace_bytes, int B, int Hq, int Hkv, int Nq, int Np, int Nk, int d, int page_size, int prefix_pages,
+                  int pages_per_seq, float scale, int causal, void* stream) {
+  return prefix_fwd_any(0, Q, Kprefix, Vprefix, prefix_table, Kcache, Vcache, seqlens_k, block_table, O, LSE, workspace, workspace_bytes, B,
+                        Hq, Hkv, Nq, Np, Nk, d, page_size, prefix_pages, pages_per_seq, scale, causal, stream);
+}
+
+int fa_prefix_fwd_f16(const void* Q, const void* Kprefix, const void* Vprefix, const int32_t* prefix_table, const void* Kcache,
+                      const void* Vcache, const int32_t* seqlens_k, const int32_t* block_table, void* O, float* LSE, void* workspace,
+                      size_t workspace_bytes, int B, int Hq, int Hkv, int Nq, int Np, int Nk, int d, int page_size,
+                      int prefix_pages, int pages_per_seq, float scale, int causal, void* stream) {
+  return prefix_fwd_any(1, Q, Kprefix, Vprefix, prefix_table, Kcache, Vcache, seqlens_k, block_table, O, LSE, workspace, workspace_bytes, B,
+                        Hq, Hkv, Nq, Np, Nk, d, page_size, prefix_pages, pages_per_seq, scale, causal, stream);
+}
+
+int fa_cache_append(const void* Knew, const void* Vnew, void* Kcache, void* Vcache, const int32_t* seqlens_k, const int32_t* block_table,
+                    float* weights, int32_t* positions, const int32_t* first_position, int B, int Hkv, int Nq, int Nk, int d,
+                    int page_size, int pages_per_seq, void* stream) {
+  if (!Knew || !Vnew || !Kcache || !Vcache) return FA_ERR_NULL;
+  if (Nq <= 0) return FA_ERR_SHAPE;
+  if (int e = check_rows(d)) return e;
+  fa::AppendArgs a;
+  if (int e = set_cache(a.c, seqlens_k, block_table, B, Hkv, Nk, d, page_size, pages_per_seq)) return e;
+  if ((double)B * Nq * Hkv * (d / 8) > (double)(1u << 31)) return FA_ERR_SHAPE;
+  if (!aligned16(Knew) || !aligned16(Vnew) || !aligned16(Kcache) || !aligned16(Vcache) || !aligned4(weights) || !aligned4(positions) ||
+      !aligned4(first_position))
+    return FA_ERR_ALIGN;
+  a.Kn = (const __bf16*)Knew;
+  a.Vn = (const __bf16*)Vnew;
+  a.K = (__bf16*)Kcache;
+  a.V = (__bf16*)Vcache;
+  a.weights = weights;
+  a.positions = positions;
+  a.first = first_position;
+  a.nseq = B;
+  a.Nq = Nq;
+  return launched(fa::launch_append(a, (hipStream_t)stream));
+}
+
+static int cache_weights_any(int f16, const void* Q, const void* Kcache, const float* LSE, const int32_t* seqlens_k,
+                             const int32_t* block_table, const int32_t* queries, float* weights, int B, int Hq, int Hkv, int Nq,
+                             int Nk, int d, int page_size, int pages_per_seq, float scale, int causal, void* stream) {
+  if (!Q || !Kcache || !LSE || !weights) return FA_ERR_NULL;
+  if (Nq <= 0) return FA_ERR_SHAPE;
+  if (int e = check_common(Hq, Hkv, d, scale, false)) return e;
+  fa::WeightsArgs a;
+  if (int e = set_cache(a.c, seqlens_k, block_table, B, Hkv, Nk, d, page_size, pages_per_seq)) return e;
+  if ((long)Nq * (Hq / Hkv) > (1 << 30)) return FA_ERR_SHAPE;
+  if (!aligned16(Q) || !aligned16(Kcache) || !aligned4(LSE) || !aligned4(weights) || !aligned4(queries)) return FA_ERR_ALIGN;
+  a.Q = (const __bf16*)Q;
+  a.K = (const __bf16*)Kcache;
+  a.LSE = LSE;
+  a.weights = weights;
+  a.queries = queries;
+  a.nseq = B;
+  a.Nq = Nq;
+  a.Hq = Hq;
+  a.G = Hq / Hkv;
+  a.f16 = f16;
+  a.causal = causal != 0;
+  a.scale = scale;
+  return launched(fa::launch_weights(a, (hipStream_t)stream));
+}
+
+int fa_cache_weights(const void* Q, const void* Kcache, const float* LSE, const int32_t* seqlens_k, const int32_t* block_table,
+                     const int32_t* queries, float* weights, int B, int Hq, int Hkv, int Nq, int Nk, int d, int page_size,
+                     int pages_per_seq, float scale, int causal, void* stream) {
+  return cache_weights_any(0, Q, Kcache, LSE, seqlens_k, block_table, queries, weights, B, Hq, Hkv, Nq, Nk, d, page_size, pages_per_seq,
+                           scale, causal, stream);
+}
+
+int fa_cache_weights_f16(const void* Q, const void* Kcache, const float* LSE, const int32_t* seqlens_k, const int32_t* block_table,
+                         const int32_t* queries, float* weights, int B, int Hq, int Hkv, int Nq, int Nk, int d, int page_size,
+                         int pages_per_seq, float scale, int causal, void* stream) {
+  return cache_weights_any(1, Q, Kcache, LSE, seqlens_k, block_table, queries, weights, B, Hq, Hkv, Nq, Nk, d, page_size, pages_per_seq,
+                           scale, causal, stream);
+}
+
+static int evict_room(int Nk, int budget) { return Nk <= budget ? 0 : (Nk - budget < budget ? Nk - budget : budget); }
+
+size_t fa_cache_evict_workspace_bytes(int B, int Hkv, int Nk, int budget) {
+  if (B <= 0 || Hkv <= 0 || Nk <= 0 || budget <= 0) return 0;
+  return round_up((size_t)B * Hkv * (1 + 2 * (size_t)evict_room(Nk, budget)) * sizeof(int32_t), 256);
+}
+
+int fa_cache_evict(void* Kcache, void* Vcache, const float* weights, const int32_t* positions, const int32_t* seqlens_k,
+                   const int32_t* block_table, float* weights_out, int32_t* positions_out, int32_t* seqlens_out, void* workspace,
+                   size_t workspace_bytes, int B, int Hkv, int Nk, int d, int budget, int sinks, int recent, int page_size,
+                   int pages_per_seq, void* stream) {
+  if (!Kcache || !Vcache || !weights || !positions || !weights_out || !positions_out || !seqlens_out || !workspace) return FA_ERR_NULL;
+  if (budget <= 0 || sinks < 0 || recent < 0 || (long)sinks + recent > budget) return FA_ERR_SHAPE;
+  if (int e = check_rows(d)) return e;
+  fa::EvictArgs a;
+  if (int e = set_cache(a.c, seqlens_k, block_table, B, Hkv, Nk, d, page_size, pages_per_seq)) return e;
+  if (!aligned16(Kcache) || !aligned16(Vcache) || !aligned4(weights) || !aligned4(positions) || !aligned4(weights_out) ||
+      !aligned4(positions_out) || !aligned4(seqlens_out) || !aligned4(workspace))
+    return FA_ERR_ALIGN;
+  if (workspace_bytes < fa_cache_evict_workspace_bytes(B, Hkv, Nk, budget)) return FA_ERR_WORKSPACE;
+  a.K = (__bf16*)Kcache;
+  a.V = (__bf16*)Vcache;
+  a.weights = weights;
+  a.positions = positions;
+  a.weights_out = weights_out;
+  a.positions_out = positions_out;
+  a.lens_out = seqlens_out;
+  a.moves = (int32_t*)workspace;
+  a.nseq = B;
+  a.budget = budget;
+  a.sinks = sinks;
+  a.recent = recent;
+  a.room = evict_room(Nk, budget);
+  return launched(fa::launch_evict(a, (hipStream_t)stream));
+}
+
+size_t fa_verify_drafts_workspace_bytes(int B, int k, int V) {
+  if (B <= 0 || k < 0 || V <= 0 || V > FA_VERIFY_MAX_VOCAB) return 0;
+  return round_up(fa::verify_workspace(B, k, V), 256);
+}
+
+int fa_verify_drafts(const int32_t* draft_tokens, const void* draft_probs, const void* target, const float* uniform, int32_t* tokens,
+                     int32_t* accepted, void* workspace, size_t workspace_bytes, int B, int k, int V, long long draft_stride,
+                     long long target_stride, int draft_type, int target_type, int target_is_logits, float inv_temperature,
+                     void* stream) {
+  if ((k > 0 && !draft_tokens) || !target || !uniform || !tokens || !accepted || !workspace) return FA_ERR_NULL;
+  if (B <= 0 || k < 0 || V <= 0 || V > FA_VERIFY_MAX_VOCAB || (long)B * ((long)k + 1) > (1 << 20)) return FA_ERR_SHAPE;
+  if (target_stride < V || (k > 0 && draft_probs && draft_stride < V)) return FA_ERR_SHAPE;
+  if (!(inv_temperature > 0.f) || !std::isfinite(inv_temperature)) return FA_ERR_SHAPE;
+  auto misplaced = [](const void* p, int type) { return (reinterpret_cast<uintptr_t>(p) & (type == FA_TYPE_F32 ? 3u : 1u)) != 0; };
+  if (target_type < FA_TYPE_F32 || target_type > FA_TYPE_F16 || (draft_probs && (draft_type < FA_TYPE_F32 || draft_type > FA_TYPE_F16)))
+    return FA_ERR_UNSUPPORTED;
+  if (misplaced(target, target_type) || misplaced(draft_probs, draft_type) || !aligned4(draft_tokens) || !aligned4(uniform) ||
+      !aligned4(tokens) || !aligned4(accepted) || (reinterpret_cast<uintptr_t>(workspace) & 7u))
+    return FA_ERR_ALIGN;
+  if (workspace_bytes < fa_verify_drafts_workspace_bytes(B, k, V)) return FA_ERR_WORKSPACE;
+  const fa::VerifyArgs a = {draft_tokens, k > 0 ? draft_probs : nullptr, target, uniform, tokens, accepted, workspace, B, k, V, draft_type,
+                            target_type, target_is_logits != 0, (long)draft_stride, (long)target_stride, target_is_logits ? inv_temperature : 1.f};
+  return launched(fa::launch_verify(a, (hipStream_t)stream));
+}
+
 size_t fa_mfma_probe_scratch_bytes(void) { return 16 + (size_t)256 * 512 * sizeof(float); }
 
 int fa_mfma_probe(int iters, int random_operands, void* scratch, void* stream) {

@@ -136,6 +136,94 @@ struct Fp8Args {
   float descale_v;
 };
 
+// A key/value cache as the cache kernels see it: slabs [nseq, Nk, Hkv, d] or, with a table, pools of pages of 2^page_log2 rows.
+// Sequence s holds lens[s] keys (nullptr: Nk), clamped into 0 .. Nk.
+struct CacheView {
+  const int32_t* lens;
+  const int32_t* table;  // page c >> page_log2 of sequence s: table[s * table_stride + (c >> page_log2)]
+  int page_log2, table_stride;
+  int Nk, Hkv, d;
+};
+__device__ __forceinline__ int held_keys(const CacheView& c, int s) {
+  const int n = c.lens ? c.lens[s] : c.Nk;
+  return n < 0 ? 0 : (n < c.Nk ? n : c.Nk);
+}
+// Row (of Hkv * d elements) in which sequence s keeps slot `c`.
+__device__ __forceinline__ long cache_row(const CacheView& v, int s, int c) {
+  if (!v.table) return (long)s * v.Nk + c;
+  const int page = v.table[(long)s * v.table_stride + (c >> v.page_log2)];
+  return ((long)page << v.page_log2) + (c & ((1 << v.page_log2) - 1));
+}
+
+// Attention of a batch that shares a prefix (fa_prefix.hip)
+struct PrefixArgs {
+  const __bf16 *Q, *Kp, *Vp, *K, *V;
+  const int32_t* prefix_table;  // pages of the prefix (of 2^page_log2 rows); nullptr: Kp, Vp are slabs of Np rows
+  CacheView own;
+  __bf16* O;
+  float* LSE;
+  float *Opart, *Lpart;  // [slot][token][Hq][d], [slot][token][Hq]: shares of the prefix, then of the own keys
+  int nseq, Nq, Np, Hq, Hkv, G, f16, causal;
+  float scale, scale_log2e;
+};
+struct PrefixPlan {  // how the prefix and the own keys are cut (a function of the sizes alone)
+  int prefix_rows, prefix_shares;  // packed rows of a workgroup, shares of the prefix
+  int own_rows, own_shares;
+};
+PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int d);
+hipError_t launch_prefix(const PrefixArgs& a, int d, hipStream_t st);
+
+// New rows into a cache (fa_cache.hip)
+struct AppendArgs {
+  CacheView c;
+  const __bf16 *Kn, *Vn;
+  __bf16 *K, *V;
+  float* weights;         // [nseq, Hkv, Nk] or nullptr
+  int32_t* positions;     // likewise
+  const int32_t* first;   // position of the first new key of each sequence (nullptr: its slot)
+  int nseq, Nq;
+};
+hipError_t launch_append(const AppendArgs& a, hipStream_t st);
+
+// Attention weight per cached key, added up (fa_weights.hip)
+struct WeightsArgs {
+  CacheView c;
+  const __bf16 *Q, *K;
+  const float* LSE;
+  float* weights;
+  const int32_t* queries;  // of sequence s only the first queries[s] count (nullptr: all)
+  int nseq, Nq, Hq, G, f16, causal;
+  float scale;
+};
+hipError_t launch_weights(const WeightsArgs& a, hipStream_t st);
+
+// Caches cut to a budget (fa_cache.hip)
+struct EvictArgs {
+  CacheView c;
+  __bf16 *K, *V;
+  const float* weights;
+  const int32_t* positions;
+  float* weights_out;
+  int32_t *positions_out, *lens_out;
+  int32_t* moves;  // workspace: [pairs] counts, then per pair `room` destinations and `room` sources
+  int nseq, budget, sinks, recent, room;
+};
+hipError_t launch_evict(const EvictArgs& a, hipStream_t st);
+
+// Drafted tokens against the target's probabilities (fa_verify.hip). Types: FA_TYPE_*.
+struct VerifyArgs {
+  const int32_t* drafts;
+  const void *q, *target;
+  const float* uniform;
+  int32_t *tokens, *accepted;
+  void* ws;
+  int nseq, k, V, q_type, target_type, logits;
+  long q_stride, target_stride;
+  float inv_t;
+};
+size_t verify_workspace(int B, int k, int V);
+hipError_t launch_verify(const VerifyArgs& a, hipStream_t st);
+
 hipError_t launch_fwd(const FwdArgs& a, int d, int causal, hipStream_t st);
 // forward in workgroups of four wavefronts for grids that leave wavefront slots empty (fa_stream.hip); d in {64, 128}
 hipError_t launch_fwd_stream(const FwdArgs& a, int d, int causal, hipStream_t st);

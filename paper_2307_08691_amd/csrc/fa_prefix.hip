@@ -1,0 +1,401 @@
+// Attention of a batch whose sequences share a prefix: every query attends to the prefix, computed once for the whole batch, and to
+// the keys that its own sequence holds. Softmax over the two together is the merge of its parts by their logsumexps (the identity of
+// section 3.1.1 between blocks), so the work is cut into items that know nothing of each other:
+//   * prefix items: rows of ALL sequences against a share of the prefix. A row is a (token, head of the group) pair, packed
+//     token * G + head; K and V of the prefix are read once per block of rows, not once per sequence.
+//   * own items: the rows of one sequence against a share of its own cache.
+// One launch does the items of both kinds, since the first are bound by the matrix units and the second by HBM; each leaves a
+// normalised partial O and its logsumexp, and a second launch merges them.
+//
+// Items of up to 32 rows (narrow) have one row tile, and the four wavefronts of a workgroup divide the keys; items of up to 128
+// rows (wide) give each wavefront 32 rows, and the four share the tiles of K and V in LDS.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "fa_kernels.h"
+#include "fa_lds.h"
+
+namespace fa {
+
+namespace {
+
+struct Item {
+  const __bf16 *K, *V;   // (already at the key/value head)
+  const int32_t* table;  // of this item's keys; nullptr: rows follow each other
+  int nk, begin, end;    // keys in all, and the share [begin, end), begin a multiple of 64
+  long tok0;             // token of packed row 0
+  int row0, rows;        // packed rows row0 .. row0 + rows - 1
+  int off;               // causal: row r sees keys up to r / G + off; else a bound past every key
+  bool causal;
+  int g, slot;
+};
+
+__device__ __forceinline__ const __bf16* item_rows(const PrefixArgs& a, const Item& it, const __bf16* pool, int key, long kstride) {
+  if (!it.table) return pool + (long)key * kstride;
+  const int page = it.table[key >> a.own.page_log2];
+  return pool + (((long)page << a.own.page_log2) + (key & ((1 << a.own.page_log2) - 1))) * kstride;
+}
+
+// Partial results of packed row r of an item
+__device__ __forceinline__ long item_row(const PrefixArgs& a, const Item& it, int r) {
+  const int row = it.row0 + r, q = row / a.G;
+  return (long)it.slot * a.nseq * a.Nq * a.Hq + (it.tok0 + q) * a.Hq + it.g * a.G + (row - q * a.G);
+}
+
+template <int D>
+constexpr int kPrefixLds = 4 * 2 * 32 * 2 * D + 2 * 4 * 32 * 4;  // narrow: two V tiles a wavefront, later partial O; m and l
+
+template <int D, bool F16>
+__device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it, char* smem) {
+  constexpr int NW = 4, KT = 32, KS = D / 16, DT = D / 32, ROWB = 2 * D, TILEB = KT * ROWB, WAVEB = 2 * TILEB, STAT_OFF = NW * WAVEB;
+  static_assert(WAVEB == D * 32 * 4 && STAT_OFF + 2 * NW * 32 * 4 <= kPrefixLds<D>, "the partial O^T of a wavefront takes the place of its V tiles");
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane & 31, hh = lane >> 5;
+  const long kstride = (long)a.Hkv * D;
+  const int prow = it.row0 + (lq < it.rows ? lq : it.rows - 1);  // (lanes past the end compute on a copy and store nothing)
+  const int q = prow / a.G;
+  bf16x8 Qf[KS];
+  {
+    const __bf16* qp = a.Q + ((it.tok0 + q) * a.Hq + it.g * a.G + (prow - q * a.G)) * D + 8 * hh;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) Qf[ks] = *(const bf16x8*)(qp + 16 * ks);
+  }
+  const int lim_row = it.causal && q + it.off < it.nk - 1 ? q + it.off : it.nk - 1;  // the last key of this lane's row
+  u32x4 Kr[2][KS];
+  char* const vbuf = smem + w * WAVEB;
+  auto issue = [&](int key0, auto BUF) {
+    constexpr int buf = decltype(BUF)::value;
+    const int last = it.end - 1 - key0;  // (rows past the end repeat the last one)
+    const __bf16* kp = item_rows(a, it, it.K, key0, kstride) + (long)(lq < last ? lq : last) * kstride + 8 * hh;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) Kr[buf][ks] = *(const u32x4*)(kp + 16 * ks);
+    tile_load_async<D, KT, 1>(vbuf + buf * TILEB, item_rows(a, it, it.V, key0, kstride), kstride, 0, last, 0, lane);
+  };
+  f32x16 O[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) O[dt] = (f32x16){0};
+  float m = -INFINITY, l = 0.f;
+  const float c2 = a.scale_log2e;
+  const int p16 = lane & 15, g16 = (lane >> 4) & 1;
+  int zcol[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) zcol[u] = swz_off<ROWB>(4 * hh + (p16 >> 2) + 8 * u, 2 * g16 + ((p16 & 3) >> 1)) + 8 * (p16 & 1);
+  auto compute = [&](int key0, auto BUF) {
+    constexpr int buf = decltype(BUF)::value;
+    f32x16 S = (f32x16){0};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) S = mfma32<F16>(__builtin_bit_cast(bf16x8, Kr[buf][ks]), Qf[ks], S);
+    if ((it.causal && key0 + KT - 1 > it.row0 / a.G + it.off) || key0 + KT > it.end) {
+      const int lim = (lim_row < it.end - 1 ? lim_row : it.end - 1) - key0 - 4 * hh;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) S[r] = acc_row(r, 0) > lim ? -INFINITY : S[r];
+    }
+    float mx = S[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, S[r]);
+    mx = max_with_partner32(mx);
+    const float m_new = fmaxf(m, mx);
+    const float alpha = m_new == -INFINITY ? 1.f : fast_exp2((m - m_new) * c2);
+    const float ref = m_new == -INFINITY ? 0.f : m_new * c2;
+    float rs = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      S[r] = fast_exp2(__builtin_fmaf(S[r], c2, -ref));
+      rs += S[r];
+    }
+    l = l * alpha + rs;
+    m = m_new;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) O[dt][r] *= alpha;
+    bf16x8 Pf[2] = {pack8<F16>(S, 0), pack8<F16>(S, 1)};
+    const int vb = w * WAVEB + buf * TILEB;
+#pragma unroll
+    for (int i = 0; i < 2 * DT; ++i) {
+      const int dt = i >> 1, ro = 16 * (i & 1) * ROWB;
+      O[dt] = mfma32<F16>(lds_tr_pair(smem, ((zcol[0] + vb) ^ (64 * dt)) + ro, ((zcol[1] + vb) ^ (64 * dt)) + ro), Pf[i & 1], O[dt]);
+    }
+  };
+  using B0 = std::integral_constant<int, 0>;
+  using B1 = std::integral_constant<int, 1>;
+  int t = it.begin + KT * w;
+  if (t < it.end) {
+    issue(t, B0{});
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) touch(Qf[ks]);
+    wait_vmem();
+    while (true) {
+      if (t + NW * KT < it.end) issue(t + NW * KT, B1{});
+      compute(t, B0{});
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (this tile has been read before its buffer is requested again)
+      wait_vmem();
+      if ((t += NW * KT) >= it.end) break;
+      if (t + NW * KT < it.end) issue(t + NW * KT, B0{});
+      compute(t, B1{});
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      wait_vmem();
+      if ((t += NW * KT) >= it.end) break;
+    }
+  }
+  // ---- the wavefronts' partial results become the item's
+  const float lsum = sum_with_partner32(l);
+  __syncthreads();
+  float* part = (float*)(smem + w * WAVEB);  // [d][row]
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) part[(32 * dt + acc_row(r, hh)) * 32 + lq] = O[dt][r];
+  float* stat = (float*)(smem + STAT_OFF);
+  if (hh == 0) {
+    stat[w * 32 + lq] = m;
+    stat[32 * NW + w * 32 + lq] = lsum;
+  }
+  __syncthreads();
+  constexpr int CPT = D / (2 * NW);  // columns of a thread
+  const int r = tid & 31, dg = tid >> 5;
+  float mm = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < NW; ++u) mm = fmaxf(mm, stat[u * 32 + r]);
+  float wgt[NW], den = 0.f;
+#pragma unroll
+  for (int u = 0; u < NW; ++u) {
+    const float mw = stat[u * 32 + r];
+    wgt[u] = mw == -INFINITY ? 0.f : fast_exp2((mw - mm) * c2);
+    den += wgt[u] * stat[32 * NW + u * 32 + r];
+  }
+  if (r >= it.rows) return;
+  const float inv = den > 0.f ? 1.f / den : 0.f;  // (no visible key: L = -inf, and the merge does not look at O)
+  const long at = item_row(a, it, r);
+  float* op = a.Opart + at * D + dg * CPT;
+#pragma unroll
+  for (int i = 0; i < CPT; i += 4) {
+    f32x4 o;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      float acc = 0.f;
+#pragma unroll
+      for (int u = 0; u < NW; ++u) acc += wgt[u] * ((const float*)(smem + u * WAVEB))[(dg * CPT + i + v) * 32 + r];
+      o[v] = acc * inv;
+    }
+    *(f32x4*)(op + i) = o;
+  }
+  if (dg == 0) a.Lpart[at] = den > 0.f ? mm * a.scale + fast_log2(den) * kLn2 : -INFINITY;
+}
+
+template <int D, bool F16>
+__device__ __forceinline__ void wide_item(const PrefixArgs& a, const Item& it, char* smem) {
+  constexpr int BC = 64, KS = D / 16, DT = D / 32, ROWB = 2 * D, TILEB = BC * ROWB, V_OFF = 2 * TILEB;
+  static_assert(4 * TILEB <= kPrefixLds<D>, "two stages of K and of V");
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane & 31, hh = lane >> 5;
+  const long kstride = (long)a.Hkv * D;
+  const int r0 = 32 * w, mine = r0 + lq;  // this lane's row of the item
+  const int prow = it.row0 + (mine < it.rows ? mine : it.rows - 1), q = prow / a.G;
+  bf16x8 Qf[KS];
+  {
+    const __bf16* qp = a.Q + ((it.tok0 + q) * a.Hq + it.g * a.G + (prow - q * a.G)) * D + 8 * hh;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) Qf[ks] = *(const bf16x8*)(qp + 16 * ks);
+  }
+  const int lim_row = it.causal && q + it.off < it.nk - 1 ? q + it.off : it.nk - 1;
+  const int lim_end = lim_row < it.end - 1 ? lim_row : it.end - 1;
+  const int lim_least = it.causal ? (it.row0 + r0) / a.G + it.off : it.end;  // keys up to here: seen by all rows of the wavefront
+  auto copy = [&](int key0, int buf) {
+    const int last = it.end - 1 - key0;
+    tile_load_async<D, BC, 4>(smem + buf * TILEB, item_rows(a, it, it.K, key0, kstride), kstride, 0, last, w, lane);
+    tile_load_async<D, BC, 4>(smem + V_OFF + buf * TILEB, item_rows(a, it, it.V, key0, kstride), kstride, 0, last, w, lane);
+  };
+  f32x16 O[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) O[dt] = (f32x16){0};
+  float m = -INFINITY, l = 0.f;
+  const float c2 = a.scale_log2e;
+  const int zrow = lq * ROWB + 16 * (hh ^ swz<ROWB>(lq));
+  const int p16 = lane & 15, g16 = (lane >> 4) & 1;
+  int zcol[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) zcol[u] = swz_off<ROWB>(4 * hh + (p16 >> 2) + 8 * u, 2 * g16 + ((p16 & 3) >> 1)) + 8 * (p16 & 1);
+  copy(it.begin, 0);
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) touch(Qf[ks]);
+  for (int key0 = it.begin, buf = 0; key0 < it.end; key0 += BC, buf ^= 1) {
+    wait_vmem();
+    lds_barrier();  // this tile has landed, everyone is done with the one before it
+    if (key0 + BC < it.end) copy(key0 + BC, buf ^ 1);
+    f32x16 S[2] = {(f32x16){0}, (f32x16){0}};
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        S[kt] = mfma32<F16>(lds_b128(smem, ((zrow + buf * TILEB) ^ (32 * ks)) + kt * 32 * ROWB), Qf[ks], S[kt]);
+    if (key0 + BC - 1 > lim_least || key0 + BC > it.end) mask_past(S, lim_end - key0 - 4 * hh);
+    // (the reference of the softmax is only advanced where some row's maximum has outgrown it: fa_common.h)
+    const float mx = row_maximum(S);
+    if (__builtin_amdgcn_ballot_w64((mx - m) * c2 > (float)kLazyLog2<F16> || (m == -INFINITY && mx != -INFINITY))) {
+      const float m_new = fmaxf(m, mx);
+      const float alpha = m_new == -INFINITY ? 1.f : fast_exp2((m - m_new) * c2);
+      l *= alpha;
+      m = m_new;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) O[dt][r] *= alpha;
+    }
+    bf16x8 P[2][2];
+    float rs0, rs1;
+    block_exponentials<F16>(S, c2, m == -INFINITY ? 0.f : -m * c2, P, rs0, rs1);
+    l += rs0 + rs1;
+#pragma unroll
+    for (int i = 0; i < 4 * DT; ++i) {
+      const int dt = i >> 2, ro = 16 * (i & 3) * ROWB, vb = V_OFF + buf * TILEB;
+      O[dt] = mfma32<F16>(lds_tr_pair(smem, ((zcol[0] + vb) ^ (64 * dt)) + ro, ((zcol[1] + vb) ^ (64 * dt)) + ro), P[(i >> 1) & 1][i & 1], O[dt]);
+    }
+  }
+  const float lsum = sum_with_partner32(l);
+  if (mine >= it.rows) return;
+  const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+  const long at = item_row(a, it, mine);
+  float* op = a.Opart + at * D + 4 * hh;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      f32x4 o;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) o[v] = O[dt][4 * r4 + v] * inv;
+      *(f32x4*)(op + 32 * dt + 8 * r4) = o;
+    }
+  if (hh == 0) a.Lpart[at] = lsum > 0.f ? m * a.scale + fast_log2(lsum) * kLn2 : -INFINITY;
+}
+
+__device__ __forceinline__ void empty_item(const PrefixArgs& a, const Item& it) {
+  for (int r = threadIdx.x; r < it.rows; r += 256) a.Lpart[item_row(a, it, r)] = -INFINITY;
+}
+
+// Share k of n keys cut into `shares`, in whole blocks of 64
+__device__ __forceinline__ void share_of(int n, int shares, int k, int& begin, int& end) {
+  const int per = ((n + 63) / 64 + shares - 1) / shares * 64;
+  const long b = (long)k * per;
+  begin = b < n ? (int)b : n;
+  end = n - begin < per ? n : begin + per;
+}
+
+template <int D, bool F16>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void prefix_items_kernel(PrefixArgs a, PrefixPlan plan, int prefix_items) {
+  __shared__ __attribute__((aligned(1024))) char smem[kPrefixLds<D>];
+  Item it;
+  const int i = blockIdx.x;
+  int rows, wide;
+  if (i < prefix_items) {
+    const int all = a.nseq * a.Nq * a.G, blocks = (all + plan.prefix_rows - 1) / plan.prefix_rows;
+    const int unit = i / blocks / kXcds * kXcds + i % kXcds, blk = i / kXcds % blocks;  // the blocks of rows of a share: on one XCD
+    if (unit >= a.Hkv * plan.prefix_shares) return;
+    it.g = unit / plan.prefix_shares;
+    it.slot = unit - it.g * plan.prefix_shares;
+    it.row0 = blk * plan.prefix_rows;
+    rows = all;
+    it.tok0 = 0;
+    it.nk = a.Np;
+    it.off = 0;
+    it.causal = false;
+    it.K = a.Kp + (long)it.g * D;
+    it.V = a.Vp + (long)it.g * D;
+    it.table = a.prefix_table;
+    share_of(it.nk, plan.prefix_shares, it.slot, it.begin, it.end);
+    wide = plan.prefix_rows;
+  } else {
+    const int j = i - prefix_items, blocks = (a.Nq * a.G + plan.own_rows - 1) / plan.own_rows, per = blocks * plan.own_shares;
+    const int pair = j / per, in = j - pair * per, s = pair / a.Hkv;
+    it.g = pair - s * a.Hkv;
+    it.slot = in % plan.own_shares;
+    it.row0 = in / plan.own_shares * plan.own_rows;
+    rows = a.Nq * a.G;
+    it.tok0 = (long)s * a.Nq;
+    it.nk = held_keys(a.own, s);
+    it.off = it.nk - a.Nq;
+    it.causal = a.causal != 0;
+    const long first = a.own.table ? 0 : (long)s * a.own.Nk * a.Hkv;
+    it.K = a.K + (first + it.g) * D;
+    it.V = a.V + (first + it.g) * D;
+    it.table = a.own.table ? a.own.table + (long)s * a.own.table_stride : nullptr;
+    share_of(it.nk, plan.own_shares, it.slot, it.begin, it.end);
+    it.slot += plan.prefix_shares;
+    wide = plan.own_rows;
+  }
+  it.rows = rows - it.row0 < wide ? rows - it.row0 : wide;
+  if (it.begin >= it.end) return empty_item(a, it);
+  if (wide == 32) narrow_item<D, F16>(a, it, smem);
+  else wide_item<D, F16>(a, it, smem);
+}
+
+// One thread per four elements of a (token, head) row.
+template <int D, bool F16>
+__global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixArgs a, int slots) {
+  constexpr int TPR = D / 4;
+  const long all = (long)a.nseq * a.Nq * a.Hq, r = (long)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+  if (r >= all) return;
+  const int c = threadIdx.x % TPR;
+  float mx = -INFINITY;
+  for (int k = 0; k < slots; ++k) mx = fmaxf(mx, a.Lpart[k * all + r]);
+  const long tok = r / a.Hq;
+  const int h = (int)(r - tok * a.Hq);
+  const long s = tok / a.Nq;
+  float* lse = a.LSE + (s * a.Hq + h) * a.Nq + (tok - s * a.Nq);
+  if (mx == -INFINITY) {  // no key anywhere
+    *(u32x2*)(a.O + r * D + 4 * c) = (u32x2){0u, 0u};
+    if (c == 0) *lse = -INFINITY;
+    return;
+  }
+  float z = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int k = 0; k < slots; ++k) {
+    const float l = a.Lpart[k * all + r];
+    if (l == -INFINITY) continue;
+    const float wgt = __expf(l - mx);
+    z += wgt;
+    acc += *(const f32x4*)(a.Opart + (k * all + r) * D + 4 * c) * wgt;
+  }
+  const float inv = 1.f / z;
+  u32x2 x;
+  x[0] = pack2<F16>(acc[0] * inv, acc[1] * inv);
+  x[1] = pack2<F16>(acc[2] * inv, acc[3] * inv);
+  *(u32x2*)(a.O + r * D + 4 * c) = x;
+  if (c == 0) *lse = mx + __logf(z);
+}
+
+template <int D, bool F16>
+hipError_t launch_prefix_d(const PrefixArgs& a, hipStream_t st) {
+  const PrefixPlan plan = prefix_plan(a.nseq, a.Hq, a.Hkv, a.Nq, a.Np, a.own.Nk, D);
+  const long all = (long)a.nseq * a.Nq * a.G, blocks = (all + plan.prefix_rows - 1) / plan.prefix_rows;
+  const long units = (long)a.Hkv * plan.prefix_shares, prefix = (units + kXcds - 1) / kXcds * kXcds * blocks;
+  const long own = (long)a.nseq * a.Hkv * (((long)a.Nq * a.G + plan.own_rows - 1) / plan.own_rows) * plan.own_shares;
+  if (prefix + own > 0x7fffffffL) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((prefix_items_kernel<D, F16>), dim3((unsigned)(prefix + own)), dim3(256), 0, st, a, plan, (int)prefix);
+  if (hipError_t e = hipGetLastError()) return e;
+  constexpr int RPB = 256 / (D / 4);
+  hipLaunchKernelGGL((prefix_merge_kernel<D, F16>), dim3((unsigned)(((long)a.nseq * a.Nq * a.Hq + RPB - 1) / RPB)), dim3(256), 0, st, a,
+                     plan.prefix_shares + plan.own_shares);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int d) {
+  PrefixPlan p;
+  const long G = Hq / Hkv, own_rows = Nq * G, all = B * own_rows;
+  auto clamp = [](long x, long lo, long hi) { return x < lo ? lo : (x > hi ? hi : x); };
+  p.prefix_rows = all <= 32 ? 32 : 128;
+  const long units = Hkv * ((all + p.prefix_rows - 1) / p.prefix_rows);
+  p.prefix_shares = Np == 0 ? 0 : (int)clamp(clamp((512 + units - 1) / units, 1, Np / 256), 1, 32);
+  p.own_rows = own_rows <= 64 ? 32 : 128;
+  const long pairs = B * Hkv * ((own_rows + p.own_rows - 1) / p.own_rows);
+  p.own_shares = (int)clamp(clamp(512 / pairs, 1, Nk / 256), 1, 32);
+  return p;
+}
+
+hipError_t launch_prefix(const PrefixArgs& a, int d, hipStream_t st) {
+  if (d == 64) return a.f16 ? launch_prefix_d<64, true>(a, st) : launch_prefix_d<64, false>(a, st);
+  return a.f16 ? launch_prefix_d<128, true>(a, st) : launch_prefix_d<128, false>(a, st);
+}
+
+}  // namespace fa
