@@ -25,11 +25,12 @@ struct FwdArgs {
   int page_log2, table_stride;
 };
 
-// Keys of sequence s in a cache with lengths of its own (a.seqlens_k is set).
-__device__ __forceinline__ int cache_length(const FwdArgs& a, int s) {
-  const int len = a.seqlens_k[s];
-  return len < 0 ? 0 : (len < a.p.Nk ? len : a.p.Nk);
+// Keys of sequence s in a cache of lengths `lens` (set), at most Nk.
+__device__ __forceinline__ int cache_length(const int32_t* lens, int Nk, int s) {
+  const int len = lens[s];
+  return len < 0 ? 0 : (len < Nk ? len : Nk);
 }
+__device__ __forceinline__ int cache_length(const FwdArgs& a, int s) { return cache_length(a.seqlens_k, a.p.Nk, s); }
 
 // Sequences of uneven cache lengths are handed out longest first: the workgroups of an XCD take
 // their (sequence, head) pairs in launch order, and a long sequence that starts last leaves the
@@ -42,13 +43,13 @@ constexpr int kRankMax = 128;
 struct CacheSequence {
   int s, len;  // the sequence, and its number of keys
 };
-__device__ __forceinline__ CacheSequence cache_sequence(const FwdArgs& a, int rank) {
-  const int nseq = a.p.nseq, lane = threadIdx.x & 63;
-  if (!a.seqlens_k) return {rank, a.p.Nk};
-  if (nseq <= 1 || nseq > kRankMax) return {rank, cache_length(a, rank)};
+__device__ __forceinline__ CacheSequence cache_sequence(const int32_t* lens, int Nk, int nseq, int rank) {
+  const int lane = threadIdx.x & 63;
+  if (!lens) return {rank, Nk};
+  if (nseq <= 1 || nseq > kRankMax) return {rank, cache_length(lens, Nk, rank)};
   static_assert(kRankMax == 128, "two candidates per lane, and seven bits of an index in a key");
   const int c0 = lane, c1 = 64 + lane;
-  const int len0 = cache_length(a, c0 < nseq ? c0 : 0), len1 = nseq > 64 ? cache_length(a, c1 < nseq ? c1 : 0) : 0;
+  const int len0 = cache_length(lens, Nk, c0 < nseq ? c0 : 0), len1 = nseq > 64 ? cache_length(lens, Nk, c1 < nseq ? c1 : 0) : 0;
   // (all keys differ, and a larger one goes first; where a length outgrows 25 bits the order is another one, but still an
   // order. Lanes without a sequence hold 0, which is larger than none.)
   const unsigned key0 = c0 < nseq ? ((unsigned)len0 << 7) | (unsigned)(127 - c0) : 0u;
@@ -73,6 +74,8 @@ __device__ __forceinline__ CacheSequence cache_sequence(const FwdArgs& a, int ra
   const int l = hit0 ? __builtin_ctzll(hit0) : (hit1 ? __builtin_ctzll(hit1) : 0);
   return {hit0 ? l : 64 + l, __builtin_amdgcn_readlane(hit0 ? len0 : len1, l)};
 }
+
+__device__ __forceinline__ CacheSequence cache_sequence(const FwdArgs& a, int rank) { return cache_sequence(a.seqlens_k, a.p.Nk, a.p.nseq, rank); }
 
 // Shares of the row-block split kernel, in blocks of 64 keys: a sequence of `ncol` blocks is cut into at
 // most nsplit equal shares, the same number for every length (shares of one size, of which a short
@@ -167,8 +170,8 @@ struct PrefixArgs {
   float scale, scale_log2e;
 };
 struct PrefixPlan {  // how the prefix and the own keys are cut (a function of the sizes alone)
-  int prefix_rows, prefix_shares;  // packed rows of a workgroup, shares of the prefix
-  int own_rows, own_shares;
+  int prefix_rows, prefix_keys, prefix_shares;  // packed rows and keys of an item, how many shares of the keys that makes
+  int own_rows, own_keys, own_shares;
 };
 PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int d);
 hipError_t launch_prefix(const PrefixArgs& a, int d, hipStream_t st);

@@ -63,13 +63,26 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
   const int lim_row = it.causal && q + it.off < it.nk - 1 ? q + it.off : it.nk - 1;  // the last key of this lane's row
   u32x4 Kr[2][KS];
   char* const vbuf = smem + w * WAVEB;
+  // Pages of this wavefront's tiles: lane i has the one of tile i of the next 64 (looked up one by one each would be a memory latency
+  // in front of its tile's requests).
+  const int mask = (1 << a.own.page_log2) - 1;
+  int pages = 0;
   auto issue = [&](int key0, auto BUF) {
     constexpr int buf = decltype(BUF)::value;
     const int last = it.end - 1 - key0;  // (rows past the end repeat the last one)
-    const __bf16* kp = item_rows(a, it, it.K, key0, kstride) + (long)(lq < last ? lq : last) * kstride + 8 * hh;
+    long row = key0;
+    if (it.table) {
+      const int i = (key0 - it.begin) / (NW * KT) & 63;
+      if (i == 0) {
+        const int t = key0 + lane * (NW * KT);
+        pages = it.table[(t < it.end ? t : key0) >> a.own.page_log2];
+      }
+      row = ((long)__builtin_amdgcn_readlane(pages, i) << a.own.page_log2) + (key0 & mask);
+    }
+    const __bf16* kp = it.K + (row + (lq < last ? lq : last)) * kstride + 8 * hh;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) Kr[buf][ks] = *(const u32x4*)(kp + 16 * ks);
-    tile_load_async<D, KT, 1>(vbuf + buf * TILEB, item_rows(a, it, it.V, key0, kstride), kstride, 0, last, 0, lane);
+    tile_load_async<D, KT, 1>(vbuf + buf * TILEB, it.V + row * kstride, kstride, 0, last, 0, lane);
   };
   f32x16 O[DT];
 #pragma unroll
@@ -94,21 +107,25 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
 #pragma unroll
     for (int r = 1; r < 16; ++r) mx = fmaxf(mx, S[r]);
     mx = max_with_partner32(mx);
-    const float m_new = fmaxf(m, mx);
-    const float alpha = m_new == -INFINITY ? 1.f : fast_exp2((m - m_new) * c2);
-    const float ref = m_new == -INFINITY ? 0.f : m_new * c2;
+    // (the reference of the softmax is only advanced where some row's maximum has outgrown it: fa_common.h)
+    if (__builtin_amdgcn_ballot_w64((mx - m) * c2 > (float)kLazyLog2<F16> || (m == -INFINITY && mx != -INFINITY))) {
+      const float m_new = fmaxf(m, mx);
+      const float alpha = m_new == -INFINITY ? 1.f : fast_exp2((m - m_new) * c2);
+      l *= alpha;
+      m = m_new;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) O[dt][r] *= alpha;
+    }
+    const float ref = m == -INFINITY ? 0.f : m * c2;
     float rs = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       S[r] = fast_exp2(__builtin_fmaf(S[r], c2, -ref));
       rs += S[r];
     }
-    l = l * alpha + rs;
-    m = m_new;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) O[dt][r] *= alpha;
+    l += rs;
     bf16x8 Pf[2] = {pack8<F16>(S, 0), pack8<F16>(S, 1)};
     const int vb = w * WAVEB + buf * TILEB;
 #pragma unroll
@@ -122,11 +139,14 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
   int t = it.begin + KT * w;
   if (t < it.end) {
     issue(t, B0{});
+    if (t + NW * KT < it.end) issue(t + NW * KT, B1{});  // (short shares hold no more, and wait once)
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) touch(Qf[ks]);
     wait_vmem();
+    bool here = true;
     while (true) {
-      if (t + NW * KT < it.end) issue(t + NW * KT, B1{});
+      if (!here && t + NW * KT < it.end) issue(t + NW * KT, B1{});
+      here = false;
       compute(t, B0{});
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (this tile has been read before its buffer is requested again)
       wait_vmem();
@@ -141,46 +161,42 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
   // ---- the wavefronts' partial results become the item's
   const float lsum = sum_with_partner32(l);
   __syncthreads();
-  float* part = (float*)(smem + w * WAVEB);  // [d][row]
+  // [d][row], the rows turned by d / 4 places: rows are written, and pieces of four columns read, without bank conflicts
+  float* part = (float*)(smem + w * WAVEB);
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) part[(32 * dt + acc_row(r, hh)) * 32 + lq] = O[dt][r];
+    for (int r = 0; r < 16; ++r) {
+      const int c = 32 * dt + acc_row(r, hh);
+      part[c * 32 + ((lq + c / 4) & 31)] = O[dt][r];
+    }
   float* stat = (float*)(smem + STAT_OFF);
   if (hh == 0) {
     stat[w * 32 + lq] = m;
     stat[32 * NW + w * 32 + lq] = lsum;
   }
   __syncthreads();
-  constexpr int CPT = D / (2 * NW);  // columns of a thread
-  const int r = tid & 31, dg = tid >> 5;
-  float mm = -INFINITY;
+  constexpr int CPR = D / 4;  // pieces of a row
+  for (int i = tid; i < it.rows * CPR; i += 64 * NW) {
+    const int r = i / CPR, c = i % CPR;
+    float mm = -INFINITY;
 #pragma unroll
-  for (int u = 0; u < NW; ++u) mm = fmaxf(mm, stat[u * 32 + r]);
-  float wgt[NW], den = 0.f;
+    for (int u = 0; u < NW; ++u) mm = fmaxf(mm, stat[u * 32 + r]);
+    float den = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int u = 0; u < NW; ++u) {
-    const float mw = stat[u * 32 + r];
-    wgt[u] = mw == -INFINITY ? 0.f : fast_exp2((mw - mm) * c2);
-    den += wgt[u] * stat[32 * NW + u * 32 + r];
-  }
-  if (r >= it.rows) return;
-  const float inv = den > 0.f ? 1.f / den : 0.f;  // (no visible key: L = -inf, and the merge does not look at O)
-  const long at = item_row(a, it, r);
-  float* op = a.Opart + at * D + dg * CPT;
+    for (int u = 0; u < NW; ++u) {
+      const float mw = stat[u * 32 + r], wgt = mw == -INFINITY ? 0.f : fast_exp2((mw - mm) * c2);
+      den += wgt * stat[32 * NW + u * 32 + r];
+      const float* x = (const float*)(smem + u * WAVEB) + 4 * c * 32 + ((r + c) & 31);
 #pragma unroll
-  for (int i = 0; i < CPT; i += 4) {
-    f32x4 o;
-#pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      float acc = 0.f;
-#pragma unroll
-      for (int u = 0; u < NW; ++u) acc += wgt[u] * ((const float*)(smem + u * WAVEB))[(dg * CPT + i + v) * 32 + r];
-      o[v] = acc * inv;
+      for (int v = 0; v < 4; ++v) o[v] += wgt * x[32 * v];
     }
-    *(f32x4*)(op + i) = o;
+    const float inv = den > 0.f ? 1.f / den : 0.f;  // (no visible key: L = -inf, and the merge does not look at O)
+    const long at = item_row(a, it, r);
+    *(f32x4*)(a.Opart + at * D + 4 * c) = o * inv;
+    if (c == 0) a.Lpart[at] = den > 0.f ? mm * a.scale + fast_log2(den) * kLn2 : -INFINITY;
   }
-  if (dg == 0) a.Lpart[at] = den > 0.f ? mm * a.scale + fast_log2(den) * kLn2 : -INFINITY;
 }
 
 template <int D, bool F16>
@@ -191,20 +207,25 @@ __device__ __forceinline__ void wide_item(const PrefixArgs& a, const Item& it, c
   const long kstride = (long)a.Hkv * D;
   const int r0 = 32 * w, mine = r0 + lq;  // this lane's row of the item
   const int prow = it.row0 + (mine < it.rows ? mine : it.rows - 1), q = prow / a.G;
+  TileCopier<BC, ROWB> copier;
+  copier.init(kstride, w, lane);
+  constexpr int CPT = TileCopier<BC, ROWB>::COPIES, AHEAD = 4;
+  auto copy = [&](const __bf16* pool, int key0, int to) {
+    const auto plan = copier.plan(item_rows(a, it, pool, key0, kstride), it.end - 1 - key0);
+    static_for<CPT>([&](auto Q) { copier.template copy<Q.value>(plan, smem + to); });
+  };
+  copy(it.K, it.begin, 0);
   bf16x8 Qf[KS];
   {
     const __bf16* qp = a.Q + ((it.tok0 + q) * a.Hq + it.g * a.G + (prow - q * a.G)) * D + 8 * hh;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) Qf[ks] = *(const bf16x8*)(qp + 16 * ks);
   }
+  copy(it.V, it.begin, V_OFF);
+  if (it.begin + BC < it.end) copy(it.K, it.begin + BC, TILEB);
   const int lim_row = it.causal && q + it.off < it.nk - 1 ? q + it.off : it.nk - 1;
   const int lim_end = lim_row < it.end - 1 ? lim_row : it.end - 1;
   const int lim_least = it.causal ? (it.row0 + r0) / a.G + it.off : it.end;  // keys up to here: seen by all rows of the wavefront
-  auto copy = [&](int key0, int buf) {
-    const int last = it.end - 1 - key0;
-    tile_load_async<D, BC, 4>(smem + buf * TILEB, item_rows(a, it, it.K, key0, kstride), kstride, 0, last, w, lane);
-    tile_load_async<D, BC, 4>(smem + V_OFF + buf * TILEB, item_rows(a, it, it.V, key0, kstride), kstride, 0, last, w, lane);
-  };
   f32x16 O[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) O[dt] = (f32x16){0};
@@ -215,24 +236,57 @@ __device__ __forceinline__ void wide_item(const PrefixArgs& a, const Item& it, c
   int zcol[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) zcol[u] = swz_off<ROWB>(4 * hh + (p16 >> 2) + 8 * u, 2 * g16 + ((p16 & 3) >> 1)) + 8 * (p16 & 1);
-  copy(it.begin, 0);
+  auto scores = [&](f32x16 (&S)[2], int buf) {
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) touch(Qf[ks]);
-  for (int key0 = it.begin, buf = 0; key0 < it.end; key0 += BC, buf ^= 1) {
-    wait_vmem();
-    lds_barrier();  // this tile has landed, everyone is done with the one before it
-    if (key0 + BC < it.end) copy(key0 + BC, buf ^ 1);
-    f32x16 S[2] = {(f32x16){0}, (f32x16){0}};
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
+    for (int kt = 0; kt < 2; ++kt) {
+      S[kt] = (f32x16){0};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
         S[kt] = mfma32<F16>(lds_b128(smem, ((zrow + buf * TILEB) ^ (32 * ks)) + kt * 32 * ROWB), Qf[ks], S[kt]);
-    if (key0 + BC - 1 > lim_least || key0 + BC > it.end) mask_past(S, lim_end - key0 - 4 * hh);
-    // (the reference of the softmax is only advanced where some row's maximum has outgrown it: fa_common.h)
-    const float mx = row_maximum(S);
-    if (__builtin_amdgcn_ballot_w64((mx - m) * c2 > (float)kLazyLog2<F16> || (m == -INFINITY && mx != -INFINITY))) {
-      const float m_new = fmaxf(m, mx);
+    }
+  };
+  auto mask = [&](f32x16 (&S)[2], int key0) {
+    if (key0 + BC - 1 > lim_least || key0 + BC > it.end) {
+      asm volatile("; keep this a branch" ::);
+      mask_past(S, lim_end - key0 - 4 * hh);
+    }
+  };
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) touch(Qf[ks]);
+  if (it.begin + BC < it.end) wait_vmem_upto<2 * CPT>();
+  else wait_vmem_upto<CPT>();
+  lds_barrier();
+  f32x16 Sa[2], Sb[2];
+  scores(Sa, 0);
+  mask(Sa, it.begin);
+  m = row_maximum(Sa);
+  // Iteration of the block at key0 (stage `buf`): the scores of the next block are formed beside the exponentials of this one, then O
+  // is updated. K of the block after the next and V of the next are on their way meanwhile.
+  auto iteration = [&](int key0, auto BUF, f32x16 (&S)[2], f32x16 (&Sn)[2]) {
+    constexpr int buf = decltype(BUF)::value;
+    const bool next = key0 + BC < it.end;
+    wait_vmem();
+    lds_barrier();
+    if (next) {
+      copy(it.V, key0 + BC, V_OFF + (buf ^ 1) * TILEB);
+      if (key0 + 2 * BC < it.end) copy(it.K, key0 + 2 * BC, buf * TILEB);
+    }
+    bf16x8 P[2][2];
+    float rs0, rs1;
+    const float ref = m == -INFINITY ? 0.f : -m * c2;
+    __builtin_amdgcn_sched_barrier(0);
+    scores(Sn, buf ^ 1);  // (past the end: of whatever is there, and not used)
+    block_exponentials<F16>(S, c2, ref, P, rs0, rs1);
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+    for (int i = 0; i < 2 * KS; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 8 * 16 / (2 * KS), 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (reference_outgrown<F16>(rs0 + rs1) || __builtin_amdgcn_ballot_w64(m == -INFINITY)) {
+      const float m_new = fmaxf(m, row_maximum(S));
       const float alpha = m_new == -INFINITY ? 1.f : fast_exp2((m - m_new) * c2);
       l *= alpha;
       m = m_new;
@@ -240,22 +294,32 @@ __device__ __forceinline__ void wide_item(const PrefixArgs& a, const Item& it, c
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) O[dt][r] *= alpha;
+      block_exponentials<F16>(S, c2, m == -INFINITY ? 0.f : -m * c2, P, rs0, rs1);
     }
-    bf16x8 P[2][2];
-    float rs0, rs1;
-    block_exponentials<F16>(S, c2, m == -INFINITY ? 0.f : -m * c2, P, rs0, rs1);
     l += rs0 + rs1;
-#pragma unroll
-    for (int i = 0; i < 4 * DT; ++i) {
-      const int dt = i >> 2, ro = 16 * (i & 3) * ROWB, vb = V_OFF + buf * TILEB;
-      O[dt] = mfma32<F16>(lds_tr_pair(smem, ((zcol[0] + vb) ^ (64 * dt)) + ro, ((zcol[1] + vb) ^ (64 * dt)) + ro), P[(i >> 1) & 1][i & 1], O[dt]);
-    }
+    __builtin_amdgcn_sched_barrier(0);
+    mfma_stream<4 * DT, AHEAD, 2>(
+        [&](int i) {
+          const int dt = i >> 2, ro = 16 * (i & 3) * ROWB, vb = V_OFF + buf * TILEB;
+          return lds_tr_pair(smem, ((zcol[0] + vb) ^ (64 * dt)) + ro, ((zcol[1] + vb) ^ (64 * dt)) + ro);
+        },
+        [&](int i, const bf16x8& v) { O[i >> 2] = mfma32<F16>(v, P[(i >> 1) & 1][i & 1], O[i >> 2]); });
+    if (next) mask(Sn, key0 + BC);
+  };
+  using B0 = std::integral_constant<int, 0>;
+  using B1 = std::integral_constant<int, 1>;
+  for (int key0 = it.begin;;) {
+    iteration(key0, B0{}, Sa, Sb);
+    if ((key0 += BC) >= it.end) break;
+    iteration(key0, B1{}, Sb, Sa);
+    if ((key0 += BC) >= it.end) break;
   }
+  // ---- through LDS, so that whole rows are stored (16 bytes a row and instruction straight from the accumulators took 1 us per MB)
   const float lsum = sum_with_partner32(l);
-  if (mine >= it.rows) return;
   const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
-  const long at = item_row(a, it, mine);
-  float* op = a.Opart + at * D + 4 * hh;
+  lds_barrier();  // everyone has read the last tiles
+  constexpr int CPR = D / 4;  // 16-byte chunks of a row
+  char* const stage = smem + w * (32 * 4 * D);
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -263,18 +327,23 @@ __device__ __forceinline__ void wide_item(const PrefixArgs& a, const Item& it, c
       f32x4 o;
 #pragma unroll
       for (int v = 0; v < 4; ++v) o[v] = O[dt][4 * r4 + v] * inv;
-      *(f32x4*)(op + 32 * dt + 8 * r4) = o;
+      *(f32x4*)(stage + lq * (4 * D) + 16 * ((8 * dt + 2 * r4 + hh) ^ (lq & (CPR - 1)))) = o;
     }
-  if (hh == 0) a.Lpart[at] = lsum > 0.f ? m * a.scale + fast_log2(lsum) * kLn2 : -INFINITY;
+#pragma unroll 4
+  for (int i = 0; i < CPR / 2; ++i) {
+    const int r = (64 * i + lane) / CPR, c = lane & (CPR - 1);
+    const f32x4 o = *(const f32x4*)(stage + r * (4 * D) + 16 * (c ^ (r & (CPR - 1))));
+    if (r0 + r < it.rows) *(f32x4*)(a.Opart + item_row(a, it, r0 + r) * D + 4 * c) = o;
+  }
+  if (hh == 0 && mine < it.rows) a.Lpart[item_row(a, it, mine)] = lsum > 0.f ? m * a.scale + fast_log2(lsum) * kLn2 : -INFINITY;
 }
 
 __device__ __forceinline__ void empty_item(const PrefixArgs& a, const Item& it) {
   for (int r = threadIdx.x; r < it.rows; r += 256) a.Lpart[item_row(a, it, r)] = -INFINITY;
 }
 
-// Share k of n keys cut into `shares`, in whole blocks of 64
-__device__ __forceinline__ void share_of(int n, int shares, int k, int& begin, int& end) {
-  const int per = ((n + 63) / 64 + shares - 1) / shares * 64;
+// Share k of n keys cut into shares of `per` (a multiple of 64)
+__device__ __forceinline__ void share_of(int n, int per, int k, int& begin, int& end) {
   const long b = (long)k * per;
   begin = b < n ? (int)b : n;
   end = n - begin < per ? n : begin + per;
@@ -301,24 +370,27 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     it.K = a.Kp + (long)it.g * D;
     it.V = a.Vp + (long)it.g * D;
     it.table = a.prefix_table;
-    share_of(it.nk, plan.prefix_shares, it.slot, it.begin, it.end);
+    share_of(it.nk, plan.prefix_keys, it.slot, it.begin, it.end);
     wide = plan.prefix_rows;
   } else {
     const int j = i - prefix_items, blocks = (a.Nq * a.G + plan.own_rows - 1) / plan.own_rows, per = blocks * plan.own_shares;
-    const int pair = j / per, in = j - pair * per, s = pair / a.Hkv;
-    it.g = pair - s * a.Hkv;
+    // (sequences of uneven lengths: longest first)
+    const int pair = j / per, in = j - pair * per, rank = pair / a.Hkv;
+    const CacheSequence cs = cache_sequence(a.own.lens, a.own.Nk, a.nseq, rank);
+    const int s = cs.s;
+    it.g = pair - rank * a.Hkv;
     it.slot = in % plan.own_shares;
     it.row0 = in / plan.own_shares * plan.own_rows;
     rows = a.Nq * a.G;
     it.tok0 = (long)s * a.Nq;
-    it.nk = held_keys(a.own, s);
+    it.nk = cs.len;
     it.off = it.nk - a.Nq;
     it.causal = a.causal != 0;
     const long first = a.own.table ? 0 : (long)s * a.own.Nk * a.Hkv;
     it.K = a.K + (first + it.g) * D;
     it.V = a.V + (first + it.g) * D;
     it.table = a.own.table ? a.own.table + (long)s * a.own.table_stride : nullptr;
-    share_of(it.nk, plan.own_shares, it.slot, it.begin, it.end);
+    share_of(it.nk, plan.own_keys, it.slot, it.begin, it.end);
     it.slot += plan.prefix_shares;
     wide = plan.own_rows;
   }
@@ -328,15 +400,27 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   else wide_item<D, F16>(a, it, smem);
 }
 
-// One thread per four elements of a (token, head) row.
-template <int D, bool F16>
+// One thread per four elements of a (token, head) row. Few threads a row and a handful of slots: the time is the chain of loads, so
+// the logsumexps and partial rows of FLY slots are requested together, and where there are no more than that none is read twice.
+// (A slot without keys for this row has written no partial O: what is read in its place is not used.)
+template <int D, bool F16, int FLY>
 __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixArgs a, int slots) {
   constexpr int TPR = D / 4;
   const long all = (long)a.nseq * a.Nq * a.Hq, r = (long)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
   if (r >= all) return;
   const int c = threadIdx.x % TPR;
-  float mx = -INFINITY;
-  for (int k = 0; k < slots; ++k) mx = fmaxf(mx, a.Lpart[k * all + r]);
+  float l[FLY], mx = -INFINITY;
+  f32x4 o[FLY];
+  auto request = [&](int k0) {
+#pragma unroll
+    for (int u = 0; u < FLY; ++u) l[u] = a.Lpart[(k0 + u < slots ? k0 + u : slots - 1) * all + r];
+#pragma unroll
+    for (int u = 0; u < FLY; ++u) o[u] = *(const f32x4*)(a.Opart + ((k0 + u < slots ? k0 + u : slots - 1) * all + r) * D + 4 * c);
+  };
+  request(0);
+  for (int k = FLY; k < slots; ++k) mx = fmaxf(mx, a.Lpart[k * all + r]);
+#pragma unroll
+  for (int u = 0; u < FLY; ++u) mx = fmaxf(mx, l[u]);
   const long tok = r / a.Hq;
   const int h = (int)(r - tok * a.Hq);
   const long s = tok / a.Nq;
@@ -348,12 +432,16 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixArgs a, int slo
   }
   float z = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int k = 0; k < slots; ++k) {
-    const float l = a.Lpart[k * all + r];
-    if (l == -INFINITY) continue;
-    const float wgt = __expf(l - mx);
-    z += wgt;
-    acc += *(const f32x4*)(a.Opart + (k * all + r) * D + 4 * c) * wgt;
+  for (int k0 = 0;;) {
+#pragma unroll
+    for (int u = 0; u < FLY; ++u) {
+      if (k0 + u >= slots || l[u] == -INFINITY) continue;
+      const float wgt = __expf(l[u] - mx);
+      z += wgt;
+      acc += o[u] * wgt;
+    }
+    if ((k0 += FLY) >= slots) break;
+    request(k0);
   }
   const float inv = 1.f / z;
   u32x2 x;
@@ -373,8 +461,11 @@ hipError_t launch_prefix_d(const PrefixArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((prefix_items_kernel<D, F16>), dim3((unsigned)(prefix + own)), dim3(256), 0, st, a, plan, (int)prefix);
   if (hipError_t e = hipGetLastError()) return e;
   constexpr int RPB = 256 / (D / 4);
-  hipLaunchKernelGGL((prefix_merge_kernel<D, F16>), dim3((unsigned)(((long)a.nseq * a.Nq * a.Hq + RPB - 1) / RPB)), dim3(256), 0, st, a,
-                     plan.prefix_shares + plan.own_shares);
+  const int slots = plan.prefix_shares + plan.own_shares;
+  const dim3 grid((unsigned)(((long)a.nseq * a.Nq * a.Hq + RPB - 1) / RPB));
+  if (slots <= 4) hipLaunchKernelGGL((prefix_merge_kernel<D, F16, 4>), grid, dim3(256), 0, st, a, slots);
+  else if (slots <= 9) hipLaunchKernelGGL((prefix_merge_kernel<D, F16, 9>), grid, dim3(256), 0, st, a, slots);
+  else hipLaunchKernelGGL((prefix_merge_kernel<D, F16, 17>), grid, dim3(256), 0, st, a, slots);
   return hipGetLastError();
 }
 
@@ -384,12 +475,25 @@ PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int d) {
   PrefixPlan p;
   const long G = Hq / Hkv, own_rows = Nq * G, all = B * own_rows;
   auto clamp = [](long x, long lo, long hi) { return x < lo ? lo : (x > hi ? hi : x); };
+  auto up = [](long x, long y) { return (x + y - 1) / y; };
+  // shares of `keys`, at most `most` of them and none below `least` keys
+  auto cut = [&](long keys, long most, long least, int& share, int& shares) {
+    const long per = clamp(up(up(keys, 64), most < 1 ? 1 : most), least / 64, 1l << 24);
+    share = (int)(64 * per);
+    shares = (int)up(keys, 64 * per);
+  };
   p.prefix_rows = all <= 32 ? 32 : 128;
-  const long units = Hkv * ((all + p.prefix_rows - 1) / p.prefix_rows);
-  p.prefix_shares = Np == 0 ? 0 : (int)clamp(clamp((512 + units - 1) / units, 1, Np / 256), 1, 32);
+  const long units = Hkv * up(all, p.prefix_rows);
+  // Half as many prefix items as compute units, or shares of 1024 keys where that makes more of them, up to one a unit (64 sequences,
+  // 32 heads on 8 of 128, 8192 shared keys, us at 4 / 6 / 8 / 12 shares, 16 blocks of rows: 60 / 51 / 49 / 53; 16 x 5 rows, 16 heads of 64,
+  // 12345 keys, 16 blocks, at 6 / 8 / 12: 46 / 40 / 36)
+  const long most = clamp(up(128, units), clamp(Np / 1024, 1, up(256, units)), 16);
+  cut(Np, most, 256, p.prefix_keys, p.prefix_shares);
   p.own_rows = own_rows <= 64 ? 32 : 128;
-  const long pairs = B * Hkv * ((own_rows + p.own_rows - 1) / p.own_rows);
-  p.own_shares = (int)clamp(clamp(512 / pairs, 1, Nk / 256), 1, 32);
+  // Own items: with those of the prefix no more than fit on the chip at once, two a compute unit (64 x 8 pairs of up to 1024 keys beside
+  // 128 prefix items, one and two shares: 49 and 58 us; 16 x 16 pairs of up to 2048 of 64, beside 128: 40 and 43)
+  const long pairs = B * Hkv * up(own_rows, p.own_rows);
+  cut(Nk, clamp((512 - units * p.prefix_shares) / pairs, 1, 8), 256, p.own_keys, p.own_shares);
   return p;
 }
 
