@@ -6,9 +6,10 @@
 // summed to draw is held in float64, whatever order it is summed in. The target's logits need their normaliser first: row maxima
 // and float32 sums over all rows settle which drafts are accepted; the one row that is drawn from is then summed once more in float64.
 //
-//   stats   (logits) maximum and sum of every row, in chunks of kChunk tokens
-//   sums    per sequence: which drafts are accepted; float64 sums of every chunk of the row that is drawn from
-//   draw    per sequence: the chunk in which the running sum passes, then the token in it
+//   stats   (logits) maximum and sum of every row, in segments of kSegment tokens, one a wavefront: bound by HBM
+//   sums    per sequence: which drafts are accepted (every workgroup finds out for itself: cheaper than a launch); float64 sums of
+//           the segments of the row that is drawn from
+//   draw    per sequence: the segment in which the running sum passes, then the token in it: a chain of latencies
 #include <hip/hip_runtime.h>
 
 #include "../../include/fa.h"
@@ -16,223 +17,366 @@
 
 namespace fa {
 
-constexpr int kChunk = 4096, kVerifyThreads = 256, kPer = kChunk / kVerifyThreads;
+constexpr int kSegment = 2048, kVerifyThreads = 256, kVerifyWaves = kVerifyThreads / 64;
+constexpr int kPieces = kSegment / 64 / 8;  // pieces of eight tokens of a lane: (64 i + lane) of the segment
 
-struct ChunkSums {
-  // p: sum of the row's weights. above, drafts: sums of p and of q over the tokens where p > q. For logits p and above are sums of
-  // exp(inv_t (l - maximum)), to be divided by the row's whole sum.
+struct SegmentSums {
+  // p: sum of the segment's weights. above, drafts: sums of p and of q over its tokens with p > q. For logits p and above are sums
+  // of exp(inv_t (l - maximum)), to be divided by the row's whole sum.
   double p, above, drafts;
 };
 struct RowPart {
   float max, sum;
 };
-__host__ __device__ inline int chunks_of(int V) { return (V + kChunk - 1) / kChunk; }
+__host__ __device__ inline int segments_of(int V) { return (V + kSegment - 1) / kSegment; }
+
+// What the drafted token of a row has: the target's value, the draft model's probability (less than 0: there is no such token).
+struct Picked {
+  float target, draft;
+};
 
 size_t verify_workspace(int B, int k, int V) {
-  return (size_t)B * chunks_of(V) * (sizeof(ChunkSums) + (size_t)(k + 1) * sizeof(RowPart));
+  return (size_t)B * (segments_of(V) * (sizeof(SegmentSums) + (size_t)(k + 1) * sizeof(RowPart)) + (size_t)(k + 1) * sizeof(Picked));
 }
-__device__ __forceinline__ ChunkSums* chunk_sums(const VerifyArgs& a, int b) { return (ChunkSums*)a.ws + (long)b * chunks_of(a.V); }
+__device__ __forceinline__ SegmentSums* segment_sums(const VerifyArgs& a, long b) { return (SegmentSums*)a.ws + b * segments_of(a.V); }
 __device__ __forceinline__ RowPart* row_parts(const VerifyArgs& a, long row) {
-  const int n = chunks_of(a.V);
-  return (RowPart*)((ChunkSums*)a.ws + (long)a.nseq * n) + row * n;
+  const int n = segments_of(a.V);
+  return (RowPart*)((SegmentSums*)a.ws + (long)a.nseq * n) + row * n;
 }
+__device__ __forceinline__ Picked* picked(const VerifyArgs& a) { return (Picked*)row_parts(a, (long)a.nseq * (a.k + 1)); }
 
 __device__ __forceinline__ float element(const void* p, int type, long i) {
   if (type == FA_TYPE_F32) return ((const float*)p)[i];
   if (type == FA_TYPE_BF16) return (float)((const __bf16*)p)[i];
   return (float)((const _Float16*)p)[i];
 }
+// Eight values from element i on, those from `n` on replaced by `none`. (16-byte loads at any element's address: rows may begin anywhere.)
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef __bf16 bf16x8_any __attribute__((ext_vector_type(8), aligned(2)));
+typedef _Float16 f16x8_any __attribute__((ext_vector_type(8), aligned(2)));
+__device__ __forceinline__ void eight(const void* p, int type, long i, int n, float none, float (&x)[8]) {
+  if (n >= 8) {
+    if (type == FA_TYPE_F32) {
+      const f32x4_any lo = *(const f32x4_any*)((const float*)p + i), hi = *(const f32x4_any*)((const float*)p + i + 4);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = u < 4 ? lo[u & 3] : hi[u & 3];
+    } else if (type == FA_TYPE_BF16) {
+      const bf16x8_any v = *(const bf16x8_any*)((const __bf16*)p + i);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = (float)v[u];
+    } else {
+      const f16x8_any v = *(const f16x8_any*)((const _Float16*)p + i);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = (float)v[u];
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[u] = u < n ? element(p, type, i + u) : none;
+  }
+}
 
-template <class T>
-__device__ __forceinline__ T block_reduce(T x, T* lds, T (*op)(T, T)) {  // the same value in every thread
-  for (int o = 32; o; o >>= 1) x = op(x, __shfl_xor(x, o));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
-  __syncthreads();
-  x = lds[0];
-  for (int i = 1; i < kVerifyThreads / 64; ++i) x = op(x, lds[i]);
+__device__ __forceinline__ float wave_max(float x) {
+  for (int o = 32; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
   return x;
 }
 template <class T>
-__device__ T add(T a, T b) {
-  return a + b;
+__device__ __forceinline__ T wave_add(T x) {
+  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+  return x;
 }
-__device__ float larger(float a, float b) { return fmaxf(a, b); }
-
-__global__ __launch_bounds__(kVerifyThreads) void verify_stats_kernel(VerifyArgs a) {
-  __shared__ float lds[kVerifyThreads / 64];
-  const long row = blockIdx.x;
-  const int c0 = blockIdx.y * kChunk, end = a.V < c0 + kChunk ? a.V : c0 + kChunk;
-  const float t2 = a.inv_t * kLog2e;
-  float x[kPer], m = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int j = c0 + i * kVerifyThreads + threadIdx.x;
-    x[i] = j < end ? element(a.target, a.target_type, row * a.target_stride + j) : -INFINITY;
-    m = fmaxf(m, x[i]);
+template <class T>
+__device__ __forceinline__ T wave_scan(T x) {  // sum of the lanes up to this one
+  const int lane = threadIdx.x & 63;
+  for (int o = 1; o < 64; o <<= 1) {
+    const T y = __shfl_up(x, o);
+    if (lane >= o) x += y;
   }
-  m = block_reduce(m, lds, larger);
-  float z = 0.f;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) z += x[i] == -INFINITY ? 0.f : fast_exp2((x[i] - m) * t2);
-  z = block_reduce(z, lds, add<float>);
-  if (threadIdx.x == 0) row_parts(a, row)[blockIdx.y] = {m, z};
+  return x;
 }
 
-// Maximum of a row, and its sum against it.
-__device__ __forceinline__ RowPart whole_row(const VerifyArgs& a, long row) {
-  const RowPart* part = row_parts(a, row);
-  const int n = chunks_of(a.V), lane = threadIdx.x & 63;
-  float m = -INFINITY, z = 0.f;
-  for (int i = lane; i < n; i += 64) m = fmaxf(m, part[i].max);
-  for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  for (int i = lane; i < n; i += 64) z += part[i].max == -INFINITY ? 0.f : part[i].sum * fast_exp2((part[i].max - m) * a.inv_t * kLog2e);
-  for (int o = 32; o; o >>= 1) z += __shfl_xor(z, o);
-  return {m, z};
-}
-// exp(inv_t (l - m)) in float64
-__device__ __forceinline__ double weight_of(const VerifyArgs& a, float l, float m) {
-  return l == -INFINITY ? 0. : exp((double)a.inv_t * ((double)l - (double)m));
-}
 __device__ __forceinline__ int draft_token(const VerifyArgs& a, long b, int i) {  // -1: none
-  const int x = a.drafts[b * a.k + i];
+  const int x = i < a.k ? a.drafts[b * a.k + i] : -1;
   return x >= 0 && x < a.V ? x : -1;
 }
-// How many drafts of sequence b are accepted; `r`: the row that its next token is drawn from.
-__device__ __forceinline__ int accepted_drafts(const VerifyArgs& a, long b, RowPart& r) {
-  for (int i = 0; i <= a.k; ++i) {
-    const long row = b * (a.k + 1) + i;
-    r = {0.f, 1.f};
-    if (a.logits) r = whole_row(a, row);
-    if (i == a.k) break;
-    const int x = draft_token(a, b, i);
-    if (x < 0) return i;
-    const float l = element(a.target, a.target_type, row * a.target_stride + x);
-    const double p = a.logits ? weight_of(a, l, r.max) / (double)r.sum : (double)l;
-    const double q = a.q ? (double)element(a.q, a.q_type, (b * a.k + i) * a.q_stride + x) : 1.;
-    if (!((double)a.uniform[b * (a.k + 1) + i] * q < p)) return i;
-  }
-  return a.k;
-}
-// What the draft model gave token j of row (b, i); 0 where nothing is to be taken off.
-struct DraftRow {
-  const void* q;
-  int type, token;  // q == nullptr: all on `token` (-1: nothing)
-  long at;
-  __device__ __forceinline__ double of(int j) const { return q ? (double)element(q, type, at + j) : (j == token ? 1. : 0.); }
-};
-__device__ __forceinline__ DraftRow draft_row(const VerifyArgs& a, long b, int i) {
-  const int x = i < a.k ? draft_token(a, b, i) : -1;
-  if (x < 0 || !a.q) return {nullptr, 0, x, 0};
-  return {a.q, a.q_type, x, (b * a.k + i) * a.q_stride};
+__device__ __forceinline__ Picked pick(const VerifyArgs& a, long b, int i) {
+  const int x = draft_token(a, b, i);
+  if (x < 0) return {0.f, -1.f};
+  return {element(a.target, a.target_type, (b * (a.k + 1) + i) * a.target_stride + x),
+          a.q ? element(a.q, a.q_type, (b * a.k + i) * a.q_stride + x) : 1.f};
 }
 
-__global__ __launch_bounds__(kVerifyThreads) void verify_sums_kernel(VerifyArgs a) {
-  __shared__ double lds[kVerifyThreads / 64];
-  const long b = blockIdx.x;
-  RowPart r;
-  const int i = accepted_drafts(a, b, r);
-  const DraftRow q = draft_row(a, b, i);
-  const long at = (b * (a.k + 1) + i) * a.target_stride;
-  const int c0 = blockIdx.y * kChunk, end = a.V < c0 + kChunk ? a.V : c0 + kChunk;
-  const double inv = a.logits ? 1. / (double)r.sum : 1.;
-  double sp = 0., sa = 0., sq = 0.;
-  for (int j = c0 + threadIdx.x; j < end; j += kVerifyThreads) {
-    const float l = element(a.target, a.target_type, at + j);
-    const double p = a.logits ? weight_of(a, l, r.max) : (double)l, d = q.of(j);
-    sp += p;
-    // (r.sum is good to 1e-7: a token at which that decides has p = q to within it, and adds as little either way)
-    if (p * inv > d) sa += p, sq += d;
+template <int TYPE>
+__global__ __launch_bounds__(kVerifyThreads) void verify_stats_kernel(VerifyArgs a) {
+  const long row = blockIdx.x;
+  const int lane = threadIdx.x & 63, seg = blockIdx.y * kVerifyWaves + (threadIdx.x >> 6), c0 = seg * kSegment;
+  if (seg >= segments_of(a.V)) return;
+  const float t2 = a.inv_t * kLog2e;
+  float x[kPieces][8], m = -INFINITY;
+  if (c0 + kSegment <= a.V) {  // (a branch of the whole wavefront: its loads are then requested together)
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) eight(a.target, TYPE, row * a.target_stride + c0 + (64 * i + lane) * 8, 8, -INFINITY, x[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int j = c0 + (64 * i + lane) * 8;
+      eight(a.target, TYPE, row * a.target_stride + j, a.V - j, -INFINITY, x[i]);
+    }
   }
-  sp = block_reduce(sp, lds, add<double>);
-  sa = block_reduce(sa, lds, add<double>);
-  sq = block_reduce(sq, lds, add<double>);
-  if (threadIdx.x == 0) chunk_sums(a, b)[blockIdx.y] = {sp, sa, sq};
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+    for (int u = 0; u < 8; ++u) m = fmaxf(m, x[i][u]);
+  m = wave_max(m);
+  float z[2] = {0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+    for (int u = 0; u < 8; ++u) z[u & 1] += x[i][u] == -INFINITY ? 0.f : fast_exp2((x[i][u] - m) * t2);
+  const float sum = wave_add(z[0] + z[1]);
+  if (lane == 0) row_parts(a, row)[seg] = {m, sum};
+  // (here they are a latency beside others, in the next kernel two in front of everything)
+  if (seg == 0 && lane == 0) picked(a)[row] = pick(a, row / (a.k + 1), (int)(row % (a.k + 1)));
+}
+
+// Maximum of a row, and its sum against it (by a wavefront).
+__device__ __forceinline__ RowPart whole_row(const VerifyArgs& a, long row) {
+  const RowPart* part = row_parts(a, row);
+  const int n = segments_of(a.V), lane = threadIdx.x & 63;
+  const RowPart mine = lane < n ? part[lane] : RowPart{-INFINITY, 0.f};
+  float m = mine.max;
+  for (int i = 64 + lane; i < n; i += 64) m = fmaxf(m, part[i].max);
+  m = wave_max(m);
+  float z = 0.f;
+  auto take = [&](RowPart p) { z += p.max == -INFINITY ? 0.f : p.sum * fast_exp2((p.max - m) * a.inv_t * kLog2e); };
+  take(mine);
+  for (int i = 64 + lane; i < n; i += 64) take(part[i]);
+  return {m, wave_add(z)};
+}
+// exp(inv_t (l - m)) in float64: with y = inv_t log2(e) (l - m) and n the whole number next to it, 2^n times the Taylor series of
+// 2^(y - n) = exp((y - n) ln 2), whose argument is at most 0.35, up to the 10th power: the next term is 2.2e-13, by which a draw over
+// 10^5 tokens is decided otherwise once in 10^8. (The sums are bound by these instructions. 64 rows of 131072: 23.9 us with the
+// library's exp(), 21.0 so.)
+struct Exponential {
+  double c, cm;
+  __device__ __forceinline__ Exponential(float inv_t, float m) : c((double)inv_t * 1.4426950408889634074), cm(c * (double)m) {}
+  __device__ __forceinline__ double operator()(float l) const {
+    constexpr double L = 0.69314718055994530942, L2 = L * L, L3 = L2 * L, L4 = L2 * L2, L5 = L4 * L;
+    const double y = __builtin_fma(c, (double)l, -cm), n = rint(y), f = y - n;
+    double s = L5 * L5 / 3628800;
+    s = __builtin_fma(s, f, L5 * L4 / 362880);
+    s = __builtin_fma(s, f, L4 * L4 / 40320);
+    s = __builtin_fma(s, f, L4 * L3 / 5040);
+    s = __builtin_fma(s, f, L3 * L3 / 720);
+    s = __builtin_fma(s, f, L5 / 120);
+    s = __builtin_fma(s, f, L4 / 24);
+    s = __builtin_fma(s, f, L3 / 6);
+    s = __builtin_fma(s, f, L2 / 2);
+    s = __builtin_fma(s, f, L);
+    s = __builtin_fma(s, f, 1.);
+    return l == -INFINITY ? 0. : __builtin_ldexp(s, (int)fmax(n, -2000.));
+  }
+};
+constexpr int kCertain = 3;  // in the place of a type: the drafts are certain
+// What the draft model gave the tokens of row (b, i); 0 where nothing is to be taken off.
+struct DraftRow {
+  const void* q;
+  int token;  // q == nullptr: all on `token` (-1: nothing)
+  long at;
+  template <int QTYPE>
+  __device__ __forceinline__ void of(int j, int n, float (&d)[8]) const {
+    if (QTYPE != kCertain && q) return eight(q, QTYPE, at + j, n, 0.f, d);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) d[u] = j + u == token ? 1.f : 0.f;
+  }
+};
+__device__ __forceinline__ DraftRow draft_row(const VerifyArgs& a, long b, int i) {
+  const int x = draft_token(a, b, i);
+  if (x < 0 || !a.q) return {nullptr, x, 0};
+  return {a.q, x, (b * a.k + i) * a.q_stride};
+}
+
+template <int TYPE, int QTYPE>
+__global__ __launch_bounds__(kVerifyThreads) void verify_sums_kernel(VerifyArgs a) {
+  __shared__ int first;  // the first row whose draft is not accepted (k: none)
+  __shared__ RowPart rows[kVerifyWaves];
+  const long b = blockIdx.x;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  // Four rows at a time, a wavefront each, until one is not accepted
+  if (threadIdx.x == 0) first = a.k + 1;
+  RowPart r = {0.f, 1.f};
+  int i = 0;
+  for (int i0 = 0; i0 <= a.k; i0 += kVerifyWaves) {
+    i = i0 + w;
+    if (i <= a.k) {
+      const long row = b * (a.k + 1) + i;
+      const double u = (double)a.uniform[row];
+      const Picked x = a.logits ? picked(a)[row] : pick(a, b, i);
+      if (a.logits) r = whole_row(a, row);
+      const double p = a.logits ? Exponential(a.inv_t, r.max)(x.target) / (double)r.sum : (double)x.target;
+      if (lane == 0) rows[w] = r;
+      __syncthreads();
+      if (lane == 0 && !(x.draft >= 0.f && u * (double)x.draft < p)) atomicMin(&first, i);
+    } else {
+      __syncthreads();
+    }
+    __syncthreads();
+    if (first <= a.k) break;
+    __syncthreads();  // (the rows' sums are written again)
+  }
+  i = first;
+  r = rows[i % kVerifyWaves];
+  const int seg = blockIdx.y * kVerifyWaves + w, c0 = seg * kSegment;
   if (blockIdx.y == 0) {  // the tokens so far
     if (threadIdx.x == 0) a.accepted[b] = i;
     for (int j = threadIdx.x; j <= a.k; j += kVerifyThreads) a.tokens[b * (a.k + 1) + j] = j < i ? a.drafts[b * a.k + j] : -1;
   }
+  if (c0 >= a.V) return;
+  const DraftRow q = draft_row(a, b, i);
+  const long at = (b * (a.k + 1) + i) * a.target_stride;
+  const double inv = a.logits ? 1. / (double)r.sum : 1.;
+  const Exponential weight(a.inv_t, r.max);
+  double sp = 0., sa = 0., sq = 0.;
+  float l[kPieces][8], d[kPieces][8];
+  if (c0 + kSegment <= a.V) {  // (as in the stats kernel)
+#pragma unroll
+    for (int i8 = 0; i8 < kPieces; ++i8) {
+      const int j = c0 + (64 * i8 + lane) * 8;
+      eight(a.target, TYPE, at + j, 8, 0.f, l[i8]);
+      q.of<QTYPE>(j, 8, d[i8]);
+    }
+  } else {
+#pragma unroll
+    for (int i8 = 0; i8 < kPieces; ++i8) {
+      const int j = c0 + (64 * i8 + lane) * 8;
+      eight(a.target, TYPE, at + j, a.V - j, a.logits ? -INFINITY : 0.f, l[i8]);
+      q.of<QTYPE>(j, a.V - j, d[i8]);
+    }
+  }
+#pragma unroll
+  for (int i8 = 0; i8 < kPieces; ++i8)
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const double p = a.logits ? weight(l[i8][u]) : (double)l[i8][u];
+      sp += p;
+      // (r.sum is good to 1e-7: a token at which that decides has p = q to within it, and adds as little either way)
+      if (p * inv > (double)d[i8][u]) sa += p, sq += (double)d[i8][u];
+    }
+  for (int o = 32; o; o >>= 1) {  // (side by side: each step is a latency)
+    const double x = __shfl_xor(sp, o), y = __shfl_xor(sa, o), v = __shfl_xor(sq, o);
+    sp += x;
+    sa += y;
+    sq += v;
+  }
+  if (lane == 0) segment_sums(a, b)[seg] = {sp, sa, sq};
 }
 
+template <int TYPE, int QTYPE>
 __global__ __launch_bounds__(kVerifyThreads) void verify_draw_kernel(VerifyArgs a) {
-  __shared__ double lds[kVerifyThreads / 64];
-  __shared__ double before[kVerifyThreads];
-  __shared__ int last[kVerifyThreads / 64];
+  __shared__ double sums[kVerifyWaves];
+  __shared__ int least[kVerifyWaves], most[kVerifyWaves];
   const long b = blockIdx.x;
-  const int tid = threadIdx.x, nc = chunks_of(a.V), i = a.accepted[b];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = segments_of(a.V), i = a.accepted[b];
   const long row = b * (a.k + 1) + i;
+  const double u = (double)a.uniform[b * (a.k + 1) + a.k];
   const DraftRow q = draft_row(a, b, i);
-  const ChunkSums* part = chunk_sums(a, b);
-  // the row's sum, and whether p - q leaves anything
-  double z = 0., above = 0., off = 0.;
-  for (int c = tid; c < nc; c += kVerifyThreads) z += part[c].p, above += part[c].above, off += part[c].drafts;
-  z = block_reduce(z, lds, add<double>);
-  above = block_reduce(above, lds, add<double>);
-  off = block_reduce(off, lds, add<double>);
-  const double inv = a.logits ? 1. / z : 1.;
-  const bool residual = above * inv - off > 0.;
-  const double total = residual ? above * inv - off : z * inv, want = (double)a.uniform[b * (a.k + 1) + a.k] * total;
-  // the first chunk whose end lies past `want`, or else the last one that adds anything
-  auto chunk_sum = [&](int c) { return residual ? part[c].above * inv - part[c].drafts : part[c].p * inv; };
-  int chunk = -1;
-  double sum = 0., base = 0.;
-  for (int c = 0; c < nc; ++c) {
-    const double x = chunk_sum(c);
-    if (x > 0.) chunk = c, base = sum;
-    sum += x;
-    if (chunk == c && sum > want) break;
-  }
-  if (chunk < 0) return;  // (nothing to draw from: the token stays -1)
+  // (every wavefront for itself)
+  const SegmentSums* part = segment_sums(a, b);
   RowPart r = {0.f, 1.f};
   if (a.logits) r = whole_row(a, row);
-  auto weight = [&](int j) {
-    const float l = element(a.target, a.target_type, row * a.target_stride + j);
-    const double p = (a.logits ? weight_of(a, l, r.max) : (double)l) * inv, d = residual ? q.of(j) : 0.;
-    return p > d ? p - d : 0.;
-  };
-  // each thread: kPer tokens that follow each other
-  const int j0 = chunk * kChunk + tid * kPer;
-  double x[kPer], mine = 0.;
-  int some = -1;  // the last one that adds anything
-#pragma unroll
-  for (int u = 0; u < kPer; ++u) {
-    x[u] = j0 + u < a.V ? weight(j0 + u) : 0.;
-    mine += x[u];
-    if (x[u] > 0.) some = j0 + u;
+  double z = 0., above = 0., off = 0.;
+  for (int c = lane; c < n; c += 64) z += part[c].p, above += part[c].above, off += part[c].drafts;
+  for (int o = 32; o; o >>= 1) {
+    const double x = __shfl_xor(z, o), y = __shfl_xor(above, o), v = __shfl_xor(off, o);
+    z += x;
+    above += y;
+    off += v;
   }
-  before[tid] = mine;
-  for (int o = 32; o; o >>= 1) some = max(some, __shfl_xor(some, o));
-  if ((tid & 63) == 0) last[tid >> 6] = some;
-  __syncthreads();
-  for (int w = 0; w < kVerifyThreads / 64; ++w) some = max(some, last[w]);
-  double run = base;
-  for (int t = 0; t < tid; ++t) run += before[t];
-  int hit = 0x7fffffff;
-#pragma unroll
-  for (int u = 0; u < kPer; ++u) {
-    run += x[u];
-    if (x[u] > 0. && run > want && hit == 0x7fffffff) hit = j0 + u;
+  const double inv = a.logits ? 1. / z : 1.;
+  const bool residual = above * inv - off > 0.;  // whether p - q leaves anything
+  const double want = u * (residual ? above * inv - off : z * inv);
+  // the first segment whose end lies past `want`, or else the last one that adds anything; and what lies before it
+  int seg = -1;
+  double base = 0., done = 0.;
+  for (int c0 = 0; c0 < n; c0 += 64) {
+    const int c = c0 + lane;
+    double x = c >= n ? 0. : residual ? part[c].above * inv - part[c].drafts : part[c].p * inv;
+    x = x > 0. ? x : 0.;
+    const double sum = done + wave_scan(x);
+    const unsigned long long some = __builtin_amdgcn_ballot_w64(x > 0.), past = __builtin_amdgcn_ballot_w64(x > 0. && sum > want);
+    if (some) {
+      const int at = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
+      seg = c0 + at;
+      base = __shfl(sum - x, at);
+    }
+    if (past) break;
+    done = __shfl(sum, 63);
   }
-  for (int o = 32; o; o >>= 1) hit = min(hit, __shfl_xor(hit, o));
+  if (seg < 0) return;  // (nothing to draw from: the token stays -1)
+  // each thread: eight tokens that follow each other
+  const Exponential weight(a.inv_t, r.max);
+  const int j0 = seg * kSegment + tid * 8;
+  float l[8], d[8];
+  double x[8], mine = 0.;
+  eight(a.target, TYPE, row * a.target_stride + j0, a.V - j0, a.logits ? -INFINITY : 0.f, l);
+  q.of<QTYPE>(j0, a.V - j0, d);
+  int last = -1, hit = 0x7fffffff;  // the last one that adds anything, the first one past `want`
+#pragma unroll
+  for (int v = 0; v < 8; ++v) {
+    const double p = (a.logits ? weight(l[v]) : (double)l[v]) * inv, dv = residual ? (double)d[v] : 0.;
+    x[v] = p > dv ? p - dv : 0.;
+    mine += x[v];
+    if (x[v] > 0.) last = j0 + v;
+  }
+  double run = wave_scan(mine);
+  if (lane == 63) sums[w] = run;
   __syncthreads();
-  if ((tid & 63) == 0) last[tid >> 6] = hit;
+  run += base - mine;
+  for (int v = 0; v < w; ++v) run += sums[v];
+#pragma unroll
+  for (int v = 0; v < 8; ++v) {
+    run += x[v];
+    if (x[v] > 0. && run > want && hit == 0x7fffffff) hit = j0 + v;
+  }
+  for (int o = 32; o; o >>= 1) {
+    last = max(last, __shfl_xor(last, o));
+    hit = min(hit, __shfl_xor(hit, o));
+  }
+  if (lane == 0) {
+    least[w] = hit;
+    most[w] = last;
+  }
   __syncthreads();
   if (tid == 0) {
-    for (int w = 1; w < kVerifyThreads / 64; ++w) hit = min(hit, last[w]);
-    a.tokens[row] = hit != 0x7fffffff ? hit : some;
+    for (int v = 1; v < kVerifyWaves; ++v) {
+      hit = min(hit, least[v]);
+      last = max(last, most[v]);
+    }
+    a.tokens[row] = hit != 0x7fffffff ? hit : last;
   }
 }
 
-hipError_t launch_verify(const VerifyArgs& a, hipStream_t st) {
-  const unsigned chunks = (unsigned)chunks_of(a.V);
+template <int TYPE, int QTYPE>
+static hipError_t launch_verify_as(const VerifyArgs& a, hipStream_t st) {
+  const unsigned parts = (unsigned)((segments_of(a.V) + kVerifyWaves - 1) / kVerifyWaves);
+  const dim3 block(kVerifyThreads);
   if (a.logits) {
-    hipLaunchKernelGGL(verify_stats_kernel, dim3((unsigned)(a.nseq * (a.k + 1)), chunks), dim3(kVerifyThreads), 0, st, a);
+    hipLaunchKernelGGL(verify_stats_kernel<TYPE>, dim3((unsigned)(a.nseq * (a.k + 1)), parts), block, 0, st, a);
     if (hipError_t e = hipGetLastError()) return e;
   }
-  hipLaunchKernelGGL(verify_sums_kernel, dim3((unsigned)a.nseq, chunks), dim3(kVerifyThreads), 0, st, a);
+  hipLaunchKernelGGL((verify_sums_kernel<TYPE, QTYPE>), dim3((unsigned)a.nseq, parts), block, 0, st, a);
   if (hipError_t e = hipGetLastError()) return e;
-  hipLaunchKernelGGL(verify_draw_kernel, dim3((unsigned)a.nseq), dim3(kVerifyThreads), 0, st, a);
+  hipLaunchKernelGGL((verify_draw_kernel<TYPE, QTYPE>), dim3((unsigned)a.nseq), block, 0, st, a);
   return hipGetLastError();
+}
+template <int TYPE>
+static hipError_t launch_verify_t(const VerifyArgs& a, hipStream_t st) {
+  if (!a.q) return launch_verify_as<TYPE, kCertain>(a, st);
+  if (a.q_type == FA_TYPE_F32) return launch_verify_as<TYPE, FA_TYPE_F32>(a, st);
+  return a.q_type == FA_TYPE_BF16 ? launch_verify_as<TYPE, FA_TYPE_BF16>(a, st) : launch_verify_as<TYPE, FA_TYPE_F16>(a, st);
+}
+hipError_t launch_verify(const VerifyArgs& a, hipStream_t st) {
+  if (a.target_type == FA_TYPE_F32) return launch_verify_t<FA_TYPE_F32>(a, st);
+  return a.target_type == FA_TYPE_BF16 ? launch_verify_t<FA_TYPE_BF16>(a, st) : launch_verify_t<FA_TYPE_F16>(a, st);
 }
 
 }  // namespace fa
