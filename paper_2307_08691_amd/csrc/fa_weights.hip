@@ -2,9 +2,8 @@
 // exp(scale * q_r . k_c - L_r), from the logsumexps L that the attention pass left: the column sums of P, which that pass never
 // has whole. One product and one exponential per (row, key), no second product.
 //
-// A row is a (query, head of the group) pair, packed as query * G + head. S = Q K^T is formed with the KEYS as columns of the MFMA
-// tile: a lane then holds 16 rows of ONE key, and the sum over rows is additions inside the lane and one exchange with the partner
-// lane. Every key's sum is formed by one lane in a fixed order: no atomics, the same bits in every run.
+// A row is a (query, head of the group) pair, packed as query * G + head. Every key's sum is formed in a fixed order: no atomics, the
+// same bits in every run.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -14,94 +13,158 @@
 
 namespace fa {
 
-// Up to 32 rows (decoding): the rows stay in registers and the keys stream past. Bound by reading K once; four wavefronts that
-// share nothing, each with tiles of 32 keys, the next tile requested before the current one is used.
-constexpr int kStepKeys = 512;  // keys of a workgroup
-template <int D, bool F16>
-__global__ __launch_bounds__(256) void weights_step_kernel(WeightsArgs a) {
-  constexpr int KS = D / 16;
+// A workgroup's (sequence, key/value head): the heads of a sequence follow each other on ONE XCD, and eight sequences are under way on
+// the eight. Heads lie side by side in memory, a row of each after the other: (64 sequences of up to 8192 keys, 8 heads of 128: 114 us
+// with a head to an XCD, 109 so; 96 of up to 2048, heads of 64: 27.0 and 24.8.) The sequences past the last eight: as they come.
+__device__ __forceinline__ void pair_of(int i, int nseq, int heads, int& s, int& g) {
+  const int set = kXcds * heads, whole = nseq / kXcds * set;
+  if (i < whole) {
+    const int in = i % set;
+    s = i / set * kXcds + in % kXcds;
+    g = in / kXcds;
+  } else {
+    s = i / heads;
+    g = i % heads;
+  }
+}
+
+// Few rows (decoding): the rows stay and the keys stream past, in tiles of 32 that each of a workgroup's four wavefronts takes in
+// turn, the next one requested before the current one is used. S = Q K^T is formed with the KEYS as columns of the MFMA tile: a lane
+// then holds 16 rows of ONE key, and the sum over rows is additions inside the lane and one exchange with the partner lane. Bound
+// by reading K once: 64 sequences of up to 8192 keys, 32 heads on 8 of 128: 107 us, 4.5 TB/s (a large read: 6.1). Up to 32 rows are held
+// in registers; MANY: up to kStepRows in LDS.
+constexpr int kStepRows = 256;
+template <int D, bool F16, bool MANY>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MANY ? 2 : D == 64 ? 4 : 3))) void weights_step_kernel(WeightsArgs a, int keys) {  // keys: of a workgroup, a multiple of 128
+  constexpr int KS = D / 16, NW = 4, ROWB = 2 * D;
+  __shared__ __attribute__((aligned(1024))) char smem[MANY ? kStepRows * (ROWB + 4) : 16];
+  float* const stat = (float*)(smem + kStepRows * ROWB);  // (MANY) nl of every row
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lq = lane & 31, hh = lane >> 5;
-  const int pair = blockIdx.x, s = pair / a.c.Hkv, g = pair - s * a.c.Hkv;
-  const int n = held_keys(a.c, s), c0 = blockIdx.y * kStepKeys;
+  int s, g;
+  pair_of(blockIdx.x, a.nseq, a.c.Hkv, s, g);
+  const int n = held_keys(a.c, s), c0 = blockIdx.y * keys;
   int nq = a.queries ? a.queries[s] : a.Nq;
   nq = nq < a.Nq ? nq : a.Nq;
   if (c0 >= n || nq <= 0) return;
   const int rows = nq * a.G, off = n - a.Nq;
   const float c2 = a.scale * kLog2e;
-  const int end = n < c0 + kStepKeys ? n : c0 + kStepKeys;
+  const int end = n - c0 < keys ? n : c0 + keys;
 
   const long kstride = (long)a.c.Hkv * D;
+  const int mask = (1 << a.c.page_log2) - 1;
+  float* W = a.weights + ((long)s * a.c.Hkv + g) * a.c.Nk;
   bf16x8 Kr[2][KS];
+  float old[2];   // (requested with the keys: loads come back in order, and one that is requested behind the next tile's waits for it)
+  int pages = 0;  // lane i: the page of tile i of this wavefront's next 64
   auto request = [&](int t, auto BUF) {  // tile of 32 keys from t on; keys past the end repeat the last one
-    const int row = t + lq < n ? t + lq : n - 1;
-    const __bf16* kp = a.K + (cache_row(a.c, s, t) + (row - t)) * kstride + (long)g * D + 8 * hh;  // (a tile lies in one page)
+    long row = (long)s * a.c.Nk + t;
+    if (a.c.table) {
+      const int i = (t - c0) / (32 * NW) & 63;
+      if (i == 0) {
+        const int x = t + lane * (32 * NW);
+        pages = a.c.table[(long)s * a.c.table_stride + ((x < end ? x : t) >> a.c.page_log2)];
+      }
+      row = ((long)__builtin_amdgcn_readlane(pages, i) << a.c.page_log2) + (t & mask);
+    }
+    const int in = t + lq < n ? lq : n - 1 - t;
+    old[decltype(BUF)::value] = W[t + in];
+    const __bf16* kp = a.K + (row + in) * kstride + (long)g * D + 8 * hh;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) Kr[decltype(BUF)::value][ks] = *(const bf16x8*)(kp + 16 * ks);
   };
   using B0 = std::integral_constant<int, 0>;
   using B1 = std::integral_constant<int, 1>;
   int t = c0 + 32 * w;
-  if (t >= end) return;
-  request(t, B0{});
+  if (!MANY && t >= end) return;
+  if (t < end) request(t, B0{});
+  if (t + 32 * NW < end) request(t + 32 * NW, B1{});
 
+  // -L of a row in the exponent's base; -inf where it adds nothing
+  auto row_stat = [&](int row) {
+    const int rc = row < rows ? row : rows - 1, q = rc / a.G;
+    const float l = a.LSE[((long)s * a.Hq + g * a.G + (rc - q * a.G)) * a.Nq + q];
+    return row < rows && l != -INFINITY ? -l * kLog2e : -INFINITY;
+  };
+  auto row_at = [&](int row) {
+    const int rc = row < rows ? row : rows - 1, q = rc / a.G;
+    return a.Q + (((long)s * a.Nq + q) * a.Hq + g * a.G + (rc - q * a.G)) * D;
+  };
   bf16x8 Qf[KS];
-  {
-    const int row = lq < rows ? lq : rows - 1;
-    const __bf16* qp = a.Q + (((long)s * a.Nq + row / a.G) * a.Hq + g * a.G + row % a.G) * D + 8 * hh;
+  f32x4 nl[4];  // of the rows of this lane's registers
+  if constexpr (MANY) {
+    constexpr int CPR = ROWB / 16;
+    for (int i = threadIdx.x; i < (rows + 31) / 32 * 32 * CPR; i += 64 * NW) {
+      const int r = i / CPR, ch = i % CPR;
+      *(bf16x8*)(smem + swz_off<ROWB>(r, ch)) = *(const bf16x8*)(row_at(r) + 8 * ch);
+    }
+    if (threadIdx.x < (rows + 31) / 32 * 32) stat[threadIdx.x] = row_stat(threadIdx.x);
+    __syncthreads();
+    if (t >= end) return;
+  } else {
+    const __bf16* qp = row_at(lq) + 8 * hh;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) Qf[ks] = *(const bf16x8*)(qp + 16 * ks);
-  }
-  float nl[16];  // -L in the exponent's base; -inf where the register's row adds nothing
+    const float mine = row_stat(lq);  // (a lane has one row's, and the registers' rows are handed round)
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int row = acc_row(r, hh), rc = row < rows ? row : rows - 1;
-    const float l = a.LSE[((long)s * a.Hq + g * a.G + rc % a.G) * a.Nq + rc / a.G];
-    nl[r] = row < rows && l != -INFINITY ? -l * kLog2e : -INFINITY;
+    for (int r = 0; r < 16; ++r) nl[r / 4][r % 4] = __shfl(mine, acc_row(r, hh));
   }
 
-  float* W = a.weights + ((long)s * a.c.Hkv + g) * a.c.Nk;
+  const int zrow = lq * ROWB + 16 * (hh ^ swz<ROWB>(lq));
   auto compute = [&](int t, auto BUF) {
-    f32x16 S = (f32x16){0};
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) S = mfma32<F16>(Qf[ks], Kr[decltype(BUF)::value][ks], S);
     const int key = t + lq;
     float sum[2] = {0.f, 0.f};
-    if (a.causal && t + 31 > off) {
-      asm volatile("; keep this a branch" ::);
+    for (int rt = 0; rt < (MANY ? rows : 1); rt += 32) {
+      const long sees = a.causal ? (long)(t - off) * a.G : 0;  // the first row that sees the tile's first key
+      if (MANY && sees > rt + 31) continue;
+      if constexpr (MANY) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float e = fast_exp2(__builtin_fmaf(S[r], c2, nl[r]));
-        sum[r & 1] += nl[r] != -INFINITY && key <= acc_row(r, hh) / a.G + off ? e : 0.f;
+        for (int i = 0; i < 4; ++i) nl[i] = *(const f32x4*)(stat + rt + 8 * i + 4 * hh);
       }
-    } else {
+      f32x16 S = (f32x16){0};
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float e = fast_exp2(__builtin_fmaf(S[r], c2, nl[r]));
-        sum[r & 1] += nl[r] != -INFINITY ? e : 0.f;
+      for (int ks = 0; ks < KS; ++ks)
+        S = mfma32<F16>(MANY ? lds_b128(smem, (zrow ^ (32 * ks)) + rt * ROWB) : Qf[ks], Kr[decltype(BUF)::value][ks], S);
+      if (a.causal && (MANY ? sees + 31l * a.G > rt : t + 31 > off)) {
+        const int first = (key - off) * a.G - 4 * hh - rt;  // the first row that sees the lane's key, from the half's first
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float x = nl[r / 4][r % 4], e = fast_exp2(__builtin_fmaf(S[r], c2, x));
+          sum[r & 1] += (x != -INFINITY) & (acc_row(r, 0) >= first) ? e : 0.f;
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float x = nl[r / 4][r % 4], e = fast_exp2(__builtin_fmaf(S[r], c2, x));
+          sum[r & 1] += x != -INFINITY ? e : 0.f;
+        }
       }
     }
     const float total = sum_with_partner32(sum[0] + sum[1]);
-    if (hh == 0 && key < end) W[key] += total;
+    if (hh == 0 && key < end) W[key] = old[decltype(BUF)::value] + total;
   };
+  bool here = true;
   while (true) {
-    if (t + 128 < end) request(t + 128, B1{});
+    if (!here && t + 32 * NW < end) request(t + 32 * NW, B1{});
+    here = false;
     compute(t, B0{});
-    if ((t += 128) >= end) break;
-    if (t + 128 < end) request(t + 128, B0{});
+    if ((t += 32 * NW) >= end) break;
+    if (t + 32 * NW < end) request(t + 32 * NW, B0{});
     compute(t, B1{});
-    if ((t += 128) >= end) break;
+    if ((t += 32 * NW) >= end) break;
   }
 }
 
-// More rows: a wavefront holds 64 keys in registers and the rows stream past in tiles of 64, which the workgroup's four wavefronts
-// (256 keys) share through LDS, one tile ahead. Bound by the exponentials. Under the causal rule tiles above the keys are not
-// visited, and the blocks of keys with the most rows are handed out first.
-constexpr int kPromptKeys = 256;
+// More rows: a workgroup has 64 keys, which each of its four wavefronts holds in registers, and the rows stream past in tiles of 32
+// that the wavefronts take in turn, straight from L2, the next one requested before the current one is used. S^T = K Q^T here: a lane
+// has ONE row (and so one L), its accumulators the keys' sums over its rows; lanes and wavefronts are joined once, at the end.
+// Bound by the exponentials: 2 prompts of 2048, 16 heads of 64, 30 us for 67 million of them (three rounds of workgroups with their starts and
+// joins; deeper requests, eight wavefronts or fewer registers change nothing). No barrier in the loop; under the causal rule rows above the keys are not visited, and the blocks of keys
+// with the most rows are handed out first.
+constexpr int kPromptKeys = 64;
 template <int D, bool F16>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void weights_prompt_kernel(WeightsArgs a) {
-  constexpr int KS = D / 16, ROWB = 2 * D, BR = 64, TILEB = BR * ROWB, CPR = ROWB / 16, RPI = 64 / CPR;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * TILEB + 2 * BR * 4];
-  float* const stat = (float*)(smem + 2 * TILEB);
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void weights_prompt_kernel(WeightsArgs a) {
+  constexpr int KS = D / 16, NW = 4, PITCH = 33;
+  __shared__ float part[NW * kPromptKeys * PITCH];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane & 31, hh = lane >> 5;
   const int pair = blockIdx.x, s = pair / a.c.Hkv, g = pair - s * a.c.Hkv;
   const int n = held_keys(a.c, s), c0 = blockIdx.y * kPromptKeys;
@@ -110,108 +173,112 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   if (c0 >= n || nq <= 0) return;
   const int rows = nq * a.G, off = n - a.Nq;
   const float c2 = a.scale * kLog2e;
-  const int kb = c0 + 64 * w;  // this wavefront's keys
   bf16x8 Kr[2][KS];
+  {
+    const __bf16* kb = a.K + (cache_row(a.c, s, c0) * a.c.Hkv + g) * D + 8 * hh;  // (a block lies in one page)
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    int key = kb + 32 * u + lq;
-    key = key < n ? key : n - 1;
-    const __bf16* kp = a.K + (cache_row(a.c, s, key) * a.c.Hkv + g) * D + 8 * hh;
+    for (int u = 0; u < 2; ++u) {
+      const int row = 32 * u + lq, last = n - 1 - c0;  // (keys past the end repeat the last one)
+      const __bf16* kp = kb + (long)(row < last ? row : last) * a.c.Hkv * D;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) Kr[u][ks] = *(const bf16x8*)(kp + 16 * ks);
+      for (int ks = 0; ks < KS; ++ks) Kr[u][ks] = *(const bf16x8*)(kp + 16 * ks);
+    }
   }
   const int q_first = a.causal && c0 > off ? c0 - off : 0;  // the first query that sees a key of the block
-  const int tiles = (rows + BR - 1) / BR, t_first = (int)((long)q_first * a.G / BR);
-  const __bf16* Qb = a.Q + ((long)s * a.Nq * a.Hq + g * a.G) * D;
+  const int tiles = (rows + 31) / 32;
+  const __bf16* Qb = a.Q + ((long)s * a.Nq * a.Hq + g * a.G) * D + 8 * hh;
   const float* Lb = a.LSE + ((long)s * a.Hq + g * a.G) * a.Nq;
-  auto copy = [&](int t, int buf) {
+  struct Rows {
+    bf16x8 q[KS];
+    float l;
+    int last;  // the last key that the lane's row sees, from c0
+  };
+  // this lane's next row: query and head, which advance by 32 NW rows a tile
+  int t = (int)((long)q_first * a.G / 32) + w;
+  int next_r = 32 * t + lq, next_q = next_r / a.G, next_h = next_r - next_q * a.G;
+  const int step_q = 32 * NW / a.G, step_h = 32 * NW - step_q * a.G;
+  auto request = [&](Rows& x) {
+    const bool in = next_r < rows;
+    const int q = in ? next_q : nq - 1, h = in ? next_h : 0;
+    x.l = in ? Lb[(long)h * a.Nq + q] : -INFINITY;
+    x.last = a.causal ? q + off - c0 : kPromptKeys;
+    const __bf16* qp = Qb + ((long)q * a.Hq + h) * D;
 #pragma unroll
-    for (int u = 0; u < BR / RPI / 4; ++u) {
-      const int rb = (w + 4 * u) * RPI, r = rb + lane / CPR, ch = (lane % CPR) ^ swz<ROWB>(r);
-      int row = t * BR + r;
-      row = row < rows ? row : rows - 1;
-      const int q = row / a.G;
-      dma16(Qb + ((long)q * a.Hq + (row - q * a.G)) * D + 8 * ch, smem + buf * TILEB + rb * ROWB);
+    for (int ks = 0; ks < KS; ++ks) x.q[ks] = *(const bf16x8*)(qp + 16 * ks);
+    next_r += 32 * NW;
+    next_q += step_q;
+    next_h += step_h;
+    if (next_h >= a.G) next_h -= a.G, ++next_q;
+  };
+  f32x16 sum[2] = {(f32x16){0}, (f32x16){0}};
+  auto compute = [&](int t, const Rows& x) {
+    const float nl = x.l != -INFINITY ? -x.l * kLog2e : -INFINITY;
+    const bool some = a.causal && 32 * t / a.G + off - c0 < kPromptKeys - 1;  // (not all rows see all keys)
+    const int last = nl != -INFINITY ? x.last - 4 * hh : -1;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x16 S = (f32x16){0};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) S = mfma32<F16>(Kr[u][ks], x.q[ks], S);
+      if (some) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float e = fast_exp2(__builtin_fmaf(S[r], c2, nl));
+          sum[u][r] += 32 * u + acc_row(r, 0) <= last ? e : 0.f;
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum[u][r] += fast_exp2(__builtin_fmaf(S[r], c2, nl));
+      }
     }
   };
-  auto row_stat = [&](int t) {  // (threads 0 .. 63)
-    const int row = t * BR + tid;
-    if (tid >= BR || row >= rows) return -INFINITY;
-    const int q = row / a.G;
-    const float l = Lb[(long)(row - q * a.G) * a.Nq + q];
-    return l != -INFINITY ? -l * kLog2e : -INFINITY;
-  };
-  float sum[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
-  const int zrow = lq * ROWB + 16 * (hh ^ swz<ROWB>(lq));
-  if (t_first < tiles) {
-    const float x = row_stat(t_first);
-    if (tid < BR) stat[tid] = x;
-    copy(t_first, 0);
+  if (t < tiles) {
+    Rows x, y;
+    request(x);
+    while (true) {
+      if (t + NW < tiles) request(y);
+      compute(t, x);
+      if ((t += NW) >= tiles) break;
+      if (t + NW < tiles) request(x);
+      compute(t, y);
+      if ((t += NW) >= tiles) break;
+    }
   }
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) touch(Kr[u][ks]);
-  for (int t = t_first, buf = 0; t < tiles; ++t, buf ^= 1) {
-    wait_vmem();
-    lds_barrier();  // tile t has landed, everyone is done with the one before it
-    float next = 0.f;
-    if (t + 1 < tiles) {
-      next = row_stat(t + 1);
-      copy(t + 1, buf ^ 1);
-    }
-    const int q0 = t * BR / a.G, q1 = (t * BR + BR - 1) / a.G;
-    if (!a.causal || q1 + off >= kb) {  // (else none of these rows sees any of these keys)
-      const bool all = !a.causal || q0 + off >= kb + 63;
+    for (int r = 0; r < 16; ++r) part[(w * kPromptKeys + 32 * u + acc_row(r, hh)) * PITCH + lq] = sum[u][r];
+  __syncthreads();
+  // thread (key, quarter of the lanes): the four wavefronts' sums one after the other, then the quarters
+  const int key = tid >> 2, quarter = tid & 3;
+  float total = 0.f;
 #pragma unroll
-      for (int rt = 0; rt < 2; ++rt) {
-        f32x16 S[2] = {(f32x16){0}, (f32x16){0}};
+  for (int u = 0; u < NW; ++u)
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const bf16x8 q = lds_b128(smem, ((zrow + buf * TILEB) ^ (32 * ks)) + rt * 32 * ROWB);
-          S[0] = mfma32<F16>(q, Kr[0][ks], S[0]);
-          S[1] = mfma32<F16>(q, Kr[1][ks], S[1]);
-        }
-        f32x4 nl[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) nl[i] = *(const f32x4*)(stat + buf * BR + 32 * rt + 8 * i + 4 * hh);
-        if (all) {
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) sum[u][r & 1] += fast_exp2(__builtin_fmaf(S[u][r], c2, nl[r / 4][r % 4]));
-        } else {
-          asm volatile("; keep this a branch" ::);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int last = (t * BR + 32 * rt + acc_row(r, hh)) / a.G + off;  // the last key that the row sees
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const float e = fast_exp2(__builtin_fmaf(S[u][r], c2, nl[r / 4][r % 4]));
-              sum[u][r & 1] += nl[r / 4][r % 4] != -INFINITY && kb + 32 * u + lq <= last ? e : 0.f;
-            }
-          }
-        }
-      }
-    }
-    if (t + 1 < tiles && tid < BR) stat[(buf ^ 1) * BR + tid] = next;
-  }
-  float* W = a.weights + ((long)s * a.c.Hkv + g) * a.c.Nk;
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const float total = sum_with_partner32(sum[u][0] + sum[u][1]);
-    const int key = kb + 32 * u + lq;
-    if (hh == 0 && key < n) W[key] += total;
-  }
+    for (int i = 0; i < 8; ++i) total += part[(u * kPromptKeys + key) * PITCH + 8 * quarter + i];
+  total += __shfl_xor(total, 1);
+  total += __shfl_xor(total, 2);
+  if (quarter == 0 && c0 + key < n) a.weights[((long)s * a.c.Hkv + g) * a.c.Nk + c0 + key] += total;
 }
 
 template <int D, bool F16>
 static hipError_t launch_weights_d(const WeightsArgs& a, hipStream_t st) {
   const unsigned pairs = (unsigned)(a.nseq * a.c.Hkv);
-  if ((long)a.Nq * a.G <= 32)
-    hipLaunchKernelGGL((weights_step_kernel<D, F16>), dim3(pairs, (unsigned)((a.c.Nk + kStepKeys - 1) / kStepKeys)), dim3(256), 0, st, a);
-  else
+  // Rows that stay, or keys that do: a prompt among its own keys has as many of these as queries, and the blocks of 64 keys make more
+  // workgroups (us, rows stay / keys stay: 256 rows among 256 keys, 2 x 8 pairs of 128: 10.4 / 7.4; 256 rows (G = 4) on 2000 keys, 4 x 8 pairs
+  // of 64: 9.1 / 13.6; 64 rows on up to 4096, 16 x 8 of 128: 29 / 54; 40 rows, 32 x 8: 46 / 101)
+  if ((long)a.Nq * a.G <= kStepRows && ((long)a.Nq * a.G <= 32 || a.c.Nk > 2l * a.Nq)) {
+    // Two workgroups a compute unit, or up to four tiles a wavefront (us at 128 / 256 / 512 / 1024 / 2048 keys: 4 sequences of up to 2048, 8
+    // heads of 128: 5.2 / 5.2 / 7.2; 8 of up to 4096: 16.1 / 14.5 / 12.3; 64 of up to 8192: - / - / 109 / 113 / 123; 96 of up to 2048, heads
+    // of 64: - / 25.8 / 24.8 / 28.4 / 30.6)
+    long keys = ((long)pairs * a.c.Nk / 512 + 127) / 128 * 128;
+    keys = keys < 128 ? 128 : (keys > 512 ? 512 : keys);
+    const dim3 grid(pairs, (unsigned)((a.c.Nk + keys - 1) / keys));
+    if (a.Nq * a.G <= 32) hipLaunchKernelGGL((weights_step_kernel<D, F16, false>), grid, dim3(256), 0, st, a, (int)keys);
+    else hipLaunchKernelGGL((weights_step_kernel<D, F16, true>), grid, dim3(256), 0, st, a, (int)keys);
+  } else {
     hipLaunchKernelGGL((weights_prompt_kernel<D, F16>), dim3(pairs, (unsigned)((a.c.Nk + kPromptKeys - 1) / kPromptKeys)), dim3(256), 0, st, a);
+  }
   return hipGetLastError();
 }
 hipError_t launch_weights(const WeightsArgs& a, hipStream_t st) {
