@@ -38,8 +38,9 @@ hipError_t launch_append(const AppendArgs& a, hipStream_t st) {
 
 // ---- evict
 // Slots are ordered by a 32-bit key: the weight's bits made monotonic (-0 as 0, NaN below everything), all ones for a protected slot.
+constexpr uint32_t kProtected = 0xffffffffu;
 __device__ __forceinline__ uint32_t evict_key(float w, int pos, int sinks, long recent_from) {
-  if (pos < sinks || pos >= recent_from) return 0xffffffffu;
+  if (pos < sinks || pos >= recent_from) return kProtected;
   if (w != w) return 0u;
   const uint32_t x = __builtin_bit_cast(uint32_t, w + 0.f);
   return x & 0x80000000u ? ~x : x | 0x80000000u;
@@ -47,190 +48,322 @@ __device__ __forceinline__ uint32_t evict_key(float w, int pos, int sinks, long 
 __device__ __forceinline__ int lane_before(unsigned long long m) {  // set bits below this lane
   return __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0u));
 }
-constexpr int kEvictThreads = 1024, kEvictWaves = 16, kEvictBins = 2048;
+constexpr int kEvictBins = 2048;
 
-// One workgroup per (sequence, key/value head). The budget-th largest key is found by three rounds of counting (11, 11 and 10 bits)
-// in LDS; what is above it stays, and of its equals the first ones in slot order. A wavefront owns a contiguous range of slots, so
-// that slot order is (wavefront, step, lane) and ranks are counts of ballots. Kept slots past the budget then move into free ones
-// below it, both ascending: as many rows move as must, in place, and what stays keeps its slot.
-// ITEMS > 0: a lane's keys stay in registers (up to 1024 * ITEMS slots); 0: they are formed again from L2 in every round.
-template <int ITEMS>
-__global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a) {
-  __shared__ int hist[kEvictBins];
-  __shared__ int part[3][kEvictWaves];
-  __shared__ int found[2];
+// Sum over the lanes up to this one (all active); the steps of wave_sum (fa_common.h).
+__device__ __forceinline__ int lane_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+// Of the wavefronts' values in LDS: the sum of those before wavefront w, and of all. (Read together: one by one each is a latency.)
+struct BeforeAndAll {
+  int before, all;
+};
+template <int NW>
+__device__ __forceinline__ BeforeAndAll over_waves(const int (&part)[NW], int w) {
+  BeforeAndAll s = {0, 0};
+  i32x4 x[NW / 4];
+#pragma unroll
+  for (int i = 0; i < NW / 4; ++i) x[i] = ((const i32x4*)part)[i];
+#pragma unroll
+  for (int i = 0; i < NW; ++i) {
+    s.before += i < w ? x[i / 4][i % 4] : 0;
+    s.all += x[i / 4][i % 4];
+  }
+  return s;
+}
+
+// One row of K and of V of a move, 16 bytes a thread
+__device__ __forceinline__ void move_piece(const EvictArgs& a, int s, int g, int src, int dst, int piece) {
+  const CacheView& c = a.c;
+  const long from = (cache_row(c, s, src) * c.Hkv + g) * c.d + 8 * piece, to = (cache_row(c, s, dst) * c.Hkv + g) * c.d + 8 * piece;
+  const u32x4 k = *(const u32x4*)(a.K + from), v = *(const u32x4*)(a.V + from);
+  *(u32x4*)(a.K + to) = k;
+  *(u32x4*)(a.V + to) = v;
+}
+
+// One workgroup per (sequence, key/value head). The last slot that stays, by key and then by slot, is found by counting the keys by
+// their upper bits in LDS (11, 11 and 10 bits), and as soon as its counter has at most kFewKeys keys by comparing those with each other:
+// after one round unless weights are much alike. A wavefront owns a contiguous range of slots, so that slot order is (wavefront,
+// step, lane) and ranks are counts of ballots. Kept slots past the budget then move into free ones
+// below it, both ascending: as many rows move as must, in place, and what stays keeps its slot. Bound by instructions where there are
+// many pairs (so: few wavefronts, each with many slots) and by a chain of barriers and LDS latencies where there are few.
+// ITEMS > 0: a lane's keys stay in registers (up to THREADS * ITEMS slots); 0: they are formed again from L2 in every round.
+// Where no more than kFewMoves rows can have to move, they do so here, else by evict_move_kernel.
+constexpr int kFewMoves = 64, kFewKeys = 64;
+template <int THREADS, int ITEMS>
+__global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
+  constexpr int NW = THREADS / 64, BPT = kEvictBins / THREADS;  // counters of a thread
+  __shared__ __attribute__((aligned(16))) int hist[kEvictBins];
+  __shared__ __attribute__((aligned(16))) int part[4][NW];
+  __shared__ int found[3][3];
+  __shared__ __attribute__((aligned(16))) uint32_t few_keys[kFewKeys];
+  __shared__ __attribute__((aligned(16))) int few_slots[kFewKeys];
+  __shared__ int few_count, last_slot;
+  __shared__ uint32_t last_key;
+  __shared__ int few[2][kFewMoves];
   const int pair = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int s = pair / a.c.Hkv, n = held_keys(a.c, s), budget = a.budget;
+  const int s = pair / a.c.Hkv, g = pair - s * a.c.Hkv, n = held_keys(a.c, s), budget = a.budget;
+  const bool here = a.room <= kFewMoves;
   const long base = (long)pair * a.c.Nk;
   const float* W = a.weights + base;
   const int32_t* P = a.positions + base;
   float* Wo = a.weights_out + base;
   int32_t* Po = a.positions_out + base;
+  if (a.lens_out != a.c.lens && g == 0 && tid == 0) a.lens_out[s] = n < budget ? n : budget;  // (else others still read it)
   if (n <= budget) {  // nothing goes
-    if (tid == 0) a.moves[pair] = 0;
+    if (!here && tid == 0) a.moves[pair] = 0;
     if (Wo != W)
-      for (int i = tid; i < n; i += kEvictThreads) Wo[i] = W[i];
+      for (int i = tid; i < n; i += THREADS) Wo[i] = W[i];
     if (Po != P)
-      for (int i = tid; i < n; i += kEvictThreads) Po[i] = P[i];
+      for (int i = tid; i < n; i += THREADS) Po[i] = P[i];
     return;
   }
-  const int steps = (n + kEvictThreads - 1) / kEvictThreads, first = w * steps * 64 + lane;  // this lane: slots first + 64 i
-  // the newest position
-  int top = -0x7fffffff - 1;
-  for (int i = 0; i < steps; ++i)
-    if (first + 64 * i < n) top = max(top, P[first + 64 * i]);
+  const int steps = (n + THREADS - 1) / THREADS, first = w * steps * 64 + lane;  // this lane: slots first + 64 i
+  auto clear = [&]() {
+#pragma unroll
+    for (int i = 0; i < BPT; ++i) hist[tid + i * THREADS] = 0;
+  };
+  float wt[ITEMS ? ITEMS : 1];
+  int pos[ITEMS ? ITEMS : 1], top = -0x7fffffff - 1;  // top: the newest position
+  if constexpr (ITEMS > 0) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {  // (slots that are not there: the last one again)
+      const int slot = i < steps && first + 64 * i < n ? first + 64 * i : n - 1;
+      wt[i] = W[slot];
+      pos[i] = P[slot];
+    }
+    clear();
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) top = max(top, pos[i]);
+  } else {
+    clear();
+    for (int i = 0; i < steps; ++i) top = max(top, P[first + 64 * i < n ? first + 64 * i : n - 1]);
+  }
   for (int o = 32; o; o >>= 1) top = max(top, __shfl_xor(top, o));
   if (lane == 0) part[0][w] = top;
+  if (tid == 0) few_count = 0;
   __syncthreads();
-  for (int i = 0; i < kEvictWaves; ++i) top = max(top, part[0][i]);
+#pragma unroll
+  for (int i = 0; i < NW / 4; ++i) {
+    const i32x4 x = ((const i32x4*)part[0])[i];
+    top = max(max(top, max(x[0], x[1])), max(x[2], x[3]));
+  }
   const long recent_from = (long)top + 1 - a.recent;
-  auto form = [&](int slot) { return evict_key(W[slot], P[slot], a.sinks, recent_from); };
   uint32_t held[ITEMS ? ITEMS : 1];
   if constexpr (ITEMS > 0) {
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i)
-      if (i < steps && first + 64 * i < n) held[i] = form(first + 64 * i);
+    for (int i = 0; i < ITEMS; ++i) held[i] = evict_key(wt[i], pos[i], a.sinks, recent_from);
   }
-  auto each = [&](auto f) {  // f(slot, key, whether the slot is held), for whole wavefronts
+  auto each = [&](auto f) {  // f(i, slot, key, whether the slot is held), for whole wavefronts
     if constexpr (ITEMS > 0) {
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i)
-        if (i < steps) f(first + 64 * i, held[i], first + 64 * i < n);
+        if (i < steps) f(i, first + 64 * i, held[i], first + 64 * i < n);
     } else {
       for (int i = 0; i < steps; ++i) {
-        const int slot = first + 64 * i;
-        f(slot, slot < n ? form(slot) : 0u, slot < n);
+        const int slot = first + 64 * i, at = slot < n ? slot : n - 1;
+        f(i, slot, evict_key(W[at], P[at], a.sinks, recent_from), slot < n);
       }
     }
   };
   // ---- the budget-th largest key
   uint32_t limit = 0, above = 0;  // bits of it known so far, and which they are
   int rest = budget;              // its rank among the keys that share them
+  int alike = n;                  // how many do
+#pragma unroll
   for (int round = 0; round < 3; ++round) {
+    if (round > 0 && alike <= kFewKeys) break;
     const int shift = round == 0 ? 21 : round == 1 ? 10 : 0;
     const uint32_t bins = round < 2 ? 2047u : 1023u;
-    hist[tid] = hist[tid + kEvictThreads] = 0;
-    __syncthreads();
-    each([&](int, uint32_t key, bool in) {
-      in = in && (key & above) == limit;
+    if (round > 0) {
+      clear();
+      __syncthreads();
+    }
+    int safe = 0;  // protected slots come first of all: they are counted apart
+    each([&](int, int, uint32_t key, bool in) {
+      if (round == 0) safe += __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && key == kProtected));
+      in = in && key != kProtected && (key & above) == limit;
       const unsigned long long m = __builtin_amdgcn_ballot_w64(in);
       if (!m) return;
-      const int bin = (key >> shift) & bins;
-      // (weights that are all alike would queue for one counter)
-      const int one = __builtin_amdgcn_readlane(bin, __builtin_ctzll(m));
-      if (__builtin_amdgcn_ballot_w64(in && bin != one) == 0) {
+      const int bin = (key >> shift) & bins, one = __builtin_amdgcn_readlane(bin, __builtin_ctzll(m));
+      if (__builtin_amdgcn_ballot_w64(in && bin != one) == 0) {  // (weights that are all alike would queue for one counter)
         if (lane == 0) atomicAdd(&hist[one], __builtin_popcountll(m));
       } else if (in) {
         atomicAdd(&hist[bin], 1);
       }
     });
+    if (round == 0 && lane == 0) part[2][w] = safe;
     __syncthreads();
-    // bins 2 t, 2 t + 1 of thread t; how many keys lie in the bins from there on
-    const int h0 = hist[2 * tid], h1 = hist[2 * tid + 1];
-    int from = h0 + h1;
-    for (int o = 1; o < 64; o <<= 1) {
-      const int x = __shfl_down(from, o);
-      if (lane + o < 64) from += x;
+    if (round == 0) {
+      const int all = over_waves(part[2], w).all;
+      if (all >= budget) {
+        limit = above = kProtected;
+        alike = all;
+        break;
+      }
+      rest -= all;
     }
-    if (lane == 0) part[1][w] = from;
+    // thread t: BPT bins, thread 0 the topmost; how many keys lie in the bins down to its last
+    int h[BPT], mine = 0;
+#pragma unroll
+    for (int i = 0; i < BPT; ++i) mine += h[i] = hist[kEvictBins - 1 - (BPT * tid + i)];
+    int down = lane_scan(mine);
+    if (lane == 63) part[1][w] = down;
     __syncthreads();
-    for (int i = w + 1; i < kEvictWaves; ++i) from += part[1][i];
-    if (from >= rest && from - h0 - h1 < rest) {
-      const int after1 = from - h0 - h1, hit1 = after1 + h1 >= rest;
-      found[0] = 2 * tid + hit1;
-      found[1] = rest - (hit1 ? after1 : after1 + h1);
+    down += over_waves(part[1], w).before;
+    int up = down - mine;
+    if (up < rest && down >= rest) {
+      int hit = 0;
+#pragma unroll
+      for (int i = 0; i < BPT - 1; ++i)
+        if (hit == i && up + h[i] < rest) up += h[i], ++hit;
+      found[round][0] = kEvictBins - 1 - (BPT * tid + hit);
+      found[round][1] = rest - up;
+      found[round][2] = h[0];
+#pragma unroll
+      for (int i = 1; i < BPT; ++i)
+        if (hit == i) found[round][2] = h[i];
     }
     __syncthreads();
-    limit |= (uint32_t)found[0] << shift;
+    limit |= (uint32_t)found[round][0] << shift;
     above |= bins << shift;
-    rest = found[1];
+    rest = found[round][1];
+    alike = found[round][2];
   }
-  // ---- who stays: larger keys, and the first `rest` equals
-  int equals = 0;
-  each([&](int, uint32_t key, bool in) { equals += __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && key == limit)); });
-  if (lane == 0) part[0][w] = equals;
-  __syncthreads();
-  int before = 0;
-  for (int i = 0; i < w; ++i) before += part[0][i];
-  auto each_kept = [&](auto f) {
-    int rank = before;
-    each([&](int slot, uint32_t key, bool in) {
-      const unsigned long long eq = __builtin_amdgcn_ballot_w64(in && key == limit);
-      const bool keep = in && (key > limit || (key == limit && rank + lane_before(eq) < rest));
-      rank += __builtin_popcountll(eq);
-      f(slot, in, keep);
+  if (alike <= kFewKeys) {  // they are written down and compared
+    each([&](int, int slot, uint32_t key, bool in) {
+      if (in && (key & above) == limit) {
+        const int at = atomicAdd(&few_count, 1);
+        few_keys[at] = key;
+        few_slots[at] = slot;
+      }
     });
-  };
+    __syncthreads();
+    if (tid < alike) {
+      const uint32_t key = few_keys[tid];
+      const int slot = few_slots[tid];
+      int ahead = 0;
+      for (int i = 0; i < alike; i += 4) {  // (what lies behind them is passed over)
+        const u32x4 k = *(const u32x4*)(few_keys + i);
+        const i32x4 x = *(const i32x4*)(few_slots + i);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) ahead += i + u < alike && (k[u] > key || (k[u] == key && x[u] < slot));
+      }
+      if (ahead == rest - 1) {
+        last_key = key;
+        last_slot = slot;
+      }
+    }
+  } else {  // (all of them equal: the rest-th in slot order)
+    int equals = 0;
+    each([&](int, int, uint32_t key, bool in) { equals += __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && key == limit)); });
+    if (lane == 0) part[0][w] = equals;
+    __syncthreads();
+    int rank = over_waves(part[0], w).before;
+    each([&](int, int slot, uint32_t key, bool in) {
+      const unsigned long long eq = __builtin_amdgcn_ballot_w64(in && key == limit);
+      if (in && key == limit && rank + lane_before(eq) == rest - 1) {
+        last_key = limit;
+        last_slot = slot;
+      }
+      rank += __builtin_popcountll(eq);
+    });
+  }
+  __syncthreads();
+  // ---- who stays
+  const uint32_t least = last_key;
+  const int least_slot = last_slot;
+  uint32_t kept = 0;  // (ITEMS > 0) of the lane's slots
   int nfree = 0, nmove = 0;
-  each_kept([&](int slot, bool in, bool keep) {
+  auto keeps = [&](int slot, uint32_t key, bool in) { return in && (key > least || (key == least && slot <= least_slot)); };
+  each([&](int i, int slot, uint32_t key, bool in) {
+    const bool keep = keeps(slot, key, in);
+    if (ITEMS > 0) kept |= (uint32_t)keep << i;
     nfree += __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && !keep && slot < budget));
     nmove += __builtin_popcountll(__builtin_amdgcn_ballot_w64(keep && slot >= budget));
   });
   if (lane == 0) {
-    part[1][w] = nfree;
-    part[2][w] = nmove;
+    part[2][w] = nfree;
+    part[3][w] = nmove;
   }
   __syncthreads();
-  int free_at = 0, move_at = 0, count = 0;
-  for (int i = 0; i < kEvictWaves; ++i) {
-    if (i < w) {
-      free_at += part[1][i];
-      move_at += part[2][i];
-    }
-    count += part[2][i];
-  }
-  int32_t* dst = a.moves + gridDim.x + (long)pair * 2 * a.room;
-  int32_t* src = dst + a.room;
-  each_kept([&](int slot, bool in, bool keep) {
+  int free_at = over_waves(part[2], w).before;
+  const BeforeAndAll moved = over_waves(part[3], w);
+  int move_at = moved.before;
+  const int count = moved.all;
+  int32_t* const dst = here ? few[0] : a.moves + gridDim.x + (long)pair * 2 * a.room;
+  int32_t* const src = here ? few[1] : dst + a.room;
+  each([&](int i, int slot, uint32_t key, bool in) {
+    const bool keep = ITEMS > 0 ? kept >> i & 1 : keeps(slot, key, in);
     const bool fr = in && !keep && slot < budget, mv = keep && slot >= budget;
     const unsigned long long mf = __builtin_amdgcn_ballot_w64(fr), mm = __builtin_amdgcn_ballot_w64(mv);
-    if (fr) dst[free_at + lane_before(mf)] = slot;
-    if (mv) src[move_at + lane_before(mm)] = slot;
-    free_at += __builtin_popcountll(mf);
-    move_at += __builtin_popcountll(mm);
+    if (mf) {
+      if (fr) dst[free_at + lane_before(mf)] = slot;
+      free_at += __builtin_popcountll(mf);
+    }
+    if (mm) {
+      if (mv) src[move_at + lane_before(mm)] = slot;
+      move_at += __builtin_popcountll(mm);
+    }
     if (keep && slot < budget) {
-      if (Wo != W) Wo[slot] = W[slot];
-      if (Po != P) Po[slot] = P[slot];
+      if (Wo != W) Wo[slot] = ITEMS > 0 ? wt[i] : W[slot];
+      if (Po != P) Po[slot] = ITEMS > 0 ? pos[i] : P[slot];
     }
   });
-  if (tid == 0) a.moves[pair] = count;
+  if (!here && tid == 0) a.moves[pair] = count;
   __syncthreads();
-  for (int j = tid; j < count; j += kEvictThreads) {  // (sources lie at or past the budget, where nothing is written)
+  for (int j = tid; j < count; j += THREADS) {  // (sources lie at or past the budget, where nothing is written)
     Wo[dst[j]] = W[src[j]];
     Po[dst[j]] = P[src[j]];
   }
+  if (here) {
+    const int cpr = a.c.d / 8;
+    for (int i = tid; i < count * cpr; i += THREADS) move_piece(a, s, g, src[i / cpr], dst[i / cpr], i % cpr);
+  }
 }
 
-// The moves of K and V rows, 16 bytes a thread; and the lengths, which the kernel above still reads.
+__device__ __forceinline__ void cut_length(const EvictArgs& a, int s) {
+  const int n = held_keys(a.c, s);
+  a.lens_out[s] = n < a.budget ? n : a.budget;
+}
+// The moves of K and V rows; and the lengths, where they are cut in place and the kernel above still reads them.
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
-  const CacheView& c = a.c;
-  const int pairs = a.nseq * c.Hkv, pair = blockIdx.x, s = pair / c.Hkv, g = pair - s * c.Hkv;
-  if (blockIdx.y == 0 && g == 0 && threadIdx.x == 0) {
-    const int n = held_keys(c, s);
-    a.lens_out[s] = n < a.budget ? n : a.budget;
-  }
+  const int pairs = a.nseq * a.c.Hkv, pair = blockIdx.x, s = pair / a.c.Hkv, g = pair - s * a.c.Hkv;
+  if (a.lens_out == a.c.lens && blockIdx.y == 0 && g == 0 && threadIdx.x == 0) cut_length(a, s);
   const int count = a.moves[pair];
   const int32_t* dst = a.moves + pairs + (long)pair * 2 * a.room;
   const int32_t* src = dst + a.room;
-  const int cpr = c.d / 8;
+  const int cpr = a.c.d / 8;
   const long pieces = (long)count * cpr;
   for (long i = (long)blockIdx.y * 256 + threadIdx.x; i < pieces; i += (long)gridDim.y * 256) {
-    const int j = (int)(i / cpr), piece = (int)(i - (long)j * cpr);
-    const long from = (cache_row(c, s, src[j]) * c.Hkv + g) * c.d + 8 * piece, to = (cache_row(c, s, dst[j]) * c.Hkv + g) * c.d + 8 * piece;
-    const u32x4 k = *(const u32x4*)(a.K + from), v = *(const u32x4*)(a.V + from);
-    *(u32x4*)(a.K + to) = k;
-    *(u32x4*)(a.V + to) = v;
+    const int j = (int)(i / cpr);
+    move_piece(a, s, g, src[j], dst[j], (int)(i - (long)j * cpr));
   }
+}
+__global__ __launch_bounds__(256) void evict_lengths_kernel(EvictArgs a) {
+  const int s = blockIdx.x * 256 + threadIdx.x;
+  if (s < a.nseq) cut_length(a, s);
 }
 
 hipError_t launch_evict(const EvictArgs& a, hipStream_t st) {
   const unsigned pairs = (unsigned)(a.nseq * a.c.Hkv);
-  const dim3 block(kEvictThreads);
-  if (a.c.Nk <= 2 * kEvictThreads) hipLaunchKernelGGL(evict_select_kernel<2>, dim3(pairs), block, 0, st, a);
-  else if (a.c.Nk <= 8 * kEvictThreads) hipLaunchKernelGGL(evict_select_kernel<8>, dim3(pairs), block, 0, st, a);
-  else hipLaunchKernelGGL(evict_select_kernel<0>, dim3(pairs), block, 0, st, a);
+  if (a.c.Nk <= 4096) hipLaunchKernelGGL((evict_select_kernel<256, 16>), dim3(pairs), dim3(256), 0, st, a);
+  else if (a.c.Nk <= 8192) hipLaunchKernelGGL((evict_select_kernel<1024, 8>), dim3(pairs), dim3(1024), 0, st, a);
+  else hipLaunchKernelGGL((evict_select_kernel<1024, 0>), dim3(pairs), dim3(1024), 0, st, a);
   if (hipError_t e = hipGetLastError()) return e;
+  if (a.room <= kFewMoves) {
+    if (a.lens_out != a.c.lens) return hipSuccess;
+    hipLaunchKernelGGL(evict_lengths_kernel, dim3((a.nseq + 255) / 256), dim3(256), 0, st, a);
+    return hipGetLastError();
+  }
   const long most = (long)a.room * (a.c.d / 8);  // pieces of a pair
   long y = (most + 255) / 256;
   y = y < 1 ? 1 : (y > 64 ? 64 : y);
