@@ -1112,6 +1112,10 @@ def fa_prefix_fwd(Q, Kprefix, Vprefix, Kcache, Vcache, scale: float, causal: boo
     (Kcache, Vcache, seqlens_k, block_table, max_seqlen_k as fa_kvcache_fwd; lengths count the own keys alone). The prefix is read once for
     the batch: Kprefix, Vprefix [Np,Hkv,d], or with prefix_table (int32 page numbers on the GPU) pools [pages,page_size,Hkv,d], of which
     the first prefix_len keys are meant. The causal rule holds among own keys. Returns O [B,Nq,Hq,d] and LSE [B,Hq,Nq] fp32 (of all keys)."""
+    if _host and O is None and LSE is None and workspace is None:
+        r = _host.prefix_fwd(Q, Kprefix, Vprefix, Kcache, Vcache, scale, causal, seqlens_k, block_table, prefix_table, prefix_len, max_seqlen_k)
+        if r is not None:
+            return r
     import torch
     et = _elem_type(Q)
     _need(Q, "Q", et)
@@ -1166,6 +1170,8 @@ def fa_cache_append(Knew, Vnew, Kcache, Vcache, seqlens_k=None, block_table=None
     """New keys and values Knew, Vnew [B,Nq,Hkv,d] (bf16 or fp16) into the slots seqlens_k[b] - Nq .. of every sequence's cache (slabs or
     pages as fa_kvcache_fwd; seqlens_k counts the new keys already). weights [B,Hkv,slots] fp32 and positions [B,Hkv,slots] int32, where
     given: weight 0 and position first_position[b] + i (int32 [B]; None: the slot) for the new slots. Returns the caches."""
+    if _host and _host.cache_append(Knew, Vnew, Kcache, Vcache, seqlens_k, block_table, weights, positions, first_position):
+        return Kcache, Vcache
     import torch
     et = _elem_type(Knew)
     _need(Knew, "Knew", et)
@@ -1194,6 +1200,8 @@ def fa_cache_weights(Q, Kcache, LSE, weights, scale: float, causal: bool, seqlen
     """weights [B,Hkv,slots] fp32 += the attention weight that each cached key draws from the queries Q [B,Nq,Hq,d] (bf16 or fp16), summed
     over the queries and the heads of its group: exp(scale q.k - LSE), LSE [B,Hq,Nq] fp32 from the attention over these keys.
     queries (int32 [B]): only the first of each sequence count (accepted drafts). Cache and lengths as fa_kvcache_fwd. Returns weights."""
+    if _host and _host.cache_weights(Q, Kcache, LSE, weights, scale, causal, seqlens_k, block_table, queries):
+        return weights
     import torch
     et = _elem_type(Q)
     _need(Q, "Q", et)
@@ -1218,6 +1226,12 @@ def fa_cache_evict(Kcache, Vcache, weights, positions, seqlens_k, budget: int, s
     of the largest weight; kept rows past the budget move into the free slots below it, in place. weights fp32, positions int32
     [B,Hkv,slots] and seqlens_k int32 [B] are updated in place, or written to weights_out, positions_out, seqlens_out. Returns those
     three."""
+    weights_out = weights if weights_out is None else weights_out
+    positions_out = positions if positions_out is None else positions_out
+    seqlens_out = seqlens_k if seqlens_out is None else seqlens_out
+    if _host and workspace is None and _host.cache_evict(Kcache, Vcache, weights, positions, seqlens_k, budget, sinks, recent, block_table,
+                                                         weights_out, positions_out, seqlens_out):
+        return weights_out, positions_out, seqlens_out
     import torch
     et = _elem_type(Kcache)
     if Kcache.dim() != 4:
@@ -1230,9 +1244,9 @@ def fa_cache_evict(Kcache, Vcache, weights, positions, seqlens_k, budget: int, s
     _need(positions, "positions", torch.int32, shape, dev)
     _need(seqlens_k, "seqlens_k", torch.int32, (B,), dev)
     Nk, page_size, pages = _cache_slots(Kcache, block_table, B, slots, dev)
-    weights_out = weights if weights_out is None else _out(weights_out, "weights_out", shape, torch.float32, dev)
-    positions_out = positions if positions_out is None else _out(positions_out, "positions_out", shape, torch.int32, dev)
-    seqlens_out = seqlens_k if seqlens_out is None else _out(seqlens_out, "seqlens_out", (B,), torch.int32, dev)
+    _need(weights_out, "weights_out", torch.float32, shape, dev)
+    _need(positions_out, "positions_out", torch.int32, shape, dev)
+    _need(seqlens_out, "seqlens_out", torch.int32, (B,), dev)
     ws = _workspace(workspace, fa_cache_evict_workspace_bytes(B, Hkv, Nk, budget), dev)
     _check(fa_cache_evict_raw(_ptr(Kcache), _ptr(Vcache), _ptr(weights), _ptr(positions), _ptr(seqlens_k), _ptr(block_table),
                               _ptr(weights_out), _ptr(positions_out), _ptr(seqlens_out), _ptr(ws), _wsbytes(ws), B, Hkv, Nk, d, budget,
@@ -1263,6 +1277,10 @@ def fa_verify_drafts(draft_tokens, draft_probs, target, uniform, logits: bool = 
     probabilities [B,k+1,V] (logits=True: softmax(inv_temperature * target)), with uniform [B,k+1] fp32 in [0,1): k to accept with, the
     last to draw the next token with. Values fp32, bf16 or fp16; rows may be slices of wider ones. Returns tokens [B,k+1] int32 (the
     accepted drafts, the drawn token, then -1) and accepted [B] int32."""
+    if _host and tokens is None and accepted is None and workspace is None:
+        r = _host.verify_drafts(draft_tokens, draft_probs, target, uniform, logits, inv_temperature)
+        if r is not None:
+            return r
     import torch
     dev = target.device
     if draft_tokens.dim() != 2 or target.dim() != 3:

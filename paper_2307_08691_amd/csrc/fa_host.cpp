@@ -32,7 +32,9 @@ namespace {
   X(fa_cross_bwd_workspace_bytes) X(fa_dropout_fwd) X(fa_dropout_fwd_f16) X(fa_dropout_bwd) X(fa_dropout_bwd_f16)       \
   X(fa_local_fwd) X(fa_local_fwd_f16) X(fa_local_bwd) X(fa_local_bwd_f16) X(fa_varlen_fwd) X(fa_varlen_fwd_f16)         \
   X(fa_varlen_bwd) X(fa_varlen_bwd_f16) X(fa_varlen_bwd_workspace_bytes) X(fa_kvcache_fwd) X(fa_kvcache_fwd_f16)        \
-  X(fa_splitkv_fwd_workspace_bytes)
+  X(fa_splitkv_fwd_workspace_bytes) X(fa_prefix_fwd) X(fa_prefix_fwd_f16) X(fa_prefix_fwd_workspace_bytes) X(fa_cache_append)      \
+  X(fa_cache_weights) X(fa_cache_weights_f16) X(fa_cache_evict) X(fa_cache_evict_workspace_bytes) X(fa_verify_drafts)             \
+  X(fa_verify_drafts_workspace_bytes)
 struct Entries {
 #define X(name) decltype(&::name) name;
   FA_HOST_ENTRIES(X)
@@ -355,6 +357,235 @@ PyObject* kvcache_fwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- a decoding batch
+
+// A cache [B, Nk, Hkv, d], or pools of pages and a table [B, pages]: as binding._cache_slots. `slots` 0: all there are.
+struct Cache {
+  const at::Tensor *K, *table = nullptr;
+  int slots, page = 0, pages = 0;
+  bool parse(const at::Tensor* k, PyObject* table_arg, int B, int slots_, c10::Device dev) {
+    K = k, slots = slots_;
+    if (table_arg == Py_None) {
+      if (K->size(0) != B || (slots && slots != K->size(1))) return false;
+      slots = (int)K->size(1);
+      return true;
+    }
+    table = plain(table_arg);
+    if (!table || table->dim() != 2 || !is(table, at::kInt, dev, {B, table->size(1)})) return false;
+    page = (int)K->size(1), pages = (int)table->size(1);
+    const long all = (long)page * pages;
+    if (all > INT_MAX || slots > all) return false;
+    if (!slots) slots = (int)all;
+    return true;
+  }
+  const int32_t* pages_of() const { return table ? (const int32_t*)in(table) : nullptr; }
+};
+// An optional int32 vector of B
+bool lengths(PyObject* o, int B, c10::Device dev, const int32_t*& v) {
+  v = nullptr;
+  if (o == Py_None) return true;
+  const at::Tensor* t = plain(o);
+  if (!is(t, at::kInt, dev, {B})) return false;
+  v = (const int32_t*)in(t);
+  return true;
+}
+
+// Q, Kprefix, Vprefix, Kcache, Vcache, scale, causal, seqlens_k, block_table, prefix_table, prefix_len, max_seqlen_k
+PyObject* prefix_fwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 12 || !plain_context()) Py_RETURN_NONE;
+  const at::Tensor *Q = plain(args[0]), *Kp = plain(args[1]), *Vp = plain(args[2]), *K = plain(args[3]), *V = plain(args[4]), *ptab = nullptr;
+  float scale;
+  int causal, prefix_len, max_k, prefix_pages = 0;
+  const int32_t* lens;
+  Cache c;
+  void* st;
+  if (!Q || !Kp || !K || Q->dim() != 4 || K->dim() != 4 || !number(args[5], scale) || !flag(args[6], causal) || !integer(args[10], prefix_len) ||
+      !integer(args[11], max_k))
+    Py_RETURN_NONE;
+  const at::ScalarType et = Q->scalar_type();
+  const c10::Device dev = Q->device();
+  const bool f16 = et == at::kHalf;
+  const int B = (int)Q->size(0), Nq = (int)Q->size(1), Hq = (int)Q->size(2), d = (int)Q->size(3), Hkv = (int)K->size(2);
+  if ((et != at::kBFloat16 && !f16) || K->size(3) != d || !is(K, et, dev, K->sizes()) || !is(V, et, dev, K->sizes()) || Hq % Hkv) Py_RETURN_NONE;
+  if (max_k < 0 || !c.parse(K, args[8], B, args[8] == Py_None ? 0 : max_k, dev) || !lengths(args[7], B, dev, lens)) Py_RETURN_NONE;
+  if (!is(Kp, et, dev, Kp->sizes()) || !is(Vp, et, dev, Kp->sizes())) Py_RETURN_NONE;
+  long Np = prefix_len;
+  int page = c.page;
+  if (args[9] == Py_None) {
+    if (Kp->dim() != 3 || Kp->size(1) != Hkv || Kp->size(2) != d || Np < 0 || Np > Kp->size(0)) Py_RETURN_NONE;
+    if (Np == 0) Np = Kp->size(0);
+  } else {
+    ptab = plain(args[9]);
+    if (!ptab || ptab->dim() != 1 || !is(ptab, at::kInt, dev, ptab->sizes()) || Kp->dim() != 4 || Kp->size(2) != Hkv || Kp->size(3) != d ||
+        (c.table && Kp->size(1) != page))
+      Py_RETURN_NONE;
+    page = (int)Kp->size(1), prefix_pages = (int)ptab->size(0);
+    if (Np <= 0 || Np > (long)page * prefix_pages) Py_RETURN_NONE;
+  }
+  const size_t nb = lib.fa_prefix_fwd_workspace_bytes(B, Hq, Hkv, Nq, (int)Np, c.slots, d);
+  if (!nb) Py_RETURN_NONE;
+  if (!current_stream(st)) return nullptr;
+  at::Tensor O = make(Q->sizes(), et, dev), L = make({B, Hq, Nq}, at::kFloat, dev), W = make({(int64_t)nb}, at::kByte, dev);
+  const void *q = in(Q), *kp = in(Kp), *vp = in(Vp), *k = in(K), *v = in(V);
+  const int32_t *tb = c.pages_of(), *pt = ptab ? (const int32_t*)in(ptab) : nullptr;
+  void *o = O.mutable_data_ptr(), *w = W.mutable_data_ptr();
+  float* l = (float*)L.mutable_data_ptr();
+  const int e = without_gil([&] {
+    return (f16 ? lib.fa_prefix_fwd_f16 : lib.fa_prefix_fwd)(q, kp, vp, pt, k, v, lens, tb, o, l, w, nb, B, Hq, Hkv, Nq, (int)Np, c.slots, d, page,
+                                                             prefix_pages, c.pages, scale, causal, st);
+  });
+  if (e) Py_RETURN_NONE;
+  return pack({O, L});
+  END_HANDLE_TH_ERRORS
+}
+
+// Knew, Vnew, Kcache, Vcache, seqlens_k, block_table, weights, positions, first_position -> True
+PyObject* cache_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 9 || !plain_context()) Py_RETURN_NONE;
+  const at::Tensor *Kn = plain(args[0]), *Vn = plain(args[1]), *K = plain(args[2]), *V = plain(args[3]), *W = nullptr, *P = nullptr;
+  const int32_t *lens, *first;
+  Cache c;
+  void* st;
+  if (!Kn || !K || Kn->dim() != 4 || K->dim() != 4) Py_RETURN_NONE;
+  const at::ScalarType et = Kn->scalar_type();
+  const c10::Device dev = Kn->device();
+  const int B = (int)Kn->size(0), Nq = (int)Kn->size(1), Hkv = (int)Kn->size(2), d = (int)Kn->size(3);
+  if ((et != at::kBFloat16 && et != at::kHalf) || !is(Vn, et, dev, Kn->sizes()) || !is(K, et, dev, {K->size(0), K->size(1), Hkv, d}) ||
+      !is(V, et, dev, K->sizes()))
+    Py_RETURN_NONE;
+  int slots = 0;
+  if (args[6] != Py_None) {
+    W = plain(args[6]);
+    if (!W || W->dim() != 3 || !is(W, at::kFloat, dev, {B, Hkv, W->size(2)})) Py_RETURN_NONE;
+    slots = (int)W->size(2);
+  }
+  if (args[7] != Py_None) {
+    P = plain(args[7]);
+    if (!P || P->dim() != 3 || !is(P, at::kInt, dev, {B, Hkv, P->size(2)}) || (W && slots != P->size(2))) Py_RETURN_NONE;
+    slots = (int)P->size(2);
+  }
+  if (!c.parse(K, args[5], B, slots, dev) || !lengths(args[4], B, dev, lens) || !lengths(args[8], B, dev, first)) Py_RETURN_NONE;
+  if (!current_stream(st)) return nullptr;
+  const void *kn = in(Kn), *vn = in(Vn);
+  void *k = K->mutable_data_ptr(), *v = V->mutable_data_ptr();
+  float* w = W ? (float*)W->mutable_data_ptr() : nullptr;
+  int32_t* p = P ? (int32_t*)P->mutable_data_ptr() : nullptr;
+  const int32_t* tb = c.pages_of();
+  const int e = without_gil([&] { return lib.fa_cache_append(kn, vn, k, v, lens, tb, w, p, first, B, Hkv, Nq, c.slots, d, c.page, c.pages, st); });
+  if (e) Py_RETURN_NONE;
+  Py_RETURN_TRUE;
+  END_HANDLE_TH_ERRORS
+}
+
+// Q, Kcache, LSE, weights, scale, causal, seqlens_k, block_table, queries -> True
+PyObject* cache_weights(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 9 || !plain_context()) Py_RETURN_NONE;
+  const at::Tensor *Q = plain(args[0]), *K = plain(args[1]), *L = plain(args[2]), *W = plain(args[3]);
+  float scale;
+  int causal;
+  const int32_t *lens, *queries;
+  Cache c;
+  void* st;
+  if (!Q || !K || !W || Q->dim() != 4 || K->dim() != 4 || W->dim() != 3 || !number(args[4], scale) || !flag(args[5], causal)) Py_RETURN_NONE;
+  const at::ScalarType et = Q->scalar_type();
+  const c10::Device dev = Q->device();
+  const bool f16 = et == at::kHalf;
+  const int B = (int)Q->size(0), Nq = (int)Q->size(1), Hq = (int)Q->size(2), d = (int)Q->size(3), Hkv = (int)K->size(2);
+  if ((et != at::kBFloat16 && !f16) || K->size(3) != d || !is(K, et, dev, K->sizes()) || !is(L, at::kFloat, dev, {B, Hq, Nq}) ||
+      !is(W, at::kFloat, dev, {B, Hkv, W->size(2)}) || !c.parse(K, args[7], B, (int)W->size(2), dev) || !lengths(args[6], B, dev, lens) ||
+      !lengths(args[8], B, dev, queries))
+    Py_RETURN_NONE;
+  if (!current_stream(st)) return nullptr;
+  const void *q = in(Q), *k = in(K);
+  const float* l = stat(L);
+  float* w = (float*)W->mutable_data_ptr();
+  const int32_t* tb = c.pages_of();
+  const int e = without_gil([&] {
+    return (f16 ? lib.fa_cache_weights_f16 : lib.fa_cache_weights)(q, k, l, lens, tb, queries, w, B, Hq, Hkv, Nq, c.slots, d, c.page, c.pages, scale,
+                                                                   causal, st);
+  });
+  if (e) Py_RETURN_NONE;
+  Py_RETURN_TRUE;
+  END_HANDLE_TH_ERRORS
+}
+
+// Kcache, Vcache, weights, positions, seqlens_k, budget, sinks, recent, block_table, weights_out, positions_out, seqlens_out -> True
+PyObject* cache_evict(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 12 || !plain_context()) Py_RETURN_NONE;
+  const at::Tensor *K = plain(args[0]), *V = plain(args[1]), *W = plain(args[2]), *P = plain(args[3]), *n = plain(args[4]), *Wo = plain(args[9]),
+                   *Po = plain(args[10]), *no = plain(args[11]);
+  int budget, sinks, recent;
+  Cache c;
+  void* st;
+  if (!K || !W || !n || K->dim() != 4 || W->dim() != 3 || !integer(args[5], budget) || !integer(args[6], sinks) || !integer(args[7], recent))
+    Py_RETURN_NONE;
+  const at::ScalarType et = K->scalar_type();
+  const c10::Device dev = K->device();
+  const int B = (int)W->size(0), Hkv = (int)K->size(2), d = (int)K->size(3), slots = (int)W->size(2);
+  if ((et != at::kBFloat16 && et != at::kHalf) || !is(V, et, dev, K->sizes()) || !is(W, at::kFloat, dev, {B, Hkv, slots}) ||
+      !is(P, at::kInt, dev, W->sizes()) || !is(n, at::kInt, dev, {B}) || !is(Wo, at::kFloat, dev, W->sizes()) || !is(Po, at::kInt, dev, W->sizes()) ||
+      !is(no, at::kInt, dev, {B}) || budget <= 0 || !c.parse(K, args[8], B, slots, dev))
+    Py_RETURN_NONE;
+  if (!current_stream(st)) return nullptr;
+  const size_t nb = lib.fa_cache_evict_workspace_bytes(B, Hkv, slots, budget);
+  at::Tensor S = make({(int64_t)nb}, at::kByte, dev);
+  void *k = K->mutable_data_ptr(), *v = V->mutable_data_ptr(), *s = S.mutable_data_ptr();
+  const float* w = stat(W);
+  const int32_t *p = (const int32_t*)in(P), *len = (const int32_t*)in(n), *tb = c.pages_of();
+  float* wo = (float*)Wo->mutable_data_ptr();
+  int32_t *po = (int32_t*)Po->mutable_data_ptr(), *lo = (int32_t*)no->mutable_data_ptr();
+  const int e = without_gil([&] {
+    return lib.fa_cache_evict(k, v, w, p, len, tb, wo, po, lo, s, nb, B, Hkv, slots, d, budget, sinks, recent, c.page, c.pages, st);
+  });
+  if (e) Py_RETURN_NONE;
+  Py_RETURN_TRUE;
+  END_HANDLE_TH_ERRORS
+}
+
+int value_type(const at::Tensor* t) {
+  switch (t->scalar_type()) {
+    case at::kFloat: return FA_TYPE_F32;
+    case at::kBFloat16: return FA_TYPE_BF16;
+    case at::kHalf: return FA_TYPE_F16;
+    default: return -1;
+  }
+}
+// draft_tokens, draft_probs, target, uniform, logits, inv_temperature (contiguous rows; others binding.py takes)
+PyObject* verify_drafts(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 6 || !plain_context()) Py_RETURN_NONE;
+  const at::Tensor *x = plain(args[0]), *q = nullptr, *t = plain(args[2]), *u = plain(args[3]);
+  int logits;
+  float inv_t;
+  void* st;
+  if (!x || !t || x->dim() != 2 || t->dim() != 3 || !flag(args[4], logits) || !number(args[5], inv_t)) Py_RETURN_NONE;
+  const c10::Device dev = t->device();
+  const int B = (int)x->size(0), k = (int)x->size(1), V = (int)t->size(2), type = value_type(t);
+  int q_type = 0;
+  if (args[1] != Py_None) {
+    q = plain(args[1]);
+    if (!q || (q_type = value_type(q)) < 0 || !is(q, q->scalar_type(), dev, {B, k, V})) Py_RETURN_NONE;
+  }
+  if (type < 0 || !is(x, at::kInt, dev, {B, k}) || !is(t, t->scalar_type(), dev, {B, k + 1, V}) || !is(u, at::kFloat, dev, {B, k + 1})) Py_RETURN_NONE;
+  const size_t nb = lib.fa_verify_drafts_workspace_bytes(B, k, V);
+  if (!nb) Py_RETURN_NONE;
+  if (!current_stream(st)) return nullptr;
+  at::Tensor T = make({B, k + 1}, at::kInt, dev), A = make({B}, at::kInt, dev), W = make({(int64_t)nb}, at::kByte, dev);
+  const int32_t* xs = (const int32_t*)in(x);
+  const void *qs = q ? in(q) : nullptr, *ts = in(t);
+  const float* us = stat(u);
+  int32_t *to = (int32_t*)T.mutable_data_ptr(), *ac = (int32_t*)A.mutable_data_ptr();
+  void* w = W.mutable_data_ptr();
+  const int e = without_gil([&] { return lib.fa_verify_drafts(xs, qs, ts, us, to, ac, w, nb, B, k, V, V, V, q_type, type, logits, inv_t, st); });
+  if (e) Py_RETURN_NONE;
+  return pack({T, A});
+  END_HANDLE_TH_ERRORS
+}
+
 PyObject* cache_splits(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   int v[6], ragged;
   for (int i = 0; i < 6; ++i)
@@ -400,6 +631,7 @@ PyObject* entry_names(PyObject*, PyObject*) {
 
 #define FAST(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(dense_fwd), FAST(dense_bwd), FAST(varlen_fwd), FAST(varlen_bwd), FAST(kvcache_fwd), FAST(cache_splits),
+                         FAST(prefix_fwd), FAST(cache_append), FAST(cache_weights), FAST(cache_evict), FAST(verify_drafts),
                          {"init", init, METH_VARARGS, nullptr}, {"entry_names", entry_names, METH_NOARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
