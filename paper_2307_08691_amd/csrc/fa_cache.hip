@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include "fa_kernels.h"
+#include "fa_lds.h"
 
 namespace fa {
 
@@ -110,13 +111,28 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
   __shared__ int few[2][kFewMoves];
   const int pair = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int s = pair / a.c.Hkv, g = pair - s * a.c.Hkv, n = held_keys(a.c, s), budget = a.budget;
+  const int s = pair / a.c.Hkv, g = pair - s * a.c.Hkv, budget = a.budget;
   const bool here = a.room <= kFewMoves;
   const long base = (long)pair * a.c.Nk;
   const float* W = a.weights + base;
   const int32_t* P = a.positions + base;
   float* Wo = a.weights_out + base;
   int32_t* Po = a.positions_out + base;
+  // This lane: slots first + 64 i. They go by the slots that there are, not by those in use, so that the values are requested together
+  // with the length.
+  const int steps = (a.c.Nk + THREADS - 1) / THREADS, first = w * steps * 64 + lane;
+  constexpr bool KEPT = ITEMS > 0 && ITEMS <= 8;  // weights and positions stay in registers too
+  float wt[KEPT ? ITEMS : 1];
+  int pos[KEPT ? ITEMS : 1];
+  if constexpr (KEPT) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {  // (slots that are not there: the last one again)
+      const int slot = i < steps && first + 64 * i < a.c.Nk ? first + 64 * i : a.c.Nk - 1;
+      wt[i] = W[slot];
+      pos[i] = P[slot];
+    }
+  }
+  const int n = held_keys(a.c, s);
   if (a.lens_out != a.c.lens && g == 0 && tid == 0) a.lens_out[s] = n < budget ? n : budget;  // (else others still read it)
   if (n <= budget) {  // nothing goes
     if (!here && tid == 0) a.moves[pair] = 0;
@@ -126,25 +142,18 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
       for (int i = tid; i < n; i += THREADS) Po[i] = P[i];
     return;
   }
-  const int steps = (n + THREADS - 1) / THREADS, first = w * steps * 64 + lane;  // this lane: slots first + 64 i
   auto clear = [&]() {
 #pragma unroll
     for (int i = 0; i < BPT; ++i) hist[tid + i * THREADS] = 0;
   };
-  float wt[ITEMS ? ITEMS : 1];
-  int pos[ITEMS ? ITEMS : 1], top = -0x7fffffff - 1;  // top: the newest position
-  if constexpr (ITEMS > 0) {
+  int top = -0x7fffffff - 1;  // the newest position
+  clear();
+  if constexpr (KEPT) {
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {  // (slots that are not there: the last one again)
-      const int slot = i < steps && first + 64 * i < n ? first + 64 * i : n - 1;
-      wt[i] = W[slot];
-      pos[i] = P[slot];
-    }
-    clear();
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i) top = max(top, pos[i]);
+    for (int i = 0; i < ITEMS; ++i)
+      if (first + 64 * i < n) top = max(top, pos[i]);
   } else {
-    clear();
+#pragma unroll 8
     for (int i = 0; i < steps; ++i) top = max(top, P[first + 64 * i < n ? first + 64 * i : n - 1]);
   }
   for (int o = 32; o; o >>= 1) top = max(top, __shfl_xor(top, o));
@@ -158,9 +167,15 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
   }
   const long recent_from = (long)top + 1 - a.recent;
   uint32_t held[ITEMS ? ITEMS : 1];
-  if constexpr (ITEMS > 0) {
+  if constexpr (KEPT) {
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) held[i] = evict_key(wt[i], pos[i], a.sinks, recent_from);
+  } else if constexpr (ITEMS > 0) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int slot = first + 64 * i < n ? first + 64 * i : n - 1;
+      held[i] = evict_key(W[slot], P[slot], a.sinks, recent_from);
+    }
   }
   auto each = [&](auto f) {  // f(i, slot, key, whether the slot is held), for whole wavefronts
     if constexpr (ITEMS > 0) {
@@ -314,12 +329,13 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
       move_at += __builtin_popcountll(mm);
     }
     if (keep && slot < budget) {
-      if (Wo != W) Wo[slot] = ITEMS > 0 ? wt[i] : W[slot];
-      if (Po != P) Po[slot] = ITEMS > 0 ? pos[i] : P[slot];
+      if (Wo != W) Wo[slot] = KEPT ? wt[i] : W[slot];
+      if (Po != P) Po[slot] = KEPT ? pos[i] : P[slot];
     }
   });
   if (!here && tid == 0) a.moves[pair] = count;
-  __syncthreads();
+  if (here) lds_barrier();  // (the lists are in LDS: what has been stored to memory need not have arrived)
+  else __syncthreads();
   for (int j = tid; j < count; j += THREADS) {  // (sources lie at or past the budget, where nothing is written)
     Wo[dst[j]] = W[src[j]];
     Po[dst[j]] = P[src[j]];
@@ -355,8 +371,11 @@ __global__ __launch_bounds__(256) void evict_lengths_kernel(EvictArgs a) {
 
 hipError_t launch_evict(const EvictArgs& a, hipStream_t st) {
   const unsigned pairs = (unsigned)(a.nseq * a.c.Hkv);
-  if (a.c.Nk <= 4096) hipLaunchKernelGGL((evict_select_kernel<256, 16>), dim3(pairs), dim3(256), 0, st, a);
+  // (us at 256 / 512 / 1024 threads: 64 x 8 pairs of 2112 slots 12.4 / 10.8 / 16.6, 1 x 8 of 4096 19.8 / 14.3 / 14.5; 8 x 8 of 8192 at 512 / 1024:
+  // 26.0 / 24.0; 2 x 8 of 32768: 110 with keys formed anew in every round, 76 with them in registers)
+  if (a.c.Nk <= 4096) hipLaunchKernelGGL((evict_select_kernel<512, 8>), dim3(pairs), dim3(512), 0, st, a);
   else if (a.c.Nk <= 8192) hipLaunchKernelGGL((evict_select_kernel<1024, 8>), dim3(pairs), dim3(1024), 0, st, a);
+  else if (a.c.Nk <= 32768) hipLaunchKernelGGL((evict_select_kernel<1024, 32>), dim3(pairs), dim3(1024), 0, st, a);
   else hipLaunchKernelGGL((evict_select_kernel<1024, 0>), dim3(pairs), dim3(1024), 0, st, a);
   if (hipError_t e = hipGetLastError()) return e;
   if (a.room <= kFewMoves) {

@@ -332,15 +332,17 @@ def check_evict(dtype, B, hkv, d, slots, page, lens, budget, sinks, recent, weig
     (1, 1, 8, 2, 0, [2], 1, 0, 0),
     (3, 2, 64, 200, 0, [200, 100, 101], 100, 4, 20),
     (4, 2, 128, 300, 64, [300, 0, 65, 1], 64, 0, 64),
-    (2, 3, 72, 2500, 0, [2500, 2047], 1000, 4, 100),   # keys held in registers, eight a lane
-    (1, 2, 64, 9000, 128, [8999], 8000, 1, 7),          # keys formed anew
+    (2, 3, 72, 2500, 0, [2500, 2047], 1000, 4, 100),
+    (2, 1, 8, 5000, 0, [5000, 4100], 4050, 4, 100),     # 1024 threads, eight keys a lane in registers
+    (1, 2, 64, 9000, 128, [8999], 8000, 1, 7),          # 32 keys a lane in registers
+    (1, 2, 8, 33000, 0, [32999], 500, 1, 7),            # keys formed anew
     (2, 1, 256, 2048, 64, [2048, 1500], 17, 4, 4),
 ])
 def test_evict(B, hkv, d, slots, page, lens, budget, sinks, recent, in_place):
     check_evict("bf16" if d != 64 else "f16", B, hkv, d, slots, page, lens, budget, sinks, recent, in_place=in_place)
 
 
-@pytest.mark.parametrize("slots", [700, 8500])
+@pytest.mark.parametrize("slots", [700, 8500, 33000])
 def test_evict_equal_and_odd_weights(slots):
     """Ties go to the lower slot; zeros of both signs are one; NaN is less than everything, infinities count; few distinct values."""
     lens, some = [slots, slots - 333], [0.0, -0.0, np.nan, np.inf, -np.inf, 1.0, -1.0, 1e-42]
