@@ -45,7 +45,13 @@ __device__ __forceinline__ void dma16(const void* gaddr, const void* lds) {
                "s"(__builtin_amdgcn_readfirstlane(lds_address(lds)))
                : "memory");
 }
-// same with a wave-uniform base pointer and a 32-bit per-lane byte offset
+// 4 bytes per lane
+__device__ __forceinline__ void dma4(const void* gaddr, const void* lds) {
+  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" ::"v"(gaddr),
+               "s"(__builtin_amdgcn_readfirstlane(lds_address(lds)))
+               : "memory");
+}
+// same as dma16 with a wave-uniform base pointer and a 32-bit per-lane byte offset
 __device__ __forceinline__ void dma16_uniform(const void* gbase, unsigned voff, const void* lds) {
   // the base must sit in scalar registers whatever the compiler believes about its uniformity
   const unsigned long long b = (unsigned long long)gbase;

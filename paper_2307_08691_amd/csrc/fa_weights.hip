@@ -154,25 +154,52 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MANY ? 2 : 
   }
 }
 
-// More rows: a workgroup has 64 keys, which each of its four wavefronts holds in registers, and the rows stream past in tiles of 32
-// that the wavefronts take in turn, straight from L2, the next one requested before the current one is used. S^T = K Q^T here: a lane
-// has ONE row (and so one L), its accumulators the keys' sums over its rows; lanes and wavefronts are joined once, at the end.
-// Bound by the exponentials: 2 prompts of 2048, 16 heads of 64, 30 us for 67 million of them (three rounds of workgroups with their starts and
-// joins; deeper requests, eight wavefronts or fewer registers change nothing). No barrier in the loop; under the causal rule rows above the keys are not visited, and the blocks of keys
-// with the most rows are handed out first.
+// More rows: a workgroup has 64 keys, which each of its four wavefronts holds in registers, and the rows stream past, head by head, in
+// tiles of 32 queries that the wavefronts take in turn: whole rows into a private piece of LDS, the next tile requested before the
+// current one is used. (A lane that loads its own row straight into registers makes every request touch 64 places: 29.5 us where this
+// takes 26.3, 2 prompts of 2048, 16 heads of 64.) S^T = K Q^T here: a lane has ONE row (and so one L), its accumulators the keys'
+// sums over its rows; lanes and wavefronts are joined once, at the end. Bound by the exponentials. No barrier in the loop; under the causal
+// rule rows above the keys are not visited, and the blocks of keys with the most rows are handed out first.
 constexpr int kPromptKeys = 64;
 template <int D, bool F16>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void weights_prompt_kernel(WeightsArgs a) {
-  constexpr int KS = D / 16, NW = 4, PITCH = 33;
-  __shared__ float part[NW * kPromptKeys * PITCH];
+  constexpr int KS = D / 16, NW = 4, PITCH = 33, ROWB = 2 * D, CPR = ROWB / 16, RPI = 64 / CPR, COPIES = 32 / RPI;
+  constexpr int STAGEB = 32 * ROWB + 256;  // a tile of rows, and the logsumexps (as many twice, a lane each)
+  constexpr int PART = NW * kPromptKeys * PITCH * 4, RING = NW * 2 * STAGEB;
+  __shared__ __attribute__((aligned(1024))) char smem[PART > RING ? PART : RING];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane & 31, hh = lane >> 5;
   const int pair = blockIdx.x, s = pair / a.c.Hkv, g = pair - s * a.c.Hkv;
   const int n = held_keys(a.c, s), c0 = blockIdx.y * kPromptKeys;
   int nq = a.queries ? a.queries[s] : a.Nq;
   nq = nq < a.Nq ? nq : a.Nq;
   if (c0 >= n || nq <= 0) return;
-  const int rows = nq * a.G, off = n - a.Nq;
+  const int off = n - a.Nq;
   const float c2 = a.scale * kLog2e;
+  const int q_first = a.causal && c0 > off ? (c0 - off) & ~31 : 0;  // no query before it sees a key of the block
+  const int per_head = nq > q_first ? (nq - q_first + 31) / 32 : 0, tiles = per_head * a.G;
+  const __bf16* const Qb = a.Q + ((long)s * a.Nq * a.Hq + g * a.G) * D;
+  const float* const Lb = a.LSE + ((long)s * a.Hq + g * a.G) * a.Nq;
+  const long qstride = (long)a.Hq * D;
+  char* const ring = smem + w * 2 * STAGEB;
+  // This wavefront's next tile to be requested: its head and first query (scalars, which advance by NW tiles)
+  int next = w, next_h = 0, next_t = w;
+  auto settle = [&]() {
+    while (next_t >= per_head && next < tiles) next_t -= per_head, ++next_h;
+  };
+  auto request = [&](int stage) {
+    settle();
+    char* const to = ring + stage * STAGEB;
+    const int q0 = q_first + 32 * next_t, last = nq - 1 - q0;  // (queries past the last one repeat it)
+    const __bf16* const base = Qb + (long)next_h * D + (long)q0 * qstride;
+    dma4(Lb + (long)next_h * a.Nq + q0 + (lq < last ? lq : last), to + 32 * ROWB);
+#pragma unroll
+    for (int u = 0; u < COPIES; ++u) {
+      const int r = u * RPI + lane / CPR, ch = (lane % CPR) ^ swz<ROWB>(r);
+      dma16(base + (long)(r < last ? r : last) * qstride + 8 * ch, to + u * 1024);
+    }
+    next += NW;
+    next_t += NW;
+  };
   bf16x8 Kr[2][KS];
   {
     const __bf16* kb = a.K + (cache_row(a.c, s, c0) * a.c.Hkv + g) * D + 8 * hh;  // (a block lies in one page)
@@ -184,42 +211,22 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3
       for (int ks = 0; ks < KS; ++ks) Kr[u][ks] = *(const bf16x8*)(kp + 16 * ks);
     }
   }
-  const int q_first = a.causal && c0 > off ? c0 - off : 0;  // the first query that sees a key of the block
-  const int tiles = (rows + 31) / 32;
-  const __bf16* Qb = a.Q + ((long)s * a.Nq * a.Hq + g * a.G) * D + 8 * hh;
-  const float* Lb = a.LSE + ((long)s * a.Hq + g * a.G) * a.Nq;
-  struct Rows {
-    bf16x8 q[KS];
-    float l;
-    int last;  // the last key that the lane's row sees, from c0
-  };
-  // this lane's next row: query and head, which advance by 32 NW rows a tile
-  int t = (int)((long)q_first * a.G / 32) + w;
-  int next_r = 32 * t + lq, next_q = next_r / a.G, next_h = next_r - next_q * a.G;
-  const int step_q = 32 * NW / a.G, step_h = 32 * NW - step_q * a.G;
-  auto request = [&](Rows& x) {
-    const bool in = next_r < rows;
-    const int q = in ? next_q : nq - 1, h = in ? next_h : 0;
-    x.l = in ? Lb[(long)h * a.Nq + q] : -INFINITY;
-    x.last = a.causal ? q + off - c0 : kPromptKeys;
-    const __bf16* qp = Qb + ((long)q * a.Hq + h) * D;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) x.q[ks] = *(const bf16x8*)(qp + 16 * ks);
-    next_r += 32 * NW;
-    next_q += step_q;
-    next_h += step_h;
-    if (next_h >= a.G) next_h -= a.G, ++next_q;
-  };
   f32x16 sum[2] = {(f32x16){0}, (f32x16){0}};
-  auto compute = [&](int t, const Rows& x) {
-    const float nl = x.l != -INFINITY ? -x.l * kLog2e : -INFINITY;
-    const bool some = a.causal && 32 * t / a.G + off - c0 < kPromptKeys - 1;  // (not all rows see all keys)
-    const int last = nl != -INFINITY ? x.last - 4 * hh : -1;
+  const int zrow = lq * ROWB + 16 * (hh ^ swz<ROWB>(lq));
+  auto compute = [&](int stage, int q0) {
+    const char* const at = ring + stage * STAGEB;
+    const float l = ((const float*)(at + 32 * ROWB))[lane];
+    const float nl = q0 + lq < nq && l != -INFINITY ? -l * kLog2e : -INFINITY;
+    bf16x8 q[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) q[ks] = lds_b128(at, zrow ^ (32 * ks));
+    const bool some = a.causal && q0 + off - c0 < kPromptKeys - 1;  // (not all rows see all keys)
+    const int last = nl != -INFINITY ? q0 + lq + off - c0 - 4 * hh : -1;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       f32x16 S = (f32x16){0};
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) S = mfma32<F16>(Kr[u][ks], x.q[ks], S);
+      for (int ks = 0; ks < KS; ++ks) S = mfma32<F16>(Kr[u][ks], q[ks], S);
       if (some) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -232,18 +239,27 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3
       }
     }
   };
-  if (t < tiles) {
-    Rows x, y;
-    request(x);
-    while (true) {
-      if (t + NW < tiles) request(y);
-      compute(t, x);
-      if ((t += NW) >= tiles) break;
-      if (t + NW < tiles) request(x);
-      compute(t, y);
-      if ((t += NW) >= tiles) break;
+  if (w < tiles) {
+    int t = w, tq = w;
+    request(0);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) touch(Kr[u][ks]);
+    for (int stage = 0; t < tiles; t += NW, tq += NW, stage ^= 1) {
+      while (tq >= per_head) tq -= per_head;
+      if (next < tiles) {
+        request(stage ^ 1);
+        wait_vmem_upto<COPIES + 1>();
+      } else {
+        wait_vmem();
+      }
+      compute(stage, q_first + 32 * tq);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (read before its place is requested again)
     }
   }
+  __syncthreads();
+  float* const part = (float*)smem;
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
