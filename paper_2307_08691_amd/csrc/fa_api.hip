@@ -1069,7 +1069,7 @@ static int prefix_fwd_any(int f16, const void* Q, const void* Kprefix, const voi
   if (int e = check_common(Hq, Hkv, d, scale, false)) return e;
   fa::PrefixArgs a;
   if (int e = set_cache(a.own, seqlens_k, block_table, B, Hkv, Nk, d, page_size, pages_per_seq)) return e;
-  if ((double)B * Nq * Hq > (1 << 26)) return FA_ERR_SHAPE;
+  if ((double)B * Nq * Hq > (1 << 26) || Hkv > (1 << 16)) return FA_ERR_SHAPE;  // (a tile's rows lie within 32 bits of its first)
   if (prefix_table && Np > 0) {
     if (page_size < 64 || (page_size & (page_size - 1))) return FA_ERR_UNSUPPORTED;
     if (prefix_pages < 1 || (long)prefix_pages * page_size < Np) return FA_ERR_SHAPE;

@@ -38,7 +38,7 @@ def test_prefix_refusals(f16):
         assert p(**{name: 0}) == fa.FA_ERR_NULL
     for bad in (dict(B=0), dict(Nq=0), dict(Np=-1), dict(Nk=0), dict(Hq=7), dict(Hkv=0), dict(scale=0.0), dict(scale=NAN), dict(scale=INF),
                 dict(tab=P, page=64, pages=3), dict(tab=P, page=64, pages=0), dict(ptab=P, page=64, ppages=1), dict(ptab=P, page=64, ppages=0),
-                dict(B=1 << 20, Nq=64), dict(B=1 << 30)):
+                dict(B=1 << 20, Nq=64), dict(B=1 << 30), dict(Hq=1 << 17, Hkv=1 << 17)):
         assert p(**bad) == fa.FA_ERR_SHAPE, bad
     for bad in (dict(d=96), dict(d=256), dict(d=60), dict(tab=P, page=32, pages=100), dict(tab=P, page=96, pages=100),
                 dict(ptab=P, page=48, ppages=100)):

@@ -94,7 +94,7 @@ def check_prefix(dtype, d, B, nq, hq, hkv, n_p, slots, page, lens, causal=True, 
     none = eL == -np.inf
     assert (L[none] == -np.inf).all() and (O.transpose(0, 2, 1, 3)[none] == 0).all()
     score = np.where(none, 0, M * d / 2**24 + (M + np.abs(np.where(none, 0, eL)) + 8) / 2**21)
-    assert (np.abs(L - eL)[~none] <= score[~none]).all()
+    assert (np.abs(L[~none] - eL[~none]) <= score[~none]).all()
     small = (n_p + slots) * 4.0 / 2**25 if dtype == "f16" else 0.0  # (|v| below 4 where it counts)
     tol = e * (A + np.abs(eO)) * (1 + 2 * e) + A * 4 * score.transpose(0, 2, 1)[..., None] + small
     assert (np.abs(O - eO) <= tol).all(), np.max(np.abs(O - eO) / np.maximum(tol, 1e-30))
@@ -110,6 +110,7 @@ def check_prefix(dtype, d, B, nq, hq, hkv, n_p, slots, page, lens, causal=True, 
     (20, 2, 16, 2, 515, 130, 64, [(7 * i) % 129 + 2 for i in range(20)]),  # 320 rows: three blocks of rows
     (2, 9, 8, 2, 333, 200, 0, [200, 9]),                  # 36 own rows: two narrow items
     (2, 70, 4, 1, 129, 500, 128, [500, 70]),              # 280 own rows: wide items under the causal rule
+    (150, 1, 2, 1, 200, 70, 0, [(11 * i) % 71 for i in range(150)]),  # more sequences than are ranked by length
 ])
 def test_prefix(dtype, d, B, nq, hq, hkv, n_p, slots, page, lens):
     check_prefix(dtype, d, B, nq, hq, hkv, n_p, slots, page, lens)
@@ -263,14 +264,18 @@ def check_weights(dtype, d, B, nq, hq, hkv, slots, page, lens, causal=True, quer
     (3, 9, 8, 2, 200, 64, [200, 9, 33]),          # 36 rows: the prompt kernel
     (2, 300, 4, 2, 300, 0, [300, 300]),           # a prompt among its own keys
     (2, 67, 6, 2, 600, 128, [600, 67]),           # three heads a group: rows off the tiles' edges
+    (11, 1, 4, 2, 260, 64, [260, 1, 2, 33, 64, 65, 96, 97, 128, 129, 200]),  # eight sequences, and three
+    (9, 5, 12, 1, 150, 0, [150, 5, 6, 31, 32, 33, 64, 65, 149]),             # 60 rows
+    (2, 150, 6, 2, 200, 64, [200, 150]),          # 450 rows, three heads a group: the prompt kernel
+    (1, 33, 16, 1, 50, 0, [40]),                  # 528 rows, one query past a tile
 ])
 def test_weights(dtype, d, B, nq, hq, hkv, slots, page, lens):
     check_weights(dtype, d, B, nq, hq, hkv, slots, page, lens)
 
 
-@pytest.mark.parametrize("nq", [3, 50])
+@pytest.mark.parametrize("nq", [3, 50, 140])
 def test_weights_of_accepted_queries_without_causal_rule_and_of_rows_without_keys(nq):
-    lens = [120, nq, 1, 0]
+    lens = [120, min(nq, 120), 1, 0]
     check_weights("bf16", 64, 4, nq, 4, 2, 120, 0, lens)  # (sequence 2: queries before the first key, with L = -inf)
     check_weights("bf16", 64, 4, nq, 4, 2, 120, 0, lens, causal=False)
     check_weights("f16", 128, 4, nq, 4, 2, 120, 64, [120, 120, 60, 90], queries=[nq, 1, 0, 2])
