@@ -567,7 +567,8 @@ int fa_cache_append(const void* Knew, const void* Vnew, void* Kcache, void* Vcac
 /*
  * Attention weight that every cached key has drawn, added up over calls:
  *     weights[b, g, c] += sum over the query heads h of group g, the queries r that see key c:  exp(scale * q_r . k_c - LSE[b, h, r])
- * with the LSE that the attention over these keys left (fa_kvcache_fwd, fa_fwd; fa_prefix_fwd, whose LSE counts the prefix too).
+ * with the LSE that the attention over these keys left (fa_kvcache_fwd, fa_fwd; fa_prefix_fwd, whose LSE counts the prefix too):
+ * element (b, h, r) at LSE[b * lse_batch_stride + h * lse_head_stride + r * lse_query_stride] (Hq * Nq, Nq and 1 as they leave it).
  * weights: float32 [B, Hkv, Nk]; slots past seqlens_k[b] are not touched. queries (DEVICE int32 [B] or NULL): only the first queries[b]
  * (clamped into 0 .. Nq) of sequence b count, the others being drafts that were rejected; positions are those of all Nq. Rows with
  * LSE = -inf add nothing. Q [B, Nq, Hq, d]; Kcache, seqlens_k, block_table, causal rule and limits as fa_kvcache_fwd
@@ -575,7 +576,8 @@ int fa_cache_append(const void* Knew, const void* Vnew, void* Kcache, void* Vcac
  */
 int fa_cache_weights(const void* Q, const void* Kcache, const float* LSE, const int32_t* seqlens_k, const int32_t* block_table,
                      const int32_t* queries, float* weights, int B, int Hq, int Hkv, int Nq, int Nk, int d, int page_size,
-                     int pages_per_seq, float scale, int causal, void* stream);
+                     int pages_per_seq, long long lse_batch_stride, long long lse_head_stride, long long lse_query_stride,
+                     float scale, int causal, void* stream);
 
 /*
  * Caches cut to `budget` keys by accumulated attention weight. Every (sequence, key/value head) with n = seqlens_k[b] > budget keeps
@@ -678,7 +680,8 @@ int fa_prefix_fwd_f16(const void* Q, const void* Kprefix, const void* Vprefix, c
                       int pages_per_seq, float scale, int causal, void* stream);
 int fa_cache_weights_f16(const void* Q, const void* Kcache, const float* LSE, const int32_t* seqlens_k,
                          const int32_t* block_table, const int32_t* queries, float* weights, int B, int Hq, int Hkv, int Nq,
-                         int Nk, int d, int page_size, int pages_per_seq, float scale, int causal, void* stream);
+                         int Nk, int d, int page_size, int pages_per_seq, long long lse_batch_stride, long long lse_head_stride,
+                         long long lse_query_stride, float scale, int causal, void* stream);
 
 /*
  * Measurement aid, not part of either algorithm: a register-resident loop of the bf16 MFMA

@@ -107,8 +107,8 @@ SIGNATURES = {
     "fa_prefix_fwd": (_c_int, [_c_void_p] * 10 + [_c_void_p, _c_size_t] + [_c_int] * 10 + [_c_float, _c_int, _c_void_p]),
     "fa_prefix_fwd_f16": (_c_int, [_c_void_p] * 10 + [_c_void_p, _c_size_t] + [_c_int] * 10 + [_c_float, _c_int, _c_void_p]),
     "fa_cache_append": (_c_int, [_c_void_p] * 9 + [_c_int] * 7 + [_c_void_p]),
-    "fa_cache_weights": (_c_int, [_c_void_p] * 7 + [_c_int] * 8 + [_c_float, _c_int, _c_void_p]),
-    "fa_cache_weights_f16": (_c_int, [_c_void_p] * 7 + [_c_int] * 8 + [_c_float, _c_int, _c_void_p]),
+    "fa_cache_weights": (_c_int, [_c_void_p] * 7 + [_c_int] * 8 + [ctypes.c_longlong] * 3 + [_c_float, _c_int, _c_void_p]),
+    "fa_cache_weights_f16": (_c_int, [_c_void_p] * 7 + [_c_int] * 8 + [ctypes.c_longlong] * 3 + [_c_float, _c_int, _c_void_p]),
     "fa_cache_evict_workspace_bytes": (_c_size_t, [_c_int] * 4),
     "fa_cache_evict": (_c_int, [_c_void_p] * 9 + [_c_void_p, _c_size_t] + [_c_int] * 9 + [_c_void_p]),
     "fa_verify_drafts_workspace_bytes": (_c_size_t, [_c_int] * 3),
@@ -387,11 +387,11 @@ def fa_cache_append_raw(Knew, Vnew, Kc, Vc, seqlens_k, block_table, weights, pos
                                   page_size, pages_per_seq, stream)
 
 
-def fa_cache_weights_raw(Q, Kc, LSE, seqlens_k, block_table, queries, weights, B, Hq, Hkv, Nq, Nk, d, page_size, pages_per_seq, scale,
-                         causal, stream=0, f16=False) -> int:
+def fa_cache_weights_raw(Q, Kc, LSE, seqlens_k, block_table, queries, weights, B, Hq, Hkv, Nq, Nk, d, page_size, pages_per_seq,
+                         lse_bs, lse_hs, lse_qs, scale, causal, stream=0, f16=False) -> int:
     fn = load().fa_cache_weights_f16 if f16 else load().fa_cache_weights
-    return fn(Q, Kc, LSE, seqlens_k, block_table, queries, weights, B, Hq, Hkv, Nq, Nk, d, page_size, pages_per_seq, scale,
-              int(causal), stream)
+    return fn(Q, Kc, LSE, seqlens_k, block_table, queries, weights, B, Hq, Hkv, Nq, Nk, d, page_size, pages_per_seq, lse_bs, lse_hs,
+              lse_qs, scale, int(causal), stream)
 
 
 def fa_cache_evict_workspace_bytes(B, Hkv, Nk, budget) -> int:
@@ -1198,7 +1198,7 @@ def fa_cache_append(Knew, Vnew, Kcache, Vcache, seqlens_k=None, block_table=None
 
 def fa_cache_weights(Q, Kcache, LSE, weights, scale: float, causal: bool, seqlens_k=None, block_table=None, queries=None):
     """weights [B,Hkv,slots] fp32 += the attention weight that each cached key draws from the queries Q [B,Nq,Hq,d] (bf16 or fp16), summed
-    over the queries and the heads of its group: exp(scale q.k - LSE), LSE [B,Hq,Nq] fp32 from the attention over these keys.
+    over the queries and the heads of its group: exp(scale q.k - LSE), LSE [B,Hq,Nq] fp32 (any strides) from the attention over these keys.
     queries (int32 [B]): only the first of each sequence count (accepted drafts). Cache and lengths as fa_kvcache_fwd. Returns weights."""
     if _host and _host.cache_weights(Q, Kcache, LSE, weights, scale, causal, seqlens_k, block_table, queries):
         return weights
@@ -1210,13 +1210,14 @@ def fa_cache_weights(Q, Kcache, LSE, weights, scale: float, causal: bool, seqlen
     B, Nq, Hq, d = Q.shape
     dev, Hkv = Q.device, Kcache.shape[2]
     _need(Kcache, "Kcache", et, (*Kcache.shape[:3], d), dev)
-    _need(LSE, "LSE", torch.float32, (B, Hq, Nq), dev)
+    if LSE.dtype != torch.float32 or tuple(LSE.shape) != (B, Hq, Nq) or LSE.device != dev:
+        raise ValueError(f"LSE must be float32 of shape {(B, Hq, Nq)}, on the device of Q")
     Nk, page_size, pages = _cache_slots(Kcache, block_table, B, _beside_slots(weights, "weights", torch.float32, B, Hkv, dev), dev)
     for t, nm in ((seqlens_k, "seqlens_k"), (queries, "queries")):
         if t is not None:
             _need(t, nm, torch.int32, (B,), dev)
     _check(fa_cache_weights_raw(_ptr(Q), _ptr(Kcache), _ptr(LSE), _ptr(seqlens_k), _ptr(block_table), _ptr(queries), _ptr(weights), B, Hq,
-                                Hkv, Nq, Nk, d, page_size, pages, scale, causal, _stream(), et == torch.float16))
+                                Hkv, Nq, Nk, d, page_size, pages, *LSE.stride(), scale, causal, _stream(), et == torch.float16))
     return weights
 
 

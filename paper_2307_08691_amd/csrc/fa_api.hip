@@ -1145,7 +1145,8 @@ int fa_cache_append(const void* Knew, const void* Vnew, void* Kcache, void* Vcac
 
 static int cache_weights_any(int f16, const void* Q, const void* Kcache, const float* LSE, const int32_t* seqlens_k,
                              const int32_t* block_table, const int32_t* queries, float* weights, int B, int Hq, int Hkv, int Nq,
-                             int Nk, int d, int page_size, int pages_per_seq, float scale, int causal, void* stream) {
+                             int Nk, int d, int page_size, int pages_per_seq, long long lse_bs, long long lse_hs, long long lse_qs, float scale,
+                         int causal, void* stream) {
   if (!Q || !Kcache || !LSE || !weights) return FA_ERR_NULL;
   if (Nq <= 0) return FA_ERR_SHAPE;
   if (int e = check_common(Hq, Hkv, d, scale, false)) return e;
@@ -1164,22 +1165,27 @@ static int cache_weights_any(int f16, const void* Q, const void* Kcache, const f
   a.G = Hq / Hkv;
   a.f16 = f16;
   a.causal = causal != 0;
+  a.lse_bs = (long)lse_bs;
+  a.lse_hs = (long)lse_hs;
+  a.lse_qs = (long)lse_qs;
   a.scale = scale;
   return launched(fa::launch_weights(a, (hipStream_t)stream));
 }
 
 int fa_cache_weights(const void* Q, const void* Kcache, const float* LSE, const int32_t* seqlens_k, const int32_t* block_table,
                      const int32_t* queries, float* weights, int B, int Hq, int Hkv, int Nq, int Nk, int d, int page_size,
-                     int pages_per_seq, float scale, int causal, void* stream) {
+                     int pages_per_seq, long long lse_bs, long long lse_hs, long long lse_qs, float scale,
+                         int causal, void* stream) {
   return cache_weights_any(0, Q, Kcache, LSE, seqlens_k, block_table, queries, weights, B, Hq, Hkv, Nq, Nk, d, page_size, pages_per_seq,
-                           scale, causal, stream);
+                           lse_bs, lse_hs, lse_qs, scale, causal, stream);
 }
 
 int fa_cache_weights_f16(const void* Q, const void* Kcache, const float* LSE, const int32_t* seqlens_k, const int32_t* block_table,
                          const int32_t* queries, float* weights, int B, int Hq, int Hkv, int Nq, int Nk, int d, int page_size,
-                         int pages_per_seq, float scale, int causal, void* stream) {
+                         int pages_per_seq, long long lse_bs, long long lse_hs, long long lse_qs, float scale,
+                         int causal, void* stream) {
   return cache_weights_any(1, Q, Kcache, LSE, seqlens_k, block_table, queries, weights, B, Hq, Hkv, Nq, Nk, d, page_size, pages_per_seq,
-                           scale, causal, stream);
+                           lse_bs, lse_hs, lse_qs, scale, causal, stream);
 }
 
 static int evict_room(int Nk, int budget) { return Nk <= budget ? 0 : (Nk - budget < budget ? Nk - budget : budget); }

@@ -48,18 +48,23 @@ bool plain_context() {
   return ready && !c10::impl::TorchDispatchModeTLS::any_modes_set() && at::impl::PythonTorchFunctionTLS::stack_len() == 0 &&
          !c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::FuncTorchDynamicLayerFrontMode);
 }
-// A dense contiguous GPU tensor with memory of its own, or nullptr.
-const at::Tensor* plain(PyObject* o) {
+// A dense GPU tensor with memory of its own, of any strides, or nullptr.
+const at::Tensor* strided(PyObject* o) {
   if (!THPVariable_CheckExact(o) && (PyObject*)Py_TYPE(o) != parameter_type) return nullptr;
   const at::Tensor& t = THPVariable_Unpack(o);
   using K = c10::DispatchKey;
-  if (!t.defined() || t.layout() != at::kStrided || !t.is_cuda() || !t.has_storage() || t.numel() == 0 || !t.is_contiguous() ||
+  if (!t.defined() || t.layout() != at::kStrided || !t.is_cuda() || !t.has_storage() || t.numel() == 0 ||
       t.key_set().has_any(c10::DispatchKeySet({K::Python, K::Negative, K::Conjugate, K::ZeroTensor, K::Functionalize,
                                                K::FuncTorchBatched, K::FuncTorchGradWrapper})))
     return nullptr;
   for (int64_t n : t.sizes())
     if (n > INT_MAX) return nullptr;
   return &t;
+}
+// ... that is contiguous
+const at::Tensor* plain(PyObject* o) {
+  const at::Tensor* t = strided(o);
+  return t && t->is_contiguous() ? t : nullptr;
 }
 bool is(const at::Tensor* t, at::ScalarType st, c10::Device dev, at::IntArrayRef shape) {
   return t && t->scalar_type() == st && t->device() == dev && t->sizes() == shape;
@@ -483,7 +488,7 @@ PyObject* cache_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 PyObject* cache_weights(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
   if (nargs != 9 || !plain_context()) Py_RETURN_NONE;
-  const at::Tensor *Q = plain(args[0]), *K = plain(args[1]), *L = plain(args[2]), *W = plain(args[3]);
+  const at::Tensor *Q = plain(args[0]), *K = plain(args[1]), *L = strided(args[2]), *W = plain(args[3]);
   float scale;
   int causal;
   const int32_t *lens, *queries;
@@ -504,8 +509,8 @@ PyObject* cache_weights(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   float* w = (float*)W->mutable_data_ptr();
   const int32_t* tb = c.pages_of();
   const int e = without_gil([&] {
-    return (f16 ? lib.fa_cache_weights_f16 : lib.fa_cache_weights)(q, k, l, lens, tb, queries, w, B, Hq, Hkv, Nq, c.slots, d, c.page, c.pages, scale,
-                                                                   causal, st);
+    return (f16 ? lib.fa_cache_weights_f16 : lib.fa_cache_weights)(q, k, l, lens, tb, queries, w, B, Hq, Hkv, Nq, c.slots, d, c.page, c.pages,
+                                                                   L->stride(0), L->stride(1), L->stride(2), scale, causal, st);
   });
   if (e) Py_RETURN_NONE;
   Py_RETURN_TRUE;

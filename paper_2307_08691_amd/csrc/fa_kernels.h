@@ -196,6 +196,7 @@ struct WeightsArgs {
   float* weights;
   const int32_t* queries;  // of sequence s only the first queries[s] count (nullptr: all)
   int nseq, Nq, Hq, G, f16, causal;
+  long lse_bs, lse_hs, lse_qs;  // strides of LSE: sequence, head, query
   float scale;
 };
 hipError_t launch_weights(const WeightsArgs& a, hipStream_t st);

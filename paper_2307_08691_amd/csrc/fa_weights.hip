@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MANY ? 2 : 
   // -L of a row in the exponent's base; -inf where it adds nothing
   auto row_stat = [&](int row) {
     const int rc = row < rows ? row : rows - 1, q = rc / a.G;
-    const float l = a.LSE[((long)s * a.Hq + g * a.G + (rc - q * a.G)) * a.Nq + q];
+    const float l = a.LSE[s * a.lse_bs + (g * a.G + (rc - q * a.G)) * a.lse_hs + q * a.lse_qs];
     return row < rows && l != -INFINITY ? -l * kLog2e : -INFINITY;
   };
   auto row_at = [&](int row) {
@@ -178,7 +178,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3
   const int q_first = a.causal && c0 > off ? (c0 - off) & ~31 : 0;  // no query before it sees a key of the block
   const int per_head = nq > q_first ? (nq - q_first + 31) / 32 : 0, tiles = per_head * a.G;
   const __bf16* const Qb = a.Q + ((long)s * a.Nq * a.Hq + g * a.G) * D;
-  const float* const Lb = a.LSE + ((long)s * a.Hq + g * a.G) * a.Nq;
+  const float* const Lb = a.LSE + s * a.lse_bs + g * a.G * a.lse_hs;
   const long qstride = (long)a.Hq * D;
   char* const ring = smem + w * 2 * STAGEB;
   // This wavefront's next tile to be requested: its head and first query (scalars, which advance by NW tiles)
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3
     char* const to = ring + stage * STAGEB;
     const int q0 = q_first + 32 * next_t, last = nq - 1 - q0;  // (queries past the last one repeat it)
     const __bf16* const base = Qb + (long)next_h * D + (long)q0 * qstride;
-    dma4(Lb + (long)next_h * a.Nq + q0 + (lq < last ? lq : last), to + 32 * ROWB);
+    dma4(Lb + next_h * a.lse_hs + (q0 + (lq < last ? lq : last)) * a.lse_qs, to + 32 * ROWB);
 #pragma unroll
     for (int u = 0; u < COPIES; ++u) {
       const int r = u * RPI + lane / CPR, ch = (lane % CPR) ^ swz<ROWB>(r);

@@ -18,7 +18,7 @@ def append(Kn=P, Vn=P, K=P, V=P, lens=P, tab=0, W=P, pos=P, first=P, B=2, Hkv=2,
 
 
 def weights(Q=P, K=P, L=P, lens=P, tab=0, queries=0, W=P, B=2, Hq=8, Hkv=2, Nq=1, Nk=200, d=64, page=0, pages=0, scale=0.1, f16=False):
-    return fa.fa_cache_weights_raw(Q, K, L, lens, tab, queries, W, B, Hq, Hkv, Nq, Nk, d, page, pages, scale, True, 0, f16)
+    return fa.fa_cache_weights_raw(Q, K, L, lens, tab, queries, W, B, Hq, Hkv, Nq, Nk, d, page, pages, Hq * Nq, Nq, 1, scale, True, 0, f16)
 
 
 def evict(K=P, V=P, W=P, pos=P, lens=P, tab=0, Wo=P, po=P, no=P, ws=P, nb=BIG, B=2, Hkv=2, Nk=200, d=64, budget=100, sinks=4, recent=20,
@@ -180,6 +180,7 @@ def test_cache_tensors():
     refused(ap, new, new, K, K, n)  # on the host
     Q, L = bf(2, 1, 8, 64), f32(2, 8, 1)
     refused(we, Q, K, f32(2, 1, 8), W, 0.1, True, n)
+    refused(we, Q, K, L.double(), W, 0.1, True, n)
     refused(we, Q, K, L, f32(2, 2, 21), 0.1, True, n)
     refused(we, Q, K, L, W.double(), 0.1, True, n)
     refused(we, Q, K, L, W, 0.1, True, n, queries=i32(1))

@@ -282,6 +282,19 @@ def test_weights_of_accepted_queries_without_causal_rule_and_of_rows_without_key
     check_weights("bf16", 64, 4, nq, 4, 2, 120, 0, [120, 120, 60, 90], queries=[nq - 1, 1, nq, 2], causal=False)
 
 
+@pytest.mark.parametrize("nq", [1, 12, 300])
+def test_weights_take_a_logsumexp_of_any_strides(nq):
+    r = rng(nq)
+    Q, K = gpu(r.normal(size=(2, nq, 4, 64)), torch.bfloat16), gpu(r.normal(size=(2, 320, 2, 64)), torch.bfloat16)
+    _, L = binding.fa_kvcache_fwd(Q, K, K, 0.125, True)
+    got = []
+    for x in (L, L.transpose(1, 2).contiguous().transpose(1, 2), L.permute(2, 1, 0).contiguous().permute(2, 1, 0), L.repeat(1, 1, 2)[..., :nq]):
+        W = torch.zeros((2, 2, 320), device="cuda")
+        binding.fa_cache_weights(Q, K, x, W, 0.125, True)
+        got.append(W)
+    assert all(torch.equal(got[0], x) for x in got[1:]) and (got[0] > 0).all()
+
+
 def test_weights_do_not_see_what_is_masked():
     """Infinities and NaN in keys that no counted query sees stay out of every sum."""
     for nq in (3, 40):
