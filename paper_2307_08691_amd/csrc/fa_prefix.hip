@@ -61,14 +61,13 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
     for (int ks = 0; ks < KS; ++ks) Qf[ks] = *(const bf16x8*)(qp + 16 * ks);
   }
   const int lim_row = it.causal && q + it.off < it.nk - 1 ? q + it.off : it.nk - 1;  // the last key of this lane's row
-  u32x4 Kr[2][KS];
+  u32x4 Kn[KS], Kc[KS];  // K of the tile on its way, of the one in use
   char* const vbuf = smem + w * WAVEB;
   // Pages of this wavefront's tiles: lane i has the one of tile i of the next 64 (looked up one by one each would be a memory latency
   // in front of its tile's requests).
   const int mask = (1 << a.own.page_log2) - 1;
   int pages = 0;
-  auto issue = [&](int key0, auto BUF) {
-    constexpr int buf = decltype(BUF)::value;
+  auto issue = [&](int key0, int buf) {
     const int last = it.end - 1 - key0;  // (rows past the end repeat the last one)
     long row = key0;
     if (it.table) {
@@ -81,7 +80,7 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
     }
     const __bf16* kp = it.K + (row + (lq < last ? lq : last)) * kstride + 8 * hh;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) Kr[buf][ks] = *(const u32x4*)(kp + 16 * ks);
+    for (int ks = 0; ks < KS; ++ks) Kn[ks] = *(const u32x4*)(kp + 16 * ks);
     tile_load_async<D, KT, 1>(vbuf + buf * TILEB, it.V + row * kstride, kstride, 0, last, 0, lane);
   };
   f32x16 O[DT];
@@ -93,11 +92,10 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
   int zcol[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) zcol[u] = swz_off<ROWB>(4 * hh + (p16 >> 2) + 8 * u, 2 * g16 + ((p16 & 3) >> 1)) + 8 * (p16 & 1);
-  auto compute = [&](int key0, auto BUF) {
-    constexpr int buf = decltype(BUF)::value;
+  auto compute = [&](int key0, int buf) {
     f32x16 S = (f32x16){0};
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) S = mfma32<F16>(__builtin_bit_cast(bf16x8, Kr[buf][ks]), Qf[ks], S);
+    for (int ks = 0; ks < KS; ++ks) S = mfma32<F16>(__builtin_bit_cast(bf16x8, Kc[ks]), Qf[ks], S);
     if ((it.causal && key0 + KT - 1 > it.row0 / a.G + it.off) || key0 + KT > it.end) {
       const int lim = (lim_row < it.end - 1 ? lim_row : it.end - 1) - key0 - 4 * hh;
 #pragma unroll
@@ -134,41 +132,36 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
       O[dt] = mfma32<F16>(lds_tr_pair(smem, ((zcol[0] + vb) ^ (64 * dt)) + ro, ((zcol[1] + vb) ^ (64 * dt)) + ro), Pf[i & 1], O[dt]);
     }
   };
-  using B0 = std::integral_constant<int, 0>;
-  using B1 = std::integral_constant<int, 1>;
+  // One copy of the code of a tile: short shares run it twice, and wait for its instructions (2 KB) the first time.
   int t = it.begin + KT * w;
   if (t < it.end) {
-    issue(t, B0{});
-    if (t + NW * KT < it.end) issue(t + NW * KT, B1{});  // (short shares hold no more, and wait once)
+    issue(t, 0);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) touch(Qf[ks]);
-    wait_vmem();
-    bool here = true;
-    while (true) {
-      if (!here && t + NW * KT < it.end) issue(t + NW * KT, B1{});
-      here = false;
-      compute(t, B0{});
+    for (int buf = 0;; buf ^= 1) {
+      wait_vmem();
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) Kc[ks] = Kn[ks];
+      if (t + NW * KT < it.end) issue(t + NW * KT, buf ^ 1);
+      compute(t, buf);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (this tile has been read before its buffer is requested again)
-      wait_vmem();
-      if ((t += NW * KT) >= it.end) break;
-      if (t + NW * KT < it.end) issue(t + NW * KT, B0{});
-      compute(t, B1{});
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      wait_vmem();
       if ((t += NW * KT) >= it.end) break;
     }
   }
   // ---- the wavefronts' partial results become the item's
   const float lsum = sum_with_partner32(l);
   __syncthreads();
-  // [d][row], the rows turned by d / 4 places: rows are written, and pieces of four columns read, without bank conflicts
-  float* part = (float*)(smem + w * WAVEB);
+  // rows of pieces of four columns, their places XOR-ed with the row
+  constexpr int CPR = D / 4;
+  char* const mine = smem + w * WAVEB + lq * (4 * D);
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int c = 32 * dt + acc_row(r, hh);
-      part[c * 32 + ((lq + c / 4) & 31)] = O[dt][r];
+    for (int r4 = 0; r4 < 4; ++r4) {
+      f32x4 o;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) o[v] = O[dt][4 * r4 + v];
+      *(f32x4*)(mine + 16 * ((8 * dt + 2 * r4 + hh) ^ (lq & (CPR - 1)))) = o;
     }
   float* stat = (float*)(smem + STAT_OFF);
   if (hh == 0) {
@@ -176,7 +169,6 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
     stat[32 * NW + w * 32 + lq] = lsum;
   }
   __syncthreads();
-  constexpr int CPR = D / 4;  // pieces of a row
   for (int i = tid; i < it.rows * CPR; i += 64 * NW) {
     const int r = i / CPR, c = i % CPR;
     float mm = -INFINITY;
@@ -188,9 +180,7 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
     for (int u = 0; u < NW; ++u) {
       const float mw = stat[u * 32 + r], wgt = mw == -INFINITY ? 0.f : fast_exp2((mw - mm) * c2);
       den += wgt * stat[32 * NW + u * 32 + r];
-      const float* x = (const float*)(smem + u * WAVEB) + 4 * c * 32 + ((r + c) & 31);
-#pragma unroll
-      for (int v = 0; v < 4; ++v) o[v] += wgt * x[32 * v];
+      o += *(const f32x4*)(smem + u * WAVEB + r * (4 * D) + 16 * (c ^ (r & (CPR - 1)))) * wgt;
     }
     const float inv = den > 0.f ? 1.f / den : 0.f;  // (no visible key: L = -inf, and the merge does not look at O)
     const long at = item_row(a, it, r);
