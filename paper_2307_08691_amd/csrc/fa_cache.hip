@@ -151,7 +151,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
   if constexpr (KEPT) {
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i)
-      if (first + 64 * i < n) top = max(top, pos[i]);
+      if (i < steps && first + 64 * i < n) top = max(top, pos[i]);
   } else {
 #pragma unroll 8
     for (int i = 0; i < steps; ++i) top = max(top, P[first + 64 * i < n ? first + 64 * i : n - 1]);

@@ -378,6 +378,22 @@ def test_evict_of_protected_positions_beyond_the_budget():
     check_evict("bf16", 1, 1, 8, 300, 0, [300], 50, 0, 5, positions=-pos - 1)
 
 
+@pytest.mark.parametrize("slots,page,lens,budget", [(362, 0, [300, 361, 362, 1], 298), (2112, 64, [2049, 2056, 2111, 100], 2048), (5000, 0, [4500, 4999], 3000),
+                                                    (9000, 0, [8200, 8999], 500), (33000, 0, [32768, 32900], 500)])
+def test_evict_does_not_look_past_a_length(slots, page, lens, budget):
+    """Slots past a length hold whatever an earlier use left there, newer positions than any key's and the largest weights among it."""
+    r = rng(slots)
+    B, hkv = len(lens), 2
+    pos = np.argsort(r.random((B, hkv, slots)), -1)
+    w = r.exponential(size=(B, hkv, slots))
+    for b, n in enumerate(lens):
+        pos[b, :, :n] = np.argsort(r.random((hkv, n)), -1)
+        pos[b, :, n:] = 10**6 + np.arange(slots - n)
+        w[b, :, n:] = 1e30
+    for in_place in (False, True):
+        check_evict("bf16", B, hkv, 64, slots, page, lens, budget, 4, budget // 4, weights=lambda r, s: w, in_place=in_place, positions=pos)
+
+
 # ---------------------------------------------------------------------------------------------
 
 def distributions(r, B, k, V, spread=3.0):
