@@ -528,6 +528,9 @@ int fa_kvcache_fwd(const void* Q, const void* Kcache, const void* Vcache, const 
                    int B, int Hq, int Hkv, int Nq, int Nk, int d, int page_size, int pages_per_seq,
                    float scale, int causal, int num_splits, void* stream);
 
+/* Slots of a sequence (Nk) and keys of a prefix that the five operators below take at most (FA_ERR_SHAPE beyond). */
+#define FA_CACHE_MAX_SLOTS (1 << 30)
+
 /*
  * Decoding a batch whose sequences share a long prefix (a system prompt, several answers to one question): the queries of all
  * sequences attend to the prefix, which is read once for the batch instead of once per sequence, and each to the keys its own

@@ -1039,6 +1039,7 @@ static int launched(hipError_t e) {
 static int set_cache(fa::CacheView& c, const int32_t* lens, const int32_t* table, int B, int Hkv, int Nk, int d, int page_size, int pages_per_seq) {
   if (B <= 0 || Hkv <= 0 || Nk <= 0) return FA_ERR_SHAPE;
   if (B > (1 << 20) || Hkv > (1 << 20) || (long)B * Hkv > (1 << 20)) return FA_ERR_SHAPE;  // (a grid has room for them)
+  if (Nk > FA_CACHE_MAX_SLOTS) return FA_ERR_SHAPE;  // (a slot and the next tile's stay within 32 bits)
   c = {lens, table, 0, pages_per_seq, Nk, Hkv, d};
   if (table) {
     if (page_size < 64 || (page_size & (page_size - 1))) return FA_ERR_UNSUPPORTED;
@@ -1069,7 +1070,7 @@ static int prefix_fwd_any(int f16, const void* Q, const void* Kprefix, const voi
   if (int e = check_common(Hq, Hkv, d, scale, false)) return e;
   fa::PrefixArgs a;
   if (int e = set_cache(a.own, seqlens_k, block_table, B, Hkv, Nk, d, page_size, pages_per_seq)) return e;
-  if ((double)B * Nq * Hq > (1 << 26) || Hkv > (1 << 16)) return FA_ERR_SHAPE;  // (a tile's rows lie within 32 bits of its first)
+  if (Np > FA_CACHE_MAX_SLOTS || (double)B * Nq * Hq > (1 << 26) || Hkv > (1 << 16)) return FA_ERR_SHAPE;  // (a tile's rows lie within 32 bits of its first)
   if (prefix_table && Np > 0) {
     if (page_size < 64 || (page_size & (page_size - 1))) return FA_ERR_UNSUPPORTED;
     if (prefix_pages < 1 || (long)prefix_pages * page_size < Np) return FA_ERR_SHAPE;

@@ -28,6 +28,13 @@ __device__ __forceinline__ void pair_of(int i, int nseq, int heads, int& s, int&
   }
 }
 
+// A workgroup's block of keys: grids hold 65535 of them along one axis, long caches have more.
+constexpr long kBlocksY = 32768;
+__device__ __forceinline__ int block_of_keys() { return (int)(blockIdx.z * gridDim.y + blockIdx.y); }
+static dim3 grid_of(unsigned pairs, long blocks) {
+  return dim3(pairs, (unsigned)(blocks < kBlocksY ? blocks : kBlocksY), (unsigned)((blocks + kBlocksY - 1) / kBlocksY));
+}
+
 // Few rows (decoding): the rows stay and the keys stream past, in tiles of 32 that each of a workgroup's four wavefronts takes in
 // turn, the next one requested before the current one is used. S = Q K^T is formed with the KEYS as columns of the MFMA tile: a lane
 // then holds 16 rows of ONE key, and the sum over rows is additions inside the lane and one exchange with the partner lane. Bound
@@ -42,7 +49,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MANY ? 2 : 
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lq = lane & 31, hh = lane >> 5;
   int s, g;
   pair_of(blockIdx.x, a.nseq, a.c.Hkv, s, g);
-  const int n = held_keys(a.c, s), c0 = blockIdx.y * keys;
+  const int n = held_keys(a.c, s), c0 = block_of_keys() * keys;
   int nq = a.queries ? a.queries[s] : a.Nq;
   nq = nq < a.Nq ? nq : a.Nq;
   if (c0 >= n || nq <= 0) return;
@@ -169,7 +176,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3
   __shared__ __attribute__((aligned(1024))) char smem[PART > RING ? PART : RING];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane & 31, hh = lane >> 5;
   const int pair = blockIdx.x, s = pair / a.c.Hkv, g = pair - s * a.c.Hkv;
-  const int n = held_keys(a.c, s), c0 = blockIdx.y * kPromptKeys;
+  const int n = held_keys(a.c, s), c0 = block_of_keys() * kPromptKeys;
   int nq = a.queries ? a.queries[s] : a.Nq;
   nq = nq < a.Nq ? nq : a.Nq;
   if (c0 >= n || nq <= 0) return;
@@ -289,11 +296,11 @@ static hipError_t launch_weights_d(const WeightsArgs& a, hipStream_t st) {
     // of 64: - / 25.8 / 24.8 / 28.4 / 30.6)
     long keys = ((long)pairs * a.c.Nk / 512 + 127) / 128 * 128;
     keys = keys < 128 ? 128 : (keys > 512 ? 512 : keys);
-    const dim3 grid(pairs, (unsigned)((a.c.Nk + keys - 1) / keys));
+    const dim3 grid = grid_of(pairs, (a.c.Nk + keys - 1) / keys);
     if (a.Nq * a.G <= 32) hipLaunchKernelGGL((weights_step_kernel<D, F16, false>), grid, dim3(256), 0, st, a, (int)keys);
     else hipLaunchKernelGGL((weights_step_kernel<D, F16, true>), grid, dim3(256), 0, st, a, (int)keys);
   } else {
-    hipLaunchKernelGGL((weights_prompt_kernel<D, F16>), dim3(pairs, (unsigned)((a.c.Nk + kPromptKeys - 1) / kPromptKeys)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((weights_prompt_kernel<D, F16>), grid_of(pairs, ((long)a.c.Nk + kPromptKeys - 1) / kPromptKeys), dim3(256), 0, st, a);
   }
   return hipGetLastError();
 }

@@ -206,3 +206,16 @@ def test_verify_tensors():
     refused(ve, x, q, f32(4, 2, 50).transpose(0, 1), u)
     refused(ve, x, q, t, u, tokens=i32(2, 3))
     refused(ve, x, q, t, u)  # on the host
+
+
+def test_slots_beyond_the_limit():
+    """A slot and the one a tile further have to fit 32 bits: 2^30 is the most, also of slots in pages that repeat."""
+    most = 1 << 30
+    paged = dict(tab=P, page=1 << 20, pages=1 << 11)
+    for call in (prefix, append, weights, evict):
+        assert call(Nk=most + 1, **paged) == fa.FA_ERR_SHAPE
+        assert call(Nk=2**31 - 1, **paged) == fa.FA_ERR_SHAPE
+    assert prefix(Np=most + 1, ptab=P, page=1 << 20, ppages=1 << 11) == fa.FA_ERR_SHAPE
+    # (accepted up to there: what is refused next is the workspace)
+    assert prefix(Nk=most, Np=most, ptab=P, ppages=1 << 11, nb=0, **paged) == fa.FA_ERR_WORKSPACE
+    assert evict(Nk=most, nb=0, **paged) == fa.FA_ERR_WORKSPACE
