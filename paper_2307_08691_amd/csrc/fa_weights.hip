@@ -35,17 +35,117 @@ static dim3 grid_of(unsigned pairs, long blocks) {
   return dim3(pairs, (unsigned)(blocks < kBlocksY ? blocks : kBlocksY), (unsigned)((blocks + kBlocksY - 1) / kBlocksY));
 }
 
-// Few rows (decoding): the rows stay and the keys stream past, in tiles of 32 that each of a workgroup's four wavefronts takes in
-// turn, the next one requested before the current one is used. S = Q K^T is formed with the KEYS as columns of the MFMA tile: a lane
-// then holds 16 rows of ONE key, and the sum over rows is additions inside the lane and one exchange with the partner lane. Bound
-// by reading K once: 64 sequences of up to 8192 keys, 32 heads on 8 of 128: 107 us, 4.5 TB/s (a large read: 6.1). Up to 32 rows are held
-// in registers; MANY: up to kStepRows in LDS.
+// Few rows (decoding): the rows stay in registers and the keys stream past, in tiles of 32 that each of a workgroup's four wavefronts
+// takes in turn: whole rows into a private piece of LDS, two tiles on their way. (A lane that loads its own key's row straight into
+// registers makes every request touch 64 places: 107 us, 4.5 TB/s, for 64 sequences of up to 8192 keys, 32 heads on 8 of 128, where
+// this takes 96, 5.0 TB/s; a kernel that only reads 4 GiB: 6.25.) S = Q K^T is formed with the KEYS as columns of the MFMA tile: a lane then holds 16
+// rows of ONE key, and the sum over rows is additions inside the lane and one exchange with the partner lane. Bound by reading K once.
+// What the rows and the slots have is requested beside the pages, before the first tile: memory answers in order, and what is
+// requested behind a tile waits for it. For the same reason the sums are written when all tiles have come.
+constexpr int kStepKeys = 512;  // of a workgroup at most
+template <int D, bool F16>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void weights_step_kernel(WeightsArgs a, int keys) {  // keys: of a workgroup, a multiple of 128
+  constexpr int KS = D / 16, NW = 4, ROWB = 2 * D, TILEB = 32 * ROWB, COPIES = TILEB / 1024, TILES = kStepKeys / (32 * NW);
+  __shared__ __attribute__((aligned(1024))) char smem[NW * 2 * TILEB];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lq = lane & 31, hh = lane >> 5;
+  int s, g;
+  pair_of(blockIdx.x, a.nseq, a.c.Hkv, s, g);
+  const int n = held_keys(a.c, s), c0 = block_of_keys() * keys;
+  int nq = a.queries ? a.queries[s] : a.Nq;
+  nq = nq < a.Nq ? nq : a.Nq;
+  const int end = n - c0 < keys ? n : c0 + keys, t0 = c0 + 32 * w;
+  if (t0 >= end || nq <= 0) return;
+  const int rows = nq * a.G, off = n - a.Nq;
+  const float c2 = a.scale * kLog2e;
+  const long kstride = (long)a.c.Hkv * D;
+  float* const W = a.weights + ((long)s * a.c.Hkv + g) * a.c.Nk;
+  const int tiles = (end - t0 + 32 * NW - 1) / (32 * NW);  // this wavefront's: from t0, t0 + 128, ...
+  int pages = 0;  // lane i: the page of tile i
+  if (a.c.table) {
+    const int x = t0 + lane * (32 * NW);
+    pages = a.c.table[(long)s * a.c.table_stride + ((x < end ? x : t0) >> a.c.page_log2)];
+  }
+  // This lane's row
+  const int rc = lq < rows ? lq : rows - 1, q = rc / a.G, h = g * a.G + (rc - q * a.G);
+  const float l = a.LSE[s * a.lse_bs + h * a.lse_hs + q * a.lse_qs];
+  bf16x8 Qf[KS];
+  {
+    const __bf16* qp = a.Q + (((long)s * a.Nq + q) * a.Hq + h) * D + 8 * hh;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) Qf[ks] = *(const bf16x8*)(qp + 16 * ks);
+  }
+  float sums[TILES];  // of the lane's key in every tile: what was there, and what is added
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) sums[i] = W[t0 + 128 * i + lq < end ? t0 + 128 * i + lq : end - 1];
+  touch(pages);
+  touch(l);
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) touch(Qf[ks]);
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) touch(sums[i]);
+  char* const mine = smem + w * 2 * TILEB;
+  auto request = [&](int i) {  // (keys past the end repeat the last one)
+    const int t = t0 + 32 * NW * i;
+    long row = (long)s * a.c.Nk + t;
+    if (a.c.table) row = ((long)__builtin_amdgcn_readlane(pages, i) << a.c.page_log2) + (t & ((1 << a.c.page_log2) - 1));
+    tile_load_async<D, 32, 1>(mine + (i & 1) * TILEB, a.K + row * kstride + (long)g * D, kstride, 0, n - 1 - t, 0, lane);
+  };
+  request(0);
+  if (tiles > 1) request(1);
+  f32x4 nl[4];  // of the rows of this lane's registers: -L in the exponent's base; -inf where the row adds nothing
+  {
+    const float x = lq < rows && l != -INFINITY ? -l * kLog2e : -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) nl[r / 4][r % 4] = __shfl(x, acc_row(r, hh));
+  }
+  const int zrow = lq * ROWB + 16 * (hh ^ swz<ROWB>(lq));
+  static_for<TILES>([&](auto I) {
+    constexpr int i = decltype(I)::value;
+    if (i >= tiles) return;
+    const int t = t0 + 32 * NW * i;
+    if (i + 1 < tiles) wait_vmem_upto<COPIES>();
+    else wait_vmem();
+    bf16x8 Kf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) Kf[ks] = lds_b128(mine + (i & 1) * TILEB, zrow ^ (32 * ks));
+    if (i + 2 < tiles) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (read before its place is requested again)
+      request(i + 2);
+    }
+    f32x16 S = (f32x16){0};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) S = mfma32<F16>(Qf[ks], Kf[ks], S);
+    float sum[2] = {0.f, 0.f};
+    if (a.causal && t + 31 > off) {
+      const int first = (t + lq - off) * a.G - 4 * hh;  // the first row that sees the lane's key, from the half's first
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float x = nl[r / 4][r % 4], e = fast_exp2(__builtin_fmaf(S[r], c2, x));
+        sum[r & 1] += (x != -INFINITY) & (acc_row(r, 0) >= first) ? e : 0.f;
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float x = nl[r / 4][r % 4], e = fast_exp2(__builtin_fmaf(S[r], c2, x));
+        sum[r & 1] += x != -INFINITY ? e : 0.f;
+      }
+    }
+    sums[i] += sum_with_partner32(sum[0] + sum[1]);
+  });
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) {
+    const int key = t0 + 32 * NW * i + lq;
+    if (hh == 0 && key < end) W[key] = sums[i];
+  }
+}
+
+// More rows, up to kStepRows, which lie in LDS: as above, the keys of a tile straight into registers.
 constexpr int kStepRows = 256;
-template <int D, bool F16, bool MANY>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MANY ? 2 : D == 64 ? 4 : 3))) void weights_step_kernel(WeightsArgs a, int keys) {  // keys: of a workgroup, a multiple of 128
+template <int D, bool F16>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void weights_rows_kernel(WeightsArgs a, int keys) {  // keys: of a workgroup, a multiple of 128
   constexpr int KS = D / 16, NW = 4, ROWB = 2 * D;
-  __shared__ __attribute__((aligned(1024))) char smem[MANY ? kStepRows * (ROWB + 4) : 16];
-  float* const stat = (float*)(smem + kStepRows * ROWB);  // (MANY) nl of every row
+  __shared__ __attribute__((aligned(1024))) char smem[kStepRows * (ROWB + 4)];
+  float* const stat = (float*)(smem + kStepRows * ROWB);  // nl of every row: -L in the exponent's base; -inf where the row adds nothing
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lq = lane & 31, hh = lane >> 5;
   int s, g;
   pair_of(blockIdx.x, a.nseq, a.c.Hkv, s, g);
@@ -82,11 +182,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MANY ? 2 : 
   using B0 = std::integral_constant<int, 0>;
   using B1 = std::integral_constant<int, 1>;
   int t = c0 + 32 * w;
-  if (!MANY && t >= end) return;
   if (t < end) request(t, B0{});
   if (t + 32 * NW < end) request(t + 32 * NW, B1{});
 
-  // -L of a row in the exponent's base; -inf where it adds nothing
   auto row_stat = [&](int row) {
     const int rc = row < rows ? row : rows - 1, q = rc / a.G;
     const float l = a.LSE[s * a.lse_bs + (g * a.G + (rc - q * a.G)) * a.lse_hs + q * a.lse_qs];
@@ -96,9 +194,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MANY ? 2 : 
     const int rc = row < rows ? row : rows - 1, q = rc / a.G;
     return a.Q + (((long)s * a.Nq + q) * a.Hq + g * a.G + (rc - q * a.G)) * D;
   };
-  bf16x8 Qf[KS];
-  f32x4 nl[4];  // of the rows of this lane's registers
-  if constexpr (MANY) {
+  {
     constexpr int CPR = ROWB / 16;
     for (int i = threadIdx.x; i < (rows + 31) / 32 * 32 * CPR; i += 64 * NW) {
       const int r = i / CPR, ch = i % CPR;
@@ -107,31 +203,23 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MANY ? 2 : 
     if (threadIdx.x < (rows + 31) / 32 * 32) stat[threadIdx.x] = row_stat(threadIdx.x);
     __syncthreads();
     if (t >= end) return;
-  } else {
-    const __bf16* qp = row_at(lq) + 8 * hh;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) Qf[ks] = *(const bf16x8*)(qp + 16 * ks);
-    const float mine = row_stat(lq);  // (a lane has one row's, and the registers' rows are handed round)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) nl[r / 4][r % 4] = __shfl(mine, acc_row(r, hh));
   }
 
   const int zrow = lq * ROWB + 16 * (hh ^ swz<ROWB>(lq));
   auto compute = [&](int t, auto BUF) {
     const int key = t + lq;
     float sum[2] = {0.f, 0.f};
-    for (int rt = 0; rt < (MANY ? rows : 1); rt += 32) {
+    for (int rt = 0; rt < rows; rt += 32) {
       const long sees = a.causal ? (long)(t - off) * a.G : 0;  // the first row that sees the tile's first key
-      if (MANY && sees > rt + 31) continue;
-      if constexpr (MANY) {
+      if (sees > rt + 31) continue;
+      f32x4 nl[4];  // of the rows of this lane's registers
 #pragma unroll
-        for (int i = 0; i < 4; ++i) nl[i] = *(const f32x4*)(stat + rt + 8 * i + 4 * hh);
-      }
+      for (int i = 0; i < 4; ++i) nl[i] = *(const f32x4*)(stat + rt + 8 * i + 4 * hh);
       f32x16 S = (f32x16){0};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
-        S = mfma32<F16>(MANY ? lds_b128(smem, (zrow ^ (32 * ks)) + rt * ROWB) : Qf[ks], Kr[decltype(BUF)::value][ks], S);
-      if (a.causal && (MANY ? sees + 31l * a.G > rt : t + 31 > off)) {
+        S = mfma32<F16>(lds_b128(smem, (zrow ^ (32 * ks)) + rt * ROWB), Kr[decltype(BUF)::value][ks], S);
+      if (a.causal && sees + 31l * a.G > rt) {
         const int first = (key - off) * a.G - 4 * hh - rt;  // the first row that sees the lane's key, from the half's first
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -163,17 +251,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MANY ? 2 : 
 
 // More rows: a workgroup has 64 keys, which each of its four wavefronts holds in registers, and the rows stream past, head by head, in
 // tiles of 32 queries that the wavefronts take in turn: whole rows into a private piece of LDS, the next tile requested before the
-// current one is used. (A lane that loads its own row straight into registers makes every request touch 64 places: 29.5 us where this
-// takes 26.3, 2 prompts of 2048, 16 heads of 64.) S^T = K Q^T here: a lane has ONE row (and so one L), its accumulators the keys'
-// sums over its rows; lanes and wavefronts are joined once, at the end. Bound by the exponentials. No barrier in the loop; under the causal
-// rule rows above the keys are not visited, and the blocks of keys with the most rows are handed out first.
+// current one is used. The keys are the columns here too: a lane's sums are two keys' (with the keys as rows, 32 sums a lane and a
+// transpose through LDS at the end, 2 prompts of 2048, 16 heads of 64, take 27.5 us instead of 23.7). Bound by the exponentials: 16
+// of the 24 cycles that a wavefront's 64 scores take. No barrier in the loop; under the causal rule rows above the keys are not
+// visited, and the blocks of keys with the most rows are handed out first.
 constexpr int kPromptKeys = 64;
 template <int D, bool F16>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void weights_prompt_kernel(WeightsArgs a) {
-  constexpr int KS = D / 16, NW = 4, PITCH = 33, ROWB = 2 * D, CPR = ROWB / 16, RPI = 64 / CPR, COPIES = 32 / RPI;
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void weights_prompt_kernel(WeightsArgs a) {
+  constexpr int KS = D / 16, NW = 4, ROWB = 2 * D, CPR = ROWB / 16, RPI = 64 / CPR, COPIES = 32 / RPI;
   constexpr int STAGEB = 32 * ROWB + 256;  // a tile of rows, and the logsumexps (as many twice, a lane each)
-  constexpr int PART = NW * kPromptKeys * PITCH * 4, RING = NW * 2 * STAGEB;
-  __shared__ __attribute__((aligned(1024))) char smem[PART > RING ? PART : RING];
+  __shared__ __attribute__((aligned(1024))) char smem[NW * 2 * STAGEB];
+  __shared__ float part[NW * kPromptKeys];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane & 31, hh = lane >> 5;
   const int pair = blockIdx.x, s = pair / a.c.Hkv, g = pair - s * a.c.Hkv;
   const int n = held_keys(a.c, s), c0 = block_of_keys() * kPromptKeys;
@@ -218,31 +306,36 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3
       for (int ks = 0; ks < KS; ++ks) Kr[u][ks] = *(const bf16x8*)(kp + 16 * ks);
     }
   }
-  f32x16 sum[2] = {(f32x16){0}, (f32x16){0}};
+  float sum[2][4] = {};  // of the lane's keys, over the rows so far
   const int zrow = lq * ROWB + 16 * (hh ^ swz<ROWB>(lq));
   auto compute = [&](int stage, int q0) {
-    const char* const at = ring + stage * STAGEB;
-    const float l = ((const float*)(at + 32 * ROWB))[lane];
-    const float nl = q0 + lq < nq && l != -INFINITY ? -l * kLog2e : -INFINITY;
+    char* const at = ring + stage * STAGEB;
+    float* const stat = (float*)(at + 32 * ROWB);
+    // the rows' L becomes -L in the exponent's base (-inf where the row adds nothing), and goes to the lanes that hold its products
+    const float l = stat[lane];
+    stat[lane] = q0 + lq < nq && l != -INFINITY ? -l * kLog2e : -INFINITY;
     bf16x8 q[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) q[ks] = lds_b128(at, zrow ^ (32 * ks));
+    f32x4 nl[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) nl[i] = *(const f32x4*)(stat + 8 * i + 4 * hh);
     const bool some = a.causal && q0 + off - c0 < kPromptKeys - 1;  // (not all rows see all keys)
-    const int last = nl != -INFINITY ? q0 + lq + off - c0 - 4 * hh : -1;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       f32x16 S = (f32x16){0};
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) S = mfma32<F16>(Kr[u][ks], q[ks], S);
+      for (int ks = 0; ks < KS; ++ks) S = mfma32<F16>(q[ks], Kr[u][ks], S);
       if (some) {
+        const int first = c0 + 32 * u + lq - off - q0 - 4 * hh;  // the first row that sees the lane's key, from the half's first
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float e = fast_exp2(__builtin_fmaf(S[r], c2, nl));
-          sum[u][r] += 32 * u + acc_row(r, 0) <= last ? e : 0.f;
+          const float x = nl[r / 4][r % 4], e = fast_exp2(__builtin_fmaf(S[r], c2, x));
+          sum[u][r & 3] += (x != -INFINITY) & (acc_row(r, 0) >= first) ? e : 0.f;
         }
       } else {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sum[u][r] += fast_exp2(__builtin_fmaf(S[r], c2, nl));
+        for (int r = 0; r < 16; ++r) sum[u][r & 3] += fast_exp2(__builtin_fmaf(S[r], c2, nl[r / 4][r % 4]));
       }
     }
   };
@@ -265,23 +358,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (read before its place is requested again)
     }
   }
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const float total = sum_with_partner32(sum[u][0] + sum[u][1] + (sum[u][2] + sum[u][3]));
+    if (hh == 0) part[w * kPromptKeys + 32 * u + lq] = total;
+  }
   __syncthreads();
-  float* const part = (float*)smem;
+  if (tid < kPromptKeys && c0 + tid < n) {
+    float total = 0.f;
 #pragma unroll
-  for (int u = 0; u < 2; ++u)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) part[(w * kPromptKeys + 32 * u + acc_row(r, hh)) * PITCH + lq] = sum[u][r];
-  __syncthreads();
-  // thread (key, quarter of the lanes): the four wavefronts' sums one after the other, then the quarters
-  const int key = tid >> 2, quarter = tid & 3;
-  float total = 0.f;
-#pragma unroll
-  for (int u = 0; u < NW; ++u)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) total += part[(u * kPromptKeys + key) * PITCH + 8 * quarter + i];
-  total += __shfl_xor(total, 1);
-  total += __shfl_xor(total, 2);
-  if (quarter == 0 && c0 + key < n) a.weights[((long)s * a.c.Hkv + g) * a.c.Nk + c0 + key] += total;
+    for (int u = 0; u < NW; ++u) total += part[u * kPromptKeys + tid];
+    a.weights[((long)s * a.c.Hkv + g) * a.c.Nk + c0 + tid] += total;
+  }
 }
 
 template <int D, bool F16>
@@ -291,14 +379,14 @@ static hipError_t launch_weights_d(const WeightsArgs& a, hipStream_t st) {
   // workgroups (us, rows stay / keys stay: 256 rows among 256 keys, 2 x 8 pairs of 128: 10.4 / 7.4; 256 rows (G = 4) on 2000 keys, 4 x 8 pairs
   // of 64: 9.1 / 13.6; 64 rows on up to 4096, 16 x 8 of 128: 29 / 54; 40 rows, 32 x 8: 46 / 101)
   if ((long)a.Nq * a.G <= kStepRows && ((long)a.Nq * a.G <= 32 || a.c.Nk > 2l * a.Nq)) {
-    // Two workgroups a compute unit, or up to four tiles a wavefront (us at 128 / 256 / 512 / 1024 / 2048 keys: 4 sequences of up to 2048, 8
-    // heads of 128: 5.2 / 5.2 / 7.2; 8 of up to 4096: 16.1 / 14.5 / 12.3; 64 of up to 8192: - / - / 109 / 113 / 123; 96 of up to 2048, heads
-    // of 64: - / 25.8 / 24.8 / 28.4 / 30.6)
+    // Two workgroups a compute unit, or up to four tiles a wavefront (us at 128 / 256 / 512 / 1024 keys: 4 sequences of up to 2048, 8
+    // heads of 128: 5.3 / 5.1 / 6.6 / 9.4; 8 of up to 4096: 14.5 / 11.3 / 10.0 / 10.0; 64 of up to 8192: 143 / 105 / 96 / 96; 96 of up to
+    // 2048, heads of 64: 34 / 27 / 25 / 27)
     long keys = ((long)pairs * a.c.Nk / 512 + 127) / 128 * 128;
-    keys = keys < 128 ? 128 : (keys > 512 ? 512 : keys);
+    keys = keys < 128 ? 128 : (keys > kStepKeys ? kStepKeys : keys);
     const dim3 grid = grid_of(pairs, (a.c.Nk + keys - 1) / keys);
-    if (a.Nq * a.G <= 32) hipLaunchKernelGGL((weights_step_kernel<D, F16, false>), grid, dim3(256), 0, st, a, (int)keys);
-    else hipLaunchKernelGGL((weights_step_kernel<D, F16, true>), grid, dim3(256), 0, st, a, (int)keys);
+    if (a.Nq * a.G <= 32) hipLaunchKernelGGL((weights_step_kernel<D, F16>), grid, dim3(256), 0, st, a, (int)keys);
+    else hipLaunchKernelGGL((weights_rows_kernel<D, F16>), grid, dim3(256), 0, st, a, (int)keys);
   } else {
     hipLaunchKernelGGL((weights_prompt_kernel<D, F16>), grid_of(pairs, ((long)a.c.Nk + kPromptKeys - 1) / kPromptKeys), dim3(256), 0, st, a);
   }
