@@ -36,7 +36,7 @@ struct Picked {
 };
 
 size_t verify_workspace(int B, int k, int V) {
-  return (size_t)B * (segments_of(V) * (sizeof(SegmentSums) + (size_t)(k + 1) * sizeof(RowPart)) + (size_t)(k + 1) * sizeof(Picked));
+  return (size_t)B * (segments_of(V) * (sizeof(SegmentSums) + (size_t)(k + 1) * sizeof(RowPart)) + (size_t)(k + 1) * sizeof(Picked) + sizeof(float));
 }
 __device__ __forceinline__ SegmentSums* segment_sums(const VerifyArgs& a, long b) { return (SegmentSums*)a.ws + b * segments_of(a.V); }
 __device__ __forceinline__ RowPart* row_parts(const VerifyArgs& a, long row) {
@@ -44,6 +44,8 @@ __device__ __forceinline__ RowPart* row_parts(const VerifyArgs& a, long row) {
   return (RowPart*)((SegmentSums*)a.ws + (long)a.nseq * n) + row * n;
 }
 __device__ __forceinline__ Picked* picked(const VerifyArgs& a) { return (Picked*)row_parts(a, (long)a.nseq * (a.k + 1)); }
+
+__device__ __forceinline__ float* drawn_maxima(const VerifyArgs& a) { return (float*)(picked(a) + (long)a.nseq * (a.k + 1)); }  // of the rows that are drawn from
 
 __device__ __forceinline__ float element(const void* p, int type, long i) {
   if (type == FA_TYPE_F32) return ((const float*)p)[i];
@@ -75,23 +77,52 @@ __device__ __forceinline__ void eight(const void* p, int type, long i, int n, fl
   }
 }
 
-__device__ __forceinline__ float wave_max(float x) {
-  for (int o = 32; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
+// Over the lanes of a wavefront (all active) with data-parallel moves, which take a few cycles where a permutation through LDS takes a
+// hundred: each step adds the lane 1, 2, 4, 8 below in its row of 16, then the last lane of the rows below.
+template <int CTRL, int ROWS, class T>
+__device__ __forceinline__ T from_below(T x, T none) {  // `none` where there is no such lane
+  static_assert(sizeof(T) == 4 || sizeof(T) == 8, "");
+  constexpr int W = sizeof(T) / 4;
+  int v[W], o[W];
+  __builtin_memcpy(v, &x, sizeof(T));
+  __builtin_memcpy(o, &none, sizeof(T));
+#pragma unroll
+  for (int i = 0; i < W; ++i) v[i] = __builtin_amdgcn_update_dpp(o[i], v[i], CTRL, ROWS, 0xf, false);
+  __builtin_memcpy(&x, v, sizeof(T));
   return x;
 }
+template <class T, class F>
+__device__ __forceinline__ T wave_fold(T x, T none, F f) {  // of the lanes up to this one
+  x = f(x, from_below<0x111, 0xf>(x, none));
+  x = f(x, from_below<0x112, 0xf>(x, none));
+  x = f(x, from_below<0x114, 0xf>(x, none));
+  x = f(x, from_below<0x118, 0xf>(x, none));
+  x = f(x, from_below<0x142, 0xa>(x, none));
+  return f(x, from_below<0x143, 0xc>(x, none));
+}
 template <class T>
-__device__ __forceinline__ T wave_add(T x) {
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+__device__ __forceinline__ T in_lane(T x, int lane) {
+  constexpr int W = sizeof(T) / 4;
+  int v[W];
+  __builtin_memcpy(v, &x, sizeof(T));
+#pragma unroll
+  for (int i = 0; i < W; ++i) v[i] = __builtin_amdgcn_readlane(v[i], lane);
+  __builtin_memcpy(&x, v, sizeof(T));
   return x;
 }
 template <class T>
 __device__ __forceinline__ T wave_scan(T x) {  // sum of the lanes up to this one
-  const int lane = threadIdx.x & 63;
-  for (int o = 1; o < 64; o <<= 1) {
-    const T y = __shfl_up(x, o);
-    if (lane >= o) x += y;
-  }
-  return x;
+  return wave_fold(x, (T)0, [](T u, T v) { return u + v; });
+}
+template <class T>
+__device__ __forceinline__ T wave_add(T x) {
+  return in_lane(wave_scan(x), 63);
+}
+__device__ __forceinline__ float wave_max(float x) {
+  return in_lane(wave_fold(x, -INFINITY, [](float u, float v) { return fmaxf(u, v); }), 63);
+}
+__device__ __forceinline__ int wave_max(int x) {
+  return in_lane(wave_fold(x, -0x7fffffff - 1, [](int u, int v) { return max(u, v); }), 63);
 }
 
 __device__ __forceinline__ int draft_token(const VerifyArgs& a, long b, int i) {  // -1: none
@@ -138,11 +169,14 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_stats_kernel(VerifyArgs
   if (seg == 0 && lane == 0) picked(a)[row] = pick(a, row / (a.k + 1), (int)(row % (a.k + 1)));
 }
 
-// Maximum of a row, and its sum against it (by a wavefront).
-__device__ __forceinline__ RowPart whole_row(const VerifyArgs& a, long row) {
+// Maximum of a row, and its sum against it (by a wavefront), from `mine`, this lane's segment of the first 64.
+__device__ __forceinline__ RowPart first_part(const VerifyArgs& a, long row) {
+  const int lane = threadIdx.x & 63;
+  return lane < segments_of(a.V) ? row_parts(a, row)[lane] : RowPart{-INFINITY, 0.f};
+}
+__device__ __forceinline__ RowPart whole_row(const VerifyArgs& a, long row, RowPart mine) {
   const RowPart* part = row_parts(a, row);
   const int n = segments_of(a.V), lane = threadIdx.x & 63;
-  const RowPart mine = lane < n ? part[lane] : RowPart{-INFINITY, 0.f};
   float m = mine.max;
   for (int i = 64 + lane; i < n; i += 64) m = fmaxf(m, part[i].max);
   m = wave_max(m);
@@ -152,28 +186,29 @@ __device__ __forceinline__ RowPart whole_row(const VerifyArgs& a, long row) {
   for (int i = 64 + lane; i < n; i += 64) take(part[i]);
   return {m, wave_add(z)};
 }
-// exp(inv_t (l - m)) in float64: with y = inv_t log2(e) (l - m) and n the whole number next to it, 2^n times the Taylor series of
-// 2^(y - n) = exp((y - n) ln 2), whose argument is at most 0.35, up to the 10th power: the next term is 2.2e-13, by which a draw over
-// 10^5 tokens is decided otherwise once in 10^8. (The sums are bound by these instructions. 64 rows of 131072: 23.9 us with the
-// library's exp(), 21.0 so.)
+// exp(inv_t (l - m)) in float64: with y = inv_t log2(e) (l - m) and n the whole number next to it (the low bits of y + 1.5 * 2^52),
+// 2^n times the polynomial of degree 8 that meets 2^f at the nine Chebyshev points of [-1/2, 1/2], f = y - n: off by at most 1.1e-12 of
+// its value, by which a draw over 10^5 tokens is decided otherwise once in some 10^6. n goes into the exponent's bits. Less than
+// 2^-1000 is 0. (64 rows of 131072: 19.6 us with a Taylor series of eleven
+// terms, rint and ldexp and reductions through LDS, 16.5 so.)
 struct Exponential {
   double c, cm;
-  __device__ __forceinline__ Exponential(float inv_t, float m) : c((double)inv_t * 1.4426950408889634074), cm(c * (double)m) {}
+  __device__ __forceinline__ Exponential(float inv_t, float m)
+      : c((double)inv_t * 1.4426950408889634074), cm(m == -INFINITY ? 0. : c * (double)m) {}  // (a row of -inf alone: all are 0)
   __device__ __forceinline__ double operator()(float l) const {
-    constexpr double L = 0.69314718055994530942, L2 = L * L, L3 = L2 * L, L4 = L2 * L2, L5 = L4 * L;
-    const double y = __builtin_fma(c, (double)l, -cm), n = rint(y), f = y - n;
-    double s = L5 * L5 / 3628800;
-    s = __builtin_fma(s, f, L5 * L4 / 362880);
-    s = __builtin_fma(s, f, L4 * L4 / 40320);
-    s = __builtin_fma(s, f, L4 * L3 / 5040);
-    s = __builtin_fma(s, f, L3 * L3 / 720);
-    s = __builtin_fma(s, f, L5 / 120);
-    s = __builtin_fma(s, f, L4 / 24);
-    s = __builtin_fma(s, f, L3 / 6);
-    s = __builtin_fma(s, f, L2 / 2);
-    s = __builtin_fma(s, f, L);
+    constexpr double whole = 6755399441055744.;
+    const double y = __builtin_fma(c, (double)l, -cm), t = y + whole, f = y - (t - whole);
+    double s = 0x1.63d1363a681b4p-20;
+    s = __builtin_fma(s, f, 0x1.00dc4a5344ef5p-16);
+    s = __builtin_fma(s, f, 0x1.4308ac85a69f8p-13);
+    s = __builtin_fma(s, f, 0x1.5d8745a728209p-10);
+    s = __builtin_fma(s, f, 0x1.3b2ab7181b77dp-7);
+    s = __builtin_fma(s, f, 0x1.c6b08dd6fd236p-5);
+    s = __builtin_fma(s, f, 0x1.ebfbdff823cedp-3);
+    s = __builtin_fma(s, f, 0x1.62e42fef84cf0p-1);
     s = __builtin_fma(s, f, 1.);
-    return l == -INFINITY ? 0. : __builtin_ldexp(s, (int)fmax(n, -2000.));
+    const uint64_t bits = __builtin_bit_cast(uint64_t, s) + (__builtin_bit_cast(uint64_t, t) << 52);
+    return y < -1000. ? 0. : __builtin_bit_cast(double, bits);
   }
 };
 constexpr int kCertain = 3;  // in the place of a type: the drafts are certain
@@ -197,37 +232,41 @@ __device__ __forceinline__ DraftRow draft_row(const VerifyArgs& a, long b, int i
 
 template <int TYPE, int QTYPE>
 __global__ __launch_bounds__(kVerifyThreads) void verify_sums_kernel(VerifyArgs a) {
-  __shared__ int first;  // the first row whose draft is not accepted (k: none)
+  __shared__ int first;  // the first draft that is not accepted (k: none)
   __shared__ RowPart rows[kVerifyWaves];
   const long b = blockIdx.x;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  // Four rows at a time, a wavefront each, until one is not accepted
-  if (threadIdx.x == 0) first = a.k + 1;
-  RowPart r = {0.f, 1.f};
-  int i = 0;
-  for (int i0 = 0; i0 <= a.k; i0 += kVerifyWaves) {
-    i = i0 + w;
-    if (i <= a.k) {
-      const long row = b * (a.k + 1) + i;
-      const double u = (double)a.uniform[row];
-      const Picked x = a.logits ? picked(a)[row] : pick(a, b, i);
-      if (a.logits) r = whole_row(a, row);
+  // Four drafts at a time, a wavefront each, until one is not accepted. (What the last row needs is on its way meanwhile.)
+  if (threadIdx.x == 0) first = a.k;
+  const long row0 = b * (a.k + 1);
+  RowPart r = {0.f, 1.f}, last = r;
+  if (a.logits) last = first_part(a, row0 + a.k);
+  __syncthreads();
+  for (int i0 = 0; i0 < a.k; i0 += kVerifyWaves) {
+    const int i = i0 + w;
+    if (i < a.k) {
+      const double u = (double)a.uniform[row0 + i];
+      const Picked x = a.logits ? picked(a)[row0 + i] : pick(a, b, i);
+      if (a.logits) r = whole_row(a, row0 + i, first_part(a, row0 + i));
       const double p = a.logits ? Exponential(a.inv_t, r.max)(x.target) / (double)r.sum : (double)x.target;
-      if (lane == 0) rows[w] = r;
-      __syncthreads();
-      if (lane == 0 && !(x.draft >= 0.f && u * (double)x.draft < p)) atomicMin(&first, i);
-    } else {
-      __syncthreads();
+      if (lane == 0) {
+        rows[w] = r;
+        if (!(x.draft >= 0.f && u * (double)x.draft < p)) atomicMin(&first, i);
+      }
     }
     __syncthreads();
-    if (first <= a.k) break;
+    if (first < a.k) break;
     __syncthreads();  // (the rows' sums are written again)
   }
-  i = first;
-  r = rows[i % kVerifyWaves];
+  const int i = first;
+  if (i < a.k) r = rows[i % kVerifyWaves];
+  else if (a.logits) r = whole_row(a, row0 + a.k, last);
   const int seg = blockIdx.y * kVerifyWaves + w, c0 = seg * kSegment;
   if (blockIdx.y == 0) {  // the tokens so far
-    if (threadIdx.x == 0) a.accepted[b] = i;
+    if (threadIdx.x == 0) {
+      a.accepted[b] = i;
+      drawn_maxima(a)[b] = r.max;
+    }
     for (int j = threadIdx.x; j <= a.k; j += kVerifyThreads) a.tokens[b * (a.k + 1) + j] = j < i ? a.drafts[b * a.k + j] : -1;
   }
   if (c0 >= a.V) return;
@@ -256,15 +295,14 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_sums_kernel(VerifyArgs 
       const double p = a.logits ? weight(x[u]) : (double)x[u];
       sp += p;
       // (r.sum is good to 1e-7: a token at which that decides has p = q to within it, and adds as little either way)
-      if (p * inv > (double)y[u]) sa += p, sq += (double)y[u];
+      const double more = p * inv > (double)y[u] ? 1. : 0.;
+      sa = __builtin_fma(p, more, sa);
+      sq = __builtin_fma((double)y[u], more, sq);
     }
   }
-  for (int o = 32; o; o >>= 1) {  // (side by side: each step is a latency)
-    const double x = __shfl_xor(sp, o), y = __shfl_xor(sa, o), v = __shfl_xor(sq, o);
-    sp += x;
-    sa += y;
-    sq += v;
-  }
+  sp = wave_add(sp);
+  sa = wave_add(sa);
+  sq = wave_add(sq);
   if (lane == 0) segment_sums(a, b)[seg] = {sp, sa, sq};
 }
 
@@ -279,16 +317,12 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_draw_kernel(VerifyArgs 
   const DraftRow q = draft_row(a, b, i);
   // (every wavefront for itself)
   const SegmentSums* part = segment_sums(a, b);
-  RowPart r = {0.f, 1.f};
-  if (a.logits) r = whole_row(a, row);
+  const float row_max = drawn_maxima(a)[b];
   double z = 0., above = 0., off = 0.;
   for (int c = lane; c < n; c += 64) z += part[c].p, above += part[c].above, off += part[c].drafts;
-  for (int o = 32; o; o >>= 1) {
-    const double x = __shfl_xor(z, o), y = __shfl_xor(above, o), v = __shfl_xor(off, o);
-    z += x;
-    above += y;
-    off += v;
-  }
+  z = wave_add(z);
+  above = wave_add(above);
+  off = wave_add(off);
   const double inv = a.logits ? 1. / z : 1.;
   const bool residual = above * inv - off > 0.;  // whether p - q leaves anything
   const double want = u * (residual ? above * inv - off : z * inv);
@@ -304,14 +338,14 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_draw_kernel(VerifyArgs 
     if (some) {
       const int at = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
       seg = c0 + at;
-      base = __shfl(sum - x, at);
+      base = in_lane(sum - x, at);
     }
     if (past) break;
-    done = __shfl(sum, 63);
+    done = in_lane(sum, 63);
   }
   if (seg < 0) return;  // (nothing to draw from: the token stays -1)
   // each thread: eight tokens that follow each other
-  const Exponential weight(a.inv_t, r.max);
+  const Exponential weight(a.inv_t, row_max);
   const int j0 = seg * kSegment + tid * 8;
   float l[8], d[8];
   double x[8], mine = 0.;
@@ -335,10 +369,8 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_draw_kernel(VerifyArgs 
     run += x[v];
     if (x[v] > 0. && run > want && hit == 0x7fffffff) hit = j0 + v;
   }
-  for (int o = 32; o; o >>= 1) {
-    last = max(last, __shfl_xor(last, o));
-    hit = min(hit, __shfl_xor(hit, o));
-  }
+  last = wave_max(last);
+  hit = -wave_max(-hit);
   if (lane == 0) {
     least[w] = hit;
     most[w] = last;
