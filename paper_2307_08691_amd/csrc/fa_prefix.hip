@@ -44,7 +44,7 @@ __device__ __forceinline__ long item_row(const PrefixArgs& a, const Item& it, in
 }
 
 template <int D>
-constexpr int kPrefixLds = 4 * 2 * 32 * 2 * D + 2 * 4 * 32 * 4;  // narrow: two V tiles a wavefront, later partial O; m and l
+constexpr int kPrefixLds = 4 * 2 * 32 * 2 * D + 2 * 4 * 32 * 4;  // narrow: a tile of K and of V a wavefront, later partial O; m and l
 
 template <int D, bool F16>
 __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it, char* smem) {
@@ -61,13 +61,11 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
     for (int ks = 0; ks < KS; ++ks) Qf[ks] = *(const bf16x8*)(qp + 16 * ks);
   }
   const int lim_row = it.causal && q + it.off < it.nk - 1 ? q + it.off : it.nk - 1;  // the last key of this lane's row
-  u32x4 Kn[KS], Kc[KS];  // K of the tile on its way, of the one in use
-  char* const vbuf = smem + w * WAVEB;
   // Pages of this wavefront's tiles: lane i has the one of tile i of the next 64 (looked up one by one each would be a memory latency
   // in front of its tile's requests).
   const int mask = (1 << a.own.page_log2) - 1;
   int pages = 0;
-  auto issue = [&](int key0, int buf) {
+  auto issue = [&](int key0) {
     const int last = it.end - 1 - key0;  // (rows past the end repeat the last one)
     long row = key0;
     if (it.table) {
@@ -78,10 +76,8 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
       }
       row = ((long)__builtin_amdgcn_readlane(pages, i) << a.own.page_log2) + (key0 & mask);
     }
-    const __bf16* kp = it.K + (row + (lq < last ? lq : last)) * kstride + 8 * hh;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) Kn[ks] = *(const u32x4*)(kp + 16 * ks);
-    tile_load_async<D, KT, 1>(vbuf + buf * TILEB, it.V + row * kstride, kstride, 0, last, 0, lane);
+    tile_load_async<D, KT, 1>(smem + w * WAVEB, it.K + row * kstride, kstride, 0, last, 0, lane);
+    tile_load_async<D, KT, 1>(smem + w * WAVEB + TILEB, it.V + row * kstride, kstride, 0, last, 0, lane);
   };
   f32x16 O[DT];
 #pragma unroll
@@ -92,10 +88,23 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
   int zcol[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) zcol[u] = swz_off<ROWB>(4 * hh + (p16 >> 2) + 8 * u, 2 * g16 + ((p16 & 3) >> 1)) + 8 * (p16 & 1);
-  auto compute = [&](int key0, int buf) {
+  const int zrow = w * WAVEB + lq * ROWB + 16 * (hh ^ swz<ROWB>(lq));
+  bf16x8 Kf[KS], Vf[2 * DT];  // of the tile in use: its place in LDS is the next one's at once
+  auto take = [&]() {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) Kf[ks] = lds_b128(smem, zrow ^ (32 * ks));
+    const int vb = w * WAVEB + TILEB;
+#pragma unroll
+    for (int i = 0; i < 2 * DT; ++i) {
+      const int dt = i >> 1, ro = 16 * (i & 1) * ROWB;
+      Vf[i] = lds_tr_pair(smem, ((zcol[0] + vb) ^ (64 * dt)) + ro, ((zcol[1] + vb) ^ (64 * dt)) + ro);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  };
+  auto compute = [&](int key0) {
     f32x16 S = (f32x16){0};
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) S = mfma32<F16>(__builtin_bit_cast(bf16x8, Kc[ks]), Qf[ks], S);
+    for (int ks = 0; ks < KS; ++ks) S = mfma32<F16>(Kf[ks], Qf[ks], S);
     if ((it.causal && key0 + KT - 1 > it.row0 / a.G + it.off) || key0 + KT > it.end) {
       const int lim = (lim_row < it.end - 1 ? lim_row : it.end - 1) - key0 - 4 * hh;
 #pragma unroll
@@ -125,26 +134,22 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
     }
     l += rs;
     bf16x8 Pf[2] = {pack8<F16>(S, 0), pack8<F16>(S, 1)};
-    const int vb = w * WAVEB + buf * TILEB;
 #pragma unroll
-    for (int i = 0; i < 2 * DT; ++i) {
-      const int dt = i >> 1, ro = 16 * (i & 1) * ROWB;
-      O[dt] = mfma32<F16>(lds_tr_pair(smem, ((zcol[0] + vb) ^ (64 * dt)) + ro, ((zcol[1] + vb) ^ (64 * dt)) + ro), Pf[i & 1], O[dt]);
-    }
+    for (int i = 0; i < 2 * DT; ++i) O[i >> 1] = mfma32<F16>(Vf[i], Pf[i & 1], O[i >> 1]);
   };
+  // (K too goes through LDS, as whole rows: a lane that loads its own row straight into registers makes every request touch 64 places.
+  // 64 sequences on 8192 shared keys, up to 1024 own ones, 32 heads on 8 of 128: 41.8 -> 39.7 us; 4 on 2048, up to 256: 8.7 -> 7.4.)
   // One copy of the code of a tile: short shares run it twice, and wait for its instructions (2 KB) the first time.
   int t = it.begin + KT * w;
   if (t < it.end) {
-    issue(t, 0);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) touch(Qf[ks]);
-    for (int buf = 0;; buf ^= 1) {
+    issue(t);
+    while (true) {
       wait_vmem();
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) Kc[ks] = Kn[ks];
-      if (t + NW * KT < it.end) issue(t + NW * KT, buf ^ 1);
-      compute(t, buf);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (this tile has been read before its buffer is requested again)
+      take();
+      if (t + NW * KT < it.end) issue(t + NW * KT);
+      compute(t);
       if ((t += NW * KT) >= it.end) break;
     }
   }
