@@ -43,13 +43,16 @@ __device__ __forceinline__ long item_row(const PrefixArgs& a, const Item& it, in
   return (long)it.slot * a.nseq * a.Nq * a.Hq + (it.tok0 + q) * a.Hq + it.g * a.G + (row - q * a.G);
 }
 
+// Tiles of K and of V that a wavefront of a narrow item has on their way (8 KB each of 64 columns, 16 of 128; eight wavefronts a unit)
 template <int D>
-constexpr int kPrefixLds = 4 * 2 * 32 * 2 * D + 2 * 4 * 32 * 4;  // narrow: a tile of K and of V a wavefront, later partial O; m and l
+constexpr int kNarrowStages = D == 64 ? 2 : 1;
+template <int D>
+constexpr int kPrefixLds = 4 * kNarrowStages<D> * 2 * 32 * 2 * D + 2 * 4 * 32 * 4;  // narrow: those, later partial O; m and l
 
 template <int D, bool F16>
 __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it, char* smem) {
-  constexpr int NW = 4, KT = 32, KS = D / 16, DT = D / 32, ROWB = 2 * D, TILEB = KT * ROWB, WAVEB = 2 * TILEB, STAT_OFF = NW * WAVEB;
-  static_assert(WAVEB == D * 32 * 4 && STAT_OFF + 2 * NW * 32 * 4 <= kPrefixLds<D>, "the partial O^T of a wavefront takes the place of its V tiles");
+  constexpr int NW = 4, KT = 32, KS = D / 16, DT = D / 32, ROWB = 2 * D, TILEB = KT * ROWB, STAGES = kNarrowStages<D>, WAVEB = STAGES * 2 * TILEB, STAT_OFF = NW * WAVEB;
+  static_assert(WAVEB >= D * 32 * 4 && STAT_OFF + 2 * NW * 32 * 4 <= kPrefixLds<D>, "the partial O^T of a wavefront takes the place of its tiles");
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane & 31, hh = lane >> 5;
   const long kstride = (long)a.Hkv * D;
   const int prow = it.row0 + (lq < it.rows ? lq : it.rows - 1);  // (lanes past the end compute on a copy and store nothing)
@@ -65,7 +68,7 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
   // in front of its tile's requests).
   const int mask = (1 << a.own.page_log2) - 1;
   int pages = 0;
-  auto issue = [&](int key0) {
+  auto issue = [&](int key0, int stage) {
     const int last = it.end - 1 - key0;  // (rows past the end repeat the last one)
     long row = key0;
     if (it.table) {
@@ -76,8 +79,9 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
       }
       row = ((long)__builtin_amdgcn_readlane(pages, i) << a.own.page_log2) + (key0 & mask);
     }
-    tile_load_async<D, KT, 1>(smem + w * WAVEB, it.K + row * kstride, kstride, 0, last, 0, lane);
-    tile_load_async<D, KT, 1>(smem + w * WAVEB + TILEB, it.V + row * kstride, kstride, 0, last, 0, lane);
+    char* const to = smem + w * WAVEB + stage * 2 * TILEB;
+    tile_load_async<D, KT, 1>(to, it.K + row * kstride, kstride, 0, last, 0, lane);
+    tile_load_async<D, KT, 1>(to + TILEB, it.V + row * kstride, kstride, 0, last, 0, lane);
   };
   f32x16 O[DT];
 #pragma unroll
@@ -88,12 +92,12 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
   int zcol[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) zcol[u] = swz_off<ROWB>(4 * hh + (p16 >> 2) + 8 * u, 2 * g16 + ((p16 & 3) >> 1)) + 8 * (p16 & 1);
-  const int zrow = w * WAVEB + lq * ROWB + 16 * (hh ^ swz<ROWB>(lq));
+  const int zrow = lq * ROWB + 16 * (hh ^ swz<ROWB>(lq));
   bf16x8 Kf[KS], Vf[2 * DT];  // of the tile in use: its place in LDS is the next one's at once
-  auto take = [&]() {
+  auto take = [&](int stage) {
+    const int kb = w * WAVEB + stage * 2 * TILEB, vb = kb + TILEB;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) Kf[ks] = lds_b128(smem, zrow ^ (32 * ks));
-    const int vb = w * WAVEB + TILEB;
+    for (int ks = 0; ks < KS; ++ks) Kf[ks] = lds_b128(smem, (zrow + kb) ^ (32 * ks));
 #pragma unroll
     for (int i = 0; i < 2 * DT; ++i) {
       const int dt = i >> 1, ro = 16 * (i & 1) * ROWB;
@@ -144,11 +148,13 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
   if (t < it.end) {
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) touch(Qf[ks]);
-    issue(t);
-    while (true) {
-      wait_vmem();
-      take();
-      if (t + NW * KT < it.end) issue(t + NW * KT);
+    issue(t, 0);
+    if (STAGES == 2 && t + NW * KT < it.end) issue(t + NW * KT, 1);
+    for (int stage = 0;; stage ^= STAGES - 1) {
+      if (STAGES == 2 && t + NW * KT < it.end) wait_vmem_upto<2 * TILEB / 1024>();
+      else wait_vmem();
+      take(stage);
+      if (t + STAGES * NW * KT < it.end) issue(t + STAGES * NW * KT, stage);
       compute(t);
       if ((t += NW * KT) >= it.end) break;
     }
