@@ -485,14 +485,15 @@ PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int d) {
   };
   p.prefix_rows = all <= 32 ? 32 : 128;
   const long units = Hkv * up(all, p.prefix_rows);
-  // Half as many prefix items as compute units, or shares of 1024 keys where that makes more of them, up to one a unit (64 sequences,
-  // 32 heads on 8 of 128, 8192 shared keys, us at 4 / 6 / 8 / 12 shares, 16 blocks of rows: 60 / 51 / 49 / 53; 16 x 5 rows, 16 heads of 64,
-  // 12345 keys, 16 blocks, at 6 / 8 / 12: 46 / 40 / 36)
+  // Half as many prefix items as compute units, or shares of 1024 keys where that makes more of them, up to one a unit (64 sequences, 32
+  // heads on 8 of 128, 8192 shared keys, 16 blocks of rows, us of the first launch at 6 / 8 / 12 / 16 shares: 45 / 40 / 43 / 43; 16 x 5 rows, 16
+  // heads of 64, 12345 keys, 16 blocks, at 6 / 12 / 16: 40 / 31 / 31)
   const long most = clamp(up(128, units), clamp(Np / 1024, 1, up(256, units)), 16);
   cut(Np, most, 256, p.prefix_keys, p.prefix_shares);
   p.own_rows = own_rows <= 64 ? 32 : 128;
-  // Own items: with those of the prefix no more than fit on the chip at once, two a compute unit (64 x 8 pairs of up to 1024 keys beside
-  // 128 prefix items, one and two shares: 49 and 58 us; 16 x 16 pairs of up to 2048 of 64, beside 128: 40 and 43)
+  // Own items: with those of the prefix no more than fit on the chip at once, two a compute unit (16 x 16
+  // pairs of up to 2048 keys of 64, beside 192 items of the prefix, one and two shares: 31 and 36 us; 24 x 8 of up to 4096 of 128, beside
+  // 96, two, three and four: 43, 44 and 48)
   const long pairs = B * Hkv * up(own_rows, p.own_rows);
   cut(Nk, clamp((512 - units * p.prefix_shares) / pairs, 1, 8), 256, p.own_keys, p.own_shares);
   return p;

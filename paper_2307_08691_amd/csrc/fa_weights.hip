@@ -14,8 +14,8 @@
 namespace fa {
 
 // A workgroup's (sequence, key/value head): the heads of a sequence follow each other on ONE XCD, and eight sequences are under way on
-// the eight. Heads lie side by side in memory, a row of each after the other: (64 sequences of up to 8192 keys, 8 heads of 128: 114 us
-// with a head to an XCD, 109 so; 96 of up to 2048, heads of 64: 27.0 and 24.8.) The sequences past the last eight: as they come.
+// the eight. Heads lie side by side in memory, a row of each after the other: (64 sequences of up to 8192 keys, 8 heads of 128: 99 us
+// with a head to an XCD, 95 so; 96 of up to 2048, heads of 64: 26.7 and 25.3.) The sequences past the last eight: as they come.
 __device__ __forceinline__ void pair_of(int i, int nseq, int heads, int& s, int& g) {
   const int set = kXcds * heads, whole = nseq / kXcds * set;
   if (i < whole) {
@@ -376,8 +376,8 @@ template <int D, bool F16>
 static hipError_t launch_weights_d(const WeightsArgs& a, hipStream_t st) {
   const unsigned pairs = (unsigned)(a.nseq * a.c.Hkv);
   // Rows that stay, or keys that do: a prompt among its own keys has as many of these as queries, and the blocks of 64 keys make more
-  // workgroups (us, rows stay / keys stay: 256 rows among 256 keys, 2 x 8 pairs of 128: 10.4 / 7.4; 256 rows (G = 4) on 2000 keys, 4 x 8 pairs
-  // of 64: 9.1 / 13.6; 64 rows on up to 4096, 16 x 8 of 128: 29 / 54; 40 rows, 32 x 8: 46 / 101)
+  // workgroups (us, rows stay / keys stay: 256 rows among 256 keys, 2 x 8 pairs of 128: 10.8 / 6.5; 256 rows (G = 4) on up to
+  // 2000 keys, 4 x 8 pairs of 64: 9.7 / 9.9; 64 rows (G = 4) on up to 4096, 16 x 8 of 128: 31 / 79; 40 rows (G = 8), 32 x 8: 57 / 153)
   if ((long)a.Nq * a.G <= kStepRows && ((long)a.Nq * a.G <= 32 || a.c.Nk > 2l * a.Nq)) {
     // Two workgroups a compute unit, or up to four tiles a wavefront (us at 128 / 256 / 512 / 1024 keys: 4 sequences of up to 2048, 8
     // heads of 128: 5.3 / 5.1 / 6.6 / 9.4; 8 of up to 4096: 14.5 / 11.3 / 10.0 / 10.0; 64 of up to 8192: 143 / 105 / 96 / 96; 96 of up to
