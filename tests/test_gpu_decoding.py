@@ -136,6 +136,17 @@ def test_prefix_in_pages(n_p, prefix_page, page):
     check_prefix("f16", 64, 12, 3, 4, 1, n_p, 190, page, [190] * 12, prefix_page=prefix_page)
 
 
+EDGES = [700, 1, 32, 33, 127, 128, 129, 160, 161, 256, 257, 288, 289, 384, 385, 415, 511, 512, 513, 640, 641, 672, 673, 699]
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f16", 128), ("bf16", 128)])
+@pytest.mark.parametrize("page", [0, 64])
+def test_prefix_of_many_sequences(dtype, d, page):
+    """So many that each has its cache to itself: one to six tiles a wavefront, ends on and off the tiles' edges."""
+    lens = (EDGES * 3)[:64]
+    check_prefix(dtype, d, 64, 1, 8, 8, 300, 700, page, lens)
+
+
 def test_prefix_of_spread_scores():
     """The softmax's reference advances (and is left behind by up to 2^8 or 2^20) when scores spread widely."""
     for dtype in ("bf16", "f16"):
@@ -270,6 +281,17 @@ def check_weights(dtype, d, B, nq, hq, hkv, slots, page, lens, causal=True, quer
     (1, 33, 16, 1, 50, 0, [40]),                  # 528 rows, one query past a tile
 ])
 def test_weights(dtype, d, B, nq, hq, hkv, slots, page, lens):
+    check_weights(dtype, d, B, nq, hq, hkv, slots, page, lens)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f16", 128), ("bf16", 128)])
+@pytest.mark.parametrize("B,nq,hq,hkv,slots,page,lens", [
+    (64, 1, 8, 8, 700, 64, (EDGES * 3)[:64]),    # 512 keys a workgroup: up to four tiles a wavefront
+    (48, 3, 16, 8, 700, 0, (EDGES * 2)[:48]),    # (queries before the first key among them)
+    (16, 2, 8, 8, 700, 0, EDGES[:16]),           # 256
+    (24, 5, 64, 8, 800, 64, EDGES),              # 40 rows, 384
+])
+def test_weights_of_many_sequences(dtype, d, B, nq, hq, hkv, slots, page, lens):
     check_weights(dtype, d, B, nq, hq, hkv, slots, page, lens)
 
 
