@@ -458,6 +458,17 @@ def test_verify(q_type, type_, logits, B, k, V, pad):
     check_verify(drafts, None if q_type is None else q, target, r.random((B, k + 1)), logits, 1.3 if logits else 1.0, q_type, type_, pad)
 
 
+@pytest.mark.parametrize("q_type", [torch.float32, torch.bfloat16, torch.float16, None])
+@pytest.mark.parametrize("type_", [torch.float32, torch.bfloat16, torch.float16])
+def test_verify_types(q_type, type_):
+    """Every pair of types, as logits and as probabilities, over more segments than a wavefront has lanes."""
+    r = rng(21)
+    l, q, drafts = distributions(r, 3, 5, 140001)
+    p = np.exp(l - l.max(-1, keepdims=True))
+    for logits, target in ((True, l), (False, p / p.sum(-1, keepdims=True))):
+        check_verify(drafts, None if q_type is None else q, target, r.random((3, 6)), logits, 0.9 if logits else 1.0, q_type, type_)
+
+
 def test_verify_without_drafts_and_with_absent_ones():
     r = rng(8)
     l, q, drafts = distributions(r, 6, 3, 500)
