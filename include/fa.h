@@ -543,7 +543,8 @@ int fa_kvcache_fwd(const void* Q, const void* Kcache, const void* Vcache, const 
  *   the caches) and prefix_table a DEVICE array of prefix_pages int32 page numbers, prefix_pages * page_size >= Np.
  * Np = 0 (Kprefix, Vprefix may then be NULL) and own lengths of 0 are allowed; a row that sees no key at all gets O = 0, LSE = -inf.
  * Values that the causal rule hides from a query, but not from a later one, have to be finite, as for fa_kvcache_fwd (they are
- * multiplied by 0); what lies past a length is not read. B * Nq * Hq at most 2^26, Hkv at most 2^16 (FA_ERR_SHAPE beyond).
+ * multiplied by 0); what lies past a length is not read. A NaN in a query or in a key that it sees, or a score of +inf, makes the row's O
+ * and LSE NaN, whichever workgroup has that key. B * Nq * Hq at most 2^26, Hkv at most 2^16 (FA_ERR_SHAPE beyond).
  * bfloat16, d in {64, 128}. How the keys are cut over workgroups goes by the sizes alone, so results are the same bits in every
  * run; `workspace` (partial results, float32) needs fa_prefix_fwd_workspace_bytes() bytes, undefined on entry and return.
  * Forward only, as fa_kvcache_fwd.

@@ -193,10 +193,10 @@ __device__ __forceinline__ void narrow_item(const PrefixArgs& a, const Item& it,
       den += wgt * stat[32 * NW + u * 32 + r];
       o += *(const f32x4*)(smem + u * WAVEB + r * (4 * D) + 16 * (c ^ (r & (CPR - 1)))) * wgt;
     }
-    const float inv = den > 0.f ? 1.f / den : 0.f;  // (no visible key: L = -inf, and the merge does not look at O)
+    const float inv = den == 0.f ? 0.f : 1.f / den;  // (no visible key: L = -inf, and the merge does not look at O; a NaN stays one)
     const long at = item_row(a, it, r);
     *(f32x4*)(a.Opart + at * D + 4 * c) = o * inv;
-    if (c == 0) a.Lpart[at] = den > 0.f ? mm * a.scale + fast_log2(den) * kLn2 : -INFINITY;
+    if (c == 0) a.Lpart[at] = den == 0.f ? -INFINITY : mm * a.scale + fast_log2(den) * kLn2;
   }
 }
 
@@ -317,7 +317,7 @@ __device__ __forceinline__ void wide_item(const PrefixArgs& a, const Item& it, c
   }
   // ---- through LDS, so that whole rows are stored (16 bytes a row and instruction straight from the accumulators took 1 us per MB)
   const float lsum = sum_with_partner32(l);
-  const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+  const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
   lds_barrier();  // everyone has read the last tiles
   constexpr int CPR = D / 4;  // 16-byte chunks of a row
   char* const stage = smem + w * (32 * 4 * D);
@@ -336,7 +336,7 @@ __device__ __forceinline__ void wide_item(const PrefixArgs& a, const Item& it, c
     const f32x4 o = *(const f32x4*)(stage + r * (4 * D) + 16 * (c ^ (r & (CPR - 1))));
     if (r0 + r < it.rows) *(f32x4*)(a.Opart + item_row(a, it, r0 + r) * D + 4 * c) = o;
   }
-  if (hh == 0 && mine < it.rows) a.Lpart[item_row(a, it, mine)] = lsum > 0.f ? m * a.scale + fast_log2(lsum) * kLn2 : -INFINITY;
+  if (hh == 0 && mine < it.rows) a.Lpart[item_row(a, it, mine)] = lsum == 0.f ? -INFINITY : m * a.scale + fast_log2(lsum) * kLn2;
 }
 
 __device__ __forceinline__ void empty_item(const PrefixArgs& a, const Item& it) {
@@ -419,9 +419,9 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixArgs a, int slo
     for (int u = 0; u < FLY; ++u) o[u] = *(const f32x4*)(a.Opart + ((k0 + u < slots ? k0 + u : slots - 1) * all + r) * D + 4 * c);
   };
   request(0);
-  for (int k = FLY; k < slots; ++k) mx = fmaxf(mx, a.Lpart[k * all + r]);
+  for (int k = FLY; k < slots; ++k) mx = max_or_nan(mx, a.Lpart[k * all + r]);
 #pragma unroll
-  for (int u = 0; u < FLY; ++u) mx = fmaxf(mx, l[u]);
+  for (int u = 0; u < FLY; ++u) mx = max_or_nan(mx, l[u]);
   const long tok = r / a.Hq;
   const int h = (int)(r - tok * a.Hq);
   const long s = tok / a.Nq;
