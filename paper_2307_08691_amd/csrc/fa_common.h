@@ -439,7 +439,7 @@ __device__ __forceinline__ void mask_past(f32x16 (&S)[2], int lim) {
 }
 
 // The larger of two, or NaN where one is. (fmaxf drops a NaN: a share of a row's keys would pass for one without keys.)
-__device__ __forceinline__ float max_or_nan(float x, float y) { return y > x || y != y ? y : x; }
+__device__ __forceinline__ float max_or_nan(float x, float y) { return __builtin_elementwise_maximum(x, y); }
 
 __device__ __forceinline__ float sum_with_partner32(float x) {
   int xi = __builtin_bit_cast(int, x);

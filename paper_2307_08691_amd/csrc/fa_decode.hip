@@ -282,7 +282,7 @@ __global__ __launch_bounds__(64 * decode_waves(D, TWO)) __attribute__((amdgpu_wa
     const bool ok = r < nrows;
     const int prow2 = ok ? r : nrows - 1;
     const int row2 = prow2 / p.G, h2 = g * p.G + prow2 % p.G;
-    const float inv = den > 0.f ? 1.f / den : 0.f;  // no visible key in this share: O = 0, L = -inf
+    const float inv = den == 0.f ? 0.f : 1.f / den;  // no visible key in this share: O = 0, L = -inf (a NaN stays one)
     float out[CPT];
 #pragma unroll
     for (int i = 0; i < CPT; ++i) {
@@ -292,7 +292,7 @@ __global__ __launch_bounds__(64 * decode_waves(D, TWO)) __attribute__((amdgpu_wa
       for (int ww = 0; ww < NW; ++ww) acc += wgt[ww] * ((const float*)(smem + ww * WAVEB))[dcol * 32 + r];
       out[i] = acc * inv;
     }
-    const float lse = den > 0.f ? mm * p.scale + fast_log2(den) * kLn2 : -INFINITY;
+    const float lse = den == 0.f ? -INFINITY : mm * p.scale + fast_log2(den) * kLn2;
     const long lidx = s * p.lse_seq_stride + (long)h2 * p.lse_head_stride + row2;
     if (direct) {  // the final result, rounded to the element type
       if (ok) {

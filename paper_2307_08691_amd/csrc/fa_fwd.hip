@@ -548,8 +548,8 @@ __global__ __launch_bounds__(512)
 
   // ---- epilogue: O = diag(l)^-1 O, L = m + log l (Algorithm 1, lines 12-15)
   const float lsum = sum_with_partner32(l);
-  if (SPLIT && !direct) {  // partial result of this share of the keys, float32; no visible key: O = 0, L = -inf
-    const float inv = lsum > 0.f ? 1.0f / lsum : 0.f;
+  if (SPLIT && !direct) {  // partial result of this share of the keys, float32; no visible key: O = 0, L = -inf (a NaN stays one)
+    const float inv = lsum == 0.f ? 0.f : 1.0f / lsum;
     if (row_ok) {
       const long tok = si.tok0 + row;
       float* op = a.Opart + (((long)split * p.total_tokens + tok) * p.Hq + h) * D + 4 * hh;
@@ -564,12 +564,12 @@ __global__ __launch_bounds__(512)
         }
       if (hh == 0)
         a.Lpart[(long)split * p.total_tokens * p.Hq + s * p.lse_seq_stride + h * p.lse_head_stride + row] =
-            lsum > 0.f ? m * p.scale + fast_log2(lsum) * kLn2 : -INFINITY;
+            lsum == 0.f ? -INFINITY : m * p.scale + fast_log2(lsum) * kLn2;
     }
     return;
   }
   // (mask, window: a row without any key ends with l = 0: O = 0, L = -inf)
-  const float inv = GUARD && !(lsum > 0.f) ? 0.f : (DROPOUT ? p.drop_rp : 1.0f) / lsum;
+  const float inv = GUARD && lsum == 0.f ? 0.f : (DROPOUT ? p.drop_rp : 1.0f) / lsum;
   {
     // O through the ring slot that neither holds a block still in use nor receives one of the
     // copies issued past the last block (those fill the three slots after block ncol - 1)
@@ -603,8 +603,8 @@ __global__ __launch_bounds__(512)
     }
     if ((SPLIT ? row_ok : row < n) && hh == 0)
       a.LSE[s * p.lse_seq_stride + h * p.lse_head_stride + (p.cu_seqlens ? si.tok0 : 0) + row] =
-          MASK    ? (lsum > 0.f ? m + fast_log2(lsum) * kLn2 : -INFINITY)
-          : GUARD ? (lsum > 0.f ? m * p.scale + fast_log2(lsum) * kLn2 : -INFINITY)
+          MASK    ? (lsum == 0.f ? -INFINITY : m + fast_log2(lsum) * kLn2)
+          : GUARD ? (lsum == 0.f ? -INFINITY : m * p.scale + fast_log2(lsum) * kLn2)
                   : m * p.scale + fast_log2(lsum) * kLn2;
   }
 }
@@ -917,12 +917,12 @@ __device__ __forceinline__ void merge_row(const FwdArgs& a, long r, int c, long 
 #pragma unroll
       for (int u = 0; u < FLY; ++u) x[u] = lse_of(k0 + u);
 #pragma unroll
-      for (int u = 0; u < FLY; ++u) mx = fmaxf(mx, x[u]);
+      for (int u = 0; u < FLY; ++u) mx = max_or_nan(mx, x[u]);
     }
   }
   request(0);
 #pragma unroll
-  for (int u = 0; u < FLY; ++u) mx = fmaxf(mx, lp[u]);
+  for (int u = 0; u < FLY; ++u) mx = max_or_nan(mx, lp[u]);
   if (mx == -INFINITY) {  // no share holds a key that this row sees: P = 0, so O = 0 and L = -inf
     *(u32x2*)(a.O + r * D + 4 * c) = (u32x2){0u, 0u};
     if (c == 0) a.LSE[li] = -INFINITY;

@@ -1,5 +1,6 @@
-"""GPU: infinities and NaN in the operators of a decoding batch. What a query, or a key that it sees, makes NaN in a row's softmax stays NaN
-in the result: no share of the keys drops out silently, and rows that do not see it keep their values."""
+"""GPU: infinities and NaN in the operators of a decoding batch and in the split-key forward beside them. What a query, or a key that it
+sees, makes NaN in a row's softmax stays NaN in the result: no share of the keys drops out silently, and rows that do not see it keep
+their values."""
 import numpy as np
 import pytest
 
@@ -117,3 +118,30 @@ def test_prefix_of_nan_queries_alone():
         p.Q[0, 0, 1] = NAN
         row = torch.tensor([[[False, True]]], device="cuda")
         same_but(p(), clean, size, row, torch.zeros_like(row))
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f16", 128)])
+@pytest.mark.parametrize("nq,splits", [(1, 1), (1, 4), (1, 11), (40, 1), (40, 4)])  # few rows, and blocks of them; the result itself, and shares
+def test_split_keys_that_are_nan(dtype, d, nq, splits):
+    r = rng(nq + splits)
+    B, hq, hkv, n = 2, 4, 2, 1500
+    Q = gpu(r.normal(size=(B, nq, hq, d)), TYPES[dtype])
+    K, V = (gpu(r.normal(size=(B, n, hkv, d)), TYPES[dtype]) for _ in range(2))
+
+    def call(V=V):
+        O, L = binding.fa_kvcache_fwd(Q, K, V, d**-0.5, True, seqlens_k=ints([n, n - 300]), num_splits=splits)
+        torch.cuda.synchronize()
+        return O, L.transpose(1, 2)
+
+    clean, size = call(), call(V.abs())[0]
+    head = torch.arange(hq, device="cuda").expand(B, nq, hq) // (hq // hkv)
+    seq = torch.arange(B, device="cuda")[:, None, None]
+    for key in (0, 800):
+        x = K[1, key, 0].clone()
+        K[1, key, 0, 9] = NAN
+        same_but(call(), clean, size, (head == 0) & (seq == 1), (head != 0) | (seq != 1))
+        K[1, key, 0] = x
+    Q[0, nq - 1, 3, 0] = NAN
+    row = torch.zeros((B, nq, hq), dtype=torch.bool, device="cuda")
+    row[0, nq - 1, 3] = True
+    same_but(call(), clean, size, row, (head != 1) | (seq != 0))
