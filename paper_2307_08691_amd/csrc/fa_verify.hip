@@ -12,6 +12,8 @@
 //   draw    per sequence: the segment in which the running sum passes, then the token in it: a chain of latencies
 #include <hip/hip_runtime.h>
 
+#include <cfloat>
+
 #include "../../include/fa.h"
 #include "fa_kernels.h"
 
@@ -141,7 +143,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_stats_kernel(VerifyArgs
   const long row = blockIdx.x;
   const int lane = threadIdx.x & 63, seg = blockIdx.y * kVerifyWaves + (threadIdx.x >> 6), c0 = seg * kSegment;
   if (seg >= segments_of(a.V)) return;
-  const float t2 = a.inv_t * kLog2e;
+  const float t2 = fminf(a.inv_t * kLog2e, FLT_MAX);  // (finite: the maximum itself is 0 of it)
   float x[kPieces][8], m = -INFINITY;
   if (c0 + kSegment <= a.V) {  // (a branch of the whole wavefront: its loads are then requested together)
 #pragma unroll
@@ -186,18 +188,19 @@ __device__ __forceinline__ RowPart whole_row(const VerifyArgs& a, long row, RowP
   for (int i = 64 + lane; i < n; i += 64) take(part[i]);
   return {m, wave_add(z)};
 }
-// exp(inv_t (l - m)) in float64: with y = inv_t log2(e) (l - m) and n the whole number next to it (the low bits of y + 1.5 * 2^52),
+// exp(inv_t (l - m)) in float64: with y = inv_t log2(e) (l - m), the difference first (the maximum's own weight is 1 whatever inv_t is; the
+// difference of two products would leave it 2^-53 of them, which counts from about 10^13 on), and n the whole number next to it (the low bits of y + 1.5 * 2^52),
 // 2^n times the polynomial of degree 8 that meets 2^f at the nine Chebyshev points of [-1/2, 1/2], f = y - n: off by at most 1.1e-12 of
 // its value, by which a draw over 10^5 tokens is decided otherwise once in some 10^6. n goes into the exponent's bits. Less than
 // 2^-1000 is 0. (64 rows of 131072: 19.6 us with a Taylor series of eleven
 // terms, rint and ldexp and reductions through LDS, 16.5 so.)
 struct Exponential {
-  double c, cm;
-  __device__ __forceinline__ Exponential(float inv_t, float m)
-      : c((double)inv_t * 1.4426950408889634074), cm(m == -INFINITY ? 0. : c * (double)m) {}  // (a row of -inf alone: all are 0)
+  double c, m;
+  __device__ __forceinline__ Exponential(float inv_t, float max)
+      : c((double)inv_t * 1.4426950408889634074), m(max == -INFINITY ? 0. : (double)max) {}  // (a row of -inf alone: all are 0)
   __device__ __forceinline__ double operator()(float l) const {
     constexpr double whole = 6755399441055744.;
-    const double y = __builtin_fma(c, (double)l, -cm), t = y + whole, f = y - (t - whole);
+    const double y = c * ((double)l - m), t = y + whole, f = y - (t - whole);
     double s = 0x1.63d1363a681b4p-20;
     s = __builtin_fma(s, f, 0x1.00dc4a5344ef5p-16);
     s = __builtin_fma(s, f, 0x1.4308ac85a69f8p-13);

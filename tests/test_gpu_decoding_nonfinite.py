@@ -1,12 +1,12 @@
 """GPU: infinities and NaN in the operators of a decoding batch and in the split-key forward beside them. What a query, or a key that it
 sees, makes NaN in a row's softmax stays NaN in the result: no share of the keys drops out silently, and rows that do not see it keep
-their values."""
+their values. And verification of drafts at inverse temperatures from the smallest to the largest float32."""
 import numpy as np
 import pytest
 
 from paper_2307_08691_amd import binding
 from oracle import decoding_oracle as dec
-from test_gpu_decoding import TYPES, Cache, f64, gpu, ints, rng
+from test_gpu_decoding import TYPES, Cache, check_verify, distributions, f64, gpu, ints, rng
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -145,3 +145,21 @@ def test_split_keys_that_are_nan(dtype, d, nq, splits):
     row = torch.zeros((B, nq, hq), dtype=torch.bool, device="cuda")
     row[0, nq - 1, 3] = True
     same_but(call(), clean, size, row, (head != 1) | (seq != 0))
+
+
+@pytest.mark.parametrize("inv_t", [1e-42, 1e-30, 1e3, 1e6, 1e14, 1e16, 1e18, 1e20, 2.4e38, float(np.finfo(np.float32).max)])
+@pytest.mark.parametrize("q_type", [torch.float32, None])
+def test_verify_extreme_temperatures(inv_t, q_type):
+    """From even to the largest logit alone (how greedy decoding is asked for): two equal largest ones share the draw, -inf stays out."""
+    r = rng(31)
+    l, q, drafts = distributions(r, 12, 3, 9000)
+    l[:, :, ::7] = -np.inf
+    top = l.max(-1) + 0.5
+    for i in (1000, 8001):
+        np.put_along_axis(l, np.full((12, 4, 1), i), top[..., None], 2)
+    l[3, 0] = -np.inf
+    l[4] += 1e4  # (far from 0)
+    drafts[:6, 0], drafts[::2, 1] = 1000, 8001
+    u = r.random((12, 4)).astype(np.float32)
+    for type_ in (torch.float32, torch.bfloat16):
+        check_verify(drafts, None if q_type is None else q, l, u, True, inv_t, q_type, type_)
