@@ -313,21 +313,23 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4
     float* const stat = (float*)(at + 32 * ROWB);
     // the rows' L becomes -L in the exponent's base (-inf where the row adds nothing), and goes to the lanes that hold its products
     const float l = stat[lane];
-    stat[lane] = q0 + lq < nq && l != -INFINITY ? -l * kLog2e : -INFINITY;
+    const bool in = q0 + lq < nq && l != -INFINITY;
+    stat[lane] = in ? -l * kLog2e : -INFINITY;
     bf16x8 q[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) q[ks] = lds_b128(at, zrow ^ (32 * ks));
     f32x4 nl[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) nl[i] = *(const f32x4*)(stat + 8 * i + 4 * hh);
-    const bool some = a.causal && q0 + off - c0 < kPromptKeys - 1;  // (not all rows see all keys)
+    // (not all rows see all keys, or some are to add nothing: their scores may be NaN or +inf, and the exponential then is no 0)
+    const bool some = (a.causal && q0 + off - c0 < kPromptKeys - 1) || __builtin_amdgcn_ballot_w64(!in);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       f32x16 S = (f32x16){0};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) S = mfma32<F16>(q[ks], Kr[u][ks], S);
       if (some) {
-        const int first = c0 + 32 * u + lq - off - q0 - 4 * hh;  // the first row that sees the lane's key, from the half's first
+        const int first = a.causal ? c0 + 32 * u + lq - off - q0 - 4 * hh : 0;  // the first row that sees the lane's key, from the half's first
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const float x = nl[r / 4][r % 4], e = fast_exp2(__builtin_fmaf(S[r], c2, x));

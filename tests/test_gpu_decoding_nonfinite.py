@@ -147,6 +147,26 @@ def test_split_keys_that_are_nan(dtype, d, nq, splits):
     same_but(call(), clean, size, row, (head != 1) | (seq != 0))
 
 
+@pytest.mark.parametrize("nq,hq", [(2, 4), (60, 4), (300, 4)])  # rows in registers, in LDS, streaming
+@pytest.mark.parametrize("causal", [False, True])
+def test_weights_rows_without_a_logsumexp_add_nothing(nq, hq, causal):
+    """LSE = -inf takes a row out, whatever its query holds."""
+    r = rng(nq)
+    K = gpu(r.normal(size=(2, 500, 2, 64)), torch.bfloat16)
+    Q = gpu(r.normal(size=(2, nq, hq, 64)), torch.bfloat16)
+    _, L = binding.fa_kvcache_fwd(Q, K, K, 0.125, causal)
+    out = rng(1).random((2, hq, nq)) < 0.3
+    out[0, 1, nq // 2] = True
+    L[torch.from_numpy(out).cuda()] = -INF
+    want = torch.zeros((2, 2, 500), device="cuda")
+    binding.fa_cache_weights(Q, K, L, want, 0.125, causal)
+    for bad in (NAN, INF):
+        Q[torch.from_numpy(out).cuda().transpose(1, 2)] = bad
+        W = torch.zeros_like(want)
+        binding.fa_cache_weights(Q, K, L, W, 0.125, causal)
+        assert want.isfinite().all() and torch.equal(W, want)
+
+
 @pytest.mark.parametrize("inv_t", [1e-42, 1e-30, 1e3, 1e6, 1e14, 1e16, 1e18, 1e20, 2.4e38, float(np.finfo(np.float32).max)])
 @pytest.mark.parametrize("q_type", [torch.float32, None])
 def test_verify_extreme_temperatures(inv_t, q_type):
