@@ -11,6 +11,7 @@
 // rows (wide) give each wavefront 32 rows, and the four share the tiles of K and V in LDS.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "fa_kernels.h"
@@ -485,10 +486,13 @@ PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int d) {
   };
   p.prefix_rows = all <= 32 ? 32 : 128;
   const long units = Hkv * up(all, p.prefix_rows);
-  // Half as many prefix items as compute units, or shares of 1024 keys where that makes more of them, up to one a unit (64 sequences, 32
-  // heads on 8 of 128, 8192 shared keys, 16 blocks of rows, us of the first launch at 6 / 8 / 12 / 16 shares: 45 / 40 / 43 / 43; 16 x 5 rows, 16
-  // heads of 64, 12345 keys, 16 blocks, at 6 / 12 / 16: 40 / 31 / 31)
-  const long most = clamp(up(128, units), clamp(Np / 1024, 1, up(256, units)), 16);
+  // Half as many prefix items as compute units, in 16 shares at most, or shares of 1024 keys where that makes more of them, up to one
+  // item a unit (64 sequences, 32 heads on 8 of 128, 8192 shared keys, 16 blocks of rows, us of the first launch at 6 / 8 / 12 / 16
+  // shares: 45 / 40 / 43 / 43; 16 x 5 rows, 16 heads of 64, 12345 keys, 16 blocks, at 6 / 12 / 16: 40 / 31 / 31. Few blocks of rows,
+  // the whole call with 16 shares and by the rule: one sequence, 4 heads on one of 128, 32768 and 65536 keys: 24.1 and 18.0, 42.7 and
+  // 23.8; 8 on 2: 25.5 and 20.0, 43.7 and 27.7; 32 sequences, 4 heads on one of 64: 32.7 and 26.2, 57.2 and 36.6; 8 sequences, 16 on 4
+  // of 128, 20480 and 32768 keys: 20.4 and 21.1, 26.7 and 25.0)
+  const long most = std::max(std::min(up(128, units), 16l), clamp(Np / 1024, 1, up(256, units)));
   cut(Np, most, 256, p.prefix_keys, p.prefix_shares);
   p.own_rows = own_rows <= 64 ? 32 : 128;
   // Own items: with those of the prefix no more than fit on the chip at once, two a compute unit (16 x 16
