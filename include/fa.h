@@ -609,7 +609,8 @@ int fa_cache_evict(void* Kcache, void* Vcache, const float* weights, const int32
  * everywhere), after all k from p_k: the lowest token whose running sum exceeds uniform[b, k] times the whole sum (else the last one
  * of weight above 0). A drafted token outside 0 .. V - 1 ends the drafts there and the next token is drawn from p_i. tokens
  * [B, k + 1]: the accepted ones, the drawn one (-1 where all weights are 0), then -1; accepted [B]: how many drafts were. Sums that
- * decide which token is drawn are float64. Logits of -inf are probabilities of 0. k >= 0 (k = 0: draft_tokens may be NULL, a
+ * decide which token is drawn are float64; of logits, a draft is accepted by a p whose normaliser is summed in float32 (good to about 1e-6
+ * of itself). Logits of -inf are probabilities of 0. k >= 0 (k = 0: draft_tokens may be NULL, a
  * draw from the target). Types: FA_TYPE_*. 1 <= V <= FA_VERIFY_MAX_VOCAB, strides >= V, inv_temperature > 0 and finite.
  * Pointers aligned to their elements; workspace (8-byte aligned) of fa_verify_drafts_workspace_bytes() bytes.
  */

@@ -4,8 +4,12 @@
 //   * prefix items: rows of ALL sequences against a share of the prefix. A row is a (token, head of the group) pair, packed
 //     token * G + head; K and V of the prefix are read once per block of rows, not once per sequence.
 //   * own items: the rows of one sequence against a share of its own cache.
-// One launch does the items of both kinds, since the first are bound by the matrix units and the second by HBM; each leaves a
-// normalised partial O and its logsumexp, and a second launch merges them.
+// One launch does the items of both kinds, since the first do many products with a key that they read and the second few: they ask
+// different things of a compute unit. (Neither is at its limit: 64 sequences on 8192 shared keys, up to 1024 own ones, read 4.3 TB/s
+// with the matrix units busy 12% of the launch; what is waited for is the longest share's chain of tiles.) Each leaves a normalised
+// partial O and its logsumexp in float32, and a second launch merges them. P is rounded to the element type for the second product, as
+// in every forward kernel here: O is then 1.3 to 1.4 times as far from the exact result as its own rounding alone would put it (bfloat16 0.0023
+// and 0.0017 of it).
 //
 // Items of up to 32 rows (narrow) have one row tile, and the four wavefronts of a workgroup divide the keys; items of up to 128
 // rows (wide) give each wavefront 32 rows, and the four share the tiles of K and V in LDS.
@@ -494,6 +498,10 @@ PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Nq, int Np, int Nk, int d) {
   // of 128, 20480 and 32768 keys: 20.4 and 21.1, 26.7 and 25.0)
   const long most = std::max(std::min(up(128, units), 16l), clamp(Np / 1024, 1, up(256, units)));
   cut(Np, most, 256, p.prefix_keys, p.prefix_shares);
+  // Up to 64 own rows are two narrow items: they read the keys twice, but divide them over four wavefronts each, where a wide one leaves
+  // two idle (us, narrow and wide: 16 sequences of up to 1024 keys, 5 x 8 rows a head, 4 heads of 64: 13.9 and 15.6; one of up to 8192, 8
+  // of 128: 18.9 and 25.9; 64 of 1024, 4 of 128, on 8192 shared: 70.4 and 72.3; but 16 of 2048, 8 of 128: 37.0 and 35.6; 32 of 2048, 9 x 4
+  // rows, 8 of 64: 43.5 and 42.3; 64 of 512, 16 x 4 rows, 4 of 128: 38.9 and 35.4)
   p.own_rows = own_rows <= 64 ? 32 : 128;
   // Own items: with those of the prefix no more than fit on the chip at once, two a compute unit (16 x 16
   // pairs of up to 2048 keys of 64, beside 192 items of the prefix, one and two shares: 31 and 36 us; 24 x 8 of up to 4096 of 128, beside

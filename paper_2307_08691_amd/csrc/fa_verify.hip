@@ -4,7 +4,8 @@
 //
 // A running sum over 100 000 probabilities passes a random number at another token if it is off by 1e-7, so everything that is
 // summed to draw is held in float64, whatever order it is summed in. The target's logits need their normaliser first: row maxima
-// and float32 sums over all rows settle which drafts are accepted; the one row that is drawn from is then summed once more in float64.
+// and float32 sums over all rows settle which drafts are accepted (one whose u q lies within 1e-6 of p may be taken the other way, which
+// changes its odds by as little); the one row that is drawn from is then summed once more in float64.
 //
 //   stats   (logits) maximum and sum of every row, in segments of kSegment tokens, one a wavefront: bound by HBM
 //   sums    per sequence: which drafts are accepted (every workgroup finds out for itself: cheaper than a launch); float64 sums of
@@ -188,12 +189,11 @@ __device__ __forceinline__ RowPart whole_row(const VerifyArgs& a, long row, RowP
   for (int i = 64 + lane; i < n; i += 64) take(part[i]);
   return {m, wave_add(z)};
 }
-// exp(inv_t (l - m)) in float64: with y = inv_t log2(e) (l - m), the difference first (the maximum's own weight is 1 whatever inv_t is; the
-// difference of two products would leave it 2^-53 of them, which counts from about 10^13 on), and n the whole number next to it (the low bits of y + 1.5 * 2^52),
-// 2^n times the polynomial of degree 8 that meets 2^f at the nine Chebyshev points of [-1/2, 1/2], f = y - n: off by at most 1.1e-12 of
+// exp(inv_t (l - m)) in float64: with y = inv_t log2(e) (l - m), the difference first (the maximum's own weight is then 1 whatever inv_t
+// is; the difference of two products would be off by 2^-53 of them, which counts from about 10^13 on), and n the whole number next to
+// it (the low bits of y + 1.5 * 2^52), 2^n times the polynomial of degree 8 that meets 2^f at the nine Chebyshev points of [-1/2, 1/2], f = y - n: off by at most 1.1e-12 of
 // its value, by which a draw over 10^5 tokens is decided otherwise once in some 10^6. n goes into the exponent's bits. Less than
-// 2^-1000 is 0. (64 rows of 131072: 19.6 us with a Taylor series of eleven
-// terms, rint and ldexp and reductions through LDS, 16.5 so.)
+// 2^-1000 is 0. (64 rows of 131072: 19.6 us with a Taylor series of eleven terms, rint and ldexp and reductions through LDS, 16.9 so.)
 struct Exponential {
   double c, m;
   __device__ __forceinline__ Exponential(float inv_t, float max)
@@ -278,8 +278,8 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_sums_kernel(VerifyArgs 
   const double inv = a.logits ? 1. / (double)r.sum : 1.;
   const Exponential weight(a.inv_t, r.max);
   double sp = 0., sa = 0., sq = 0.;
-  // A loop, though it is short: as straight code (10 KB of it) the wavefronts wait for instructions, which each of them runs once
-  // (us, straight and so: 9400 logits 13.0 and 7.3; 59 rows of 43057 16.9 and 12.5; 64 of 131072 19.4 and 19.3).
+  // A loop, though it is short: in straight code the wavefronts wait for instructions, which each of them runs once (us of this launch,
+  // unrolled and so: 5 rows of 9400 7.1 and 6.5; 59 x 3 of 43057 11.3 and 11.2; 64 x 5 of 131072 17.0 and 16.9).
   float l[8], d[8];
   auto request = [&](int piece) {
     const int j = c0 + (64 * piece + lane) * 8;

@@ -139,7 +139,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4
   }
 }
 
-// More rows, up to kStepRows, which lie in LDS: as above, the keys of a tile straight into registers.
+// More rows, up to kStepRows, which lie in LDS. The keys of a tile come straight into registers, a row a lane, which the kernel above
+// has left for whole rows through LDS: the rows take up to 68 KB of that here, and the other way has not been measured. 64 rows (G = 4) on
+// 16 x 8 caches of up to 4096 keys of 128: 30 us, of which reading the keys at 6.25 TB/s would take about 11.
 constexpr int kStepRows = 256;
 template <int D, bool F16>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void weights_rows_kernel(WeightsArgs a, int keys) {  // keys: of a workgroup, a multiple of 128
@@ -252,9 +254,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
 // More rows: a workgroup has 64 keys, which each of its four wavefronts holds in registers, and the rows stream past, head by head, in
 // tiles of 32 queries that the wavefronts take in turn: whole rows into a private piece of LDS, the next tile requested before the
 // current one is used. The keys are the columns here too: a lane's sums are two keys' (with the keys as rows, 32 sums a lane and a
-// transpose through LDS at the end, 2 prompts of 2048, 16 heads of 64, take 27.5 us instead of 23.7). Bound by the exponentials: 16
-// of the 24 cycles that a wavefront's 64 scores take. No barrier in the loop; under the causal rule rows above the keys are not
-// visited, and the blocks of keys with the most rows are handed out first.
+// transpose through LDS at the end, 2 prompts of 2048, 16 heads of 64, take 27.5 us instead of 23.7). Exponentials
+// are 16 of the 24 cycles that a wavefront's 64 scores take, but the vector unit is busy 44% of that launch only: under the causal rule
+// rows above the keys are not visited, a block of keys has from two to 64 row tiles there, and all blocks are resident at once, so that a
+// compute unit has what its four happen to have. The blocks with the most are handed out first. No barrier in the loop.
 constexpr int kPromptKeys = 64;
 template <int D, bool F16>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void weights_prompt_kernel(WeightsArgs a) {
