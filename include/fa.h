@@ -625,6 +625,77 @@ int fa_verify_drafts(const int32_t* draft_tokens, const void* draft_probs, const
                      float inv_temperature, void* stream);
 
 /*
+ * A key/value cache held in 4 or 8 bits. Blocks of 32 consecutive channels of a row share a scale byte e, which stands for 2^(e - 127)
+ * (255: all 32 are NaN); elements are E2M1 (bits = 4: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign; two a byte, the even channel in the low half) or E4M3
+ * (bits = 8, as in fa_fp8_fwd). Kcodes [B, Hkv, Nk, d * k_bits / 8] and Kscales [B, Hkv, Nk, d / 32] bytes, the same of V with v_bits (the two
+ * may differ); with a block_table (as fa_kvcache_fwd) pools of pages, [pages, Hkv, page_size, ..]: heads before slots, unlike the 16-bit
+ * caches. Codes 16-byte aligned, scales 4-byte. k_bits, v_bits in {4, 8} (FA_ERR_UNSUPPORTED otherwise).
+ *
+ * fa_qcache_append: new keys and values, quantised as they are written. Row i of Knew, Vnew goes to slot seqlens_k[b] - Nq + i of sequence
+ * b (seqlens_k counts the new keys already; nullptr: Nk); rows whose slot lies outside 0 .. Nk - 1 are dropped. With top the largest
+ * magnitude of a block's 32 values, the scale is the smallest power of two, 2^-111 at least, with top <= 1.75 * 2^2 of it (4 bits) or
+ * 1.75 * 2^8 (8 bits); every value over its scale is rounded to the nearest element, halves to the one with an even code, what lies
+ * above 6 to 6. (Exact but for that rounding, of half a step at most.) A block with an infinity or a NaN becomes NaN (codes 0, e = 255).
+ * Element (b, i, g, t) of Knew lies at b * k_batch_stride + i * k_token_stride + g * k_head_stride + t (elements, multiples of 8), of Vnew
+ * at v_*: both may be slices of a projection's output. Kout, Vout [B, Nq, Hkv, d] (or NULL) receive the values that the new slots now stand
+ * for, in the type of Knew: what attention within the new rows has to use to agree with later steps. Kout may be Knew and Vout Vnew,
+ * where those are dense. Dropped rows leave Kout, Vout as they were. A value within half a step of the type's range that rounds past it
+ * (to 2^16 in half precision, 2^128 in bfloat16) comes out as an infinity there, and in whatever reads it back in that type. type:
+ * FA_TYPE_BF16 or FA_TYPE_F16. d a multiple of 32 up to 256. B * Hkv * Nq * d at most 2^33.
+ */
+int fa_qcache_append(const void* Knew, const void* Vnew, void* Kcodes, void* Kscales, void* Vcodes, void* Vscales, void* Kout, void* Vout,
+                     const int32_t* seqlens_k, const int32_t* block_table, int B, int Hkv, int Nq, int Nk, int d, int k_bits, int v_bits,
+                     int page_size, int pages_per_seq, long long k_batch_stride, long long k_token_stride, long long k_head_stride,
+                     long long v_batch_stride, long long v_token_stride, long long v_head_stride, int type, void* stream);
+
+/*
+ * Slots of such a cache back in 16 bits (type: FA_TYPE_BF16 or FA_TYPE_F16; exact within the type's range).
+ *   cu_seqlens == nullptr: K, V [B, N, Hkv, d]; row i of sequence b is slot first[b] + i (first: DEVICE int32 [B], nullptr: 0).
+ *   cu_seqlens != nullptr: K, V [N, Hkv, d] packed; sequence b fills rows cu_seqlens[b] .. cu_seqlens[b + 1] - 1 from its slot 0 on (DEVICE
+ *     int32 [B + 1]; first must be nullptr, FA_ERR_SHAPE otherwise), which fa_varlen_cross_fwd can take as they are.
+ * Rows whose slot lies outside 0 .. seqlens_k[b] - 1 (nullptr: Nk), and packed rows past N, are left as they were. At most 2^30 rows a head in
+ * all (B * Hkv * min(N, Nk), rounded up to 64 rows each; FA_ERR_SHAPE beyond). Everything else as fa_qcache_append.
+ */
+int fa_qcache_read(const void* Kcodes, const void* Kscales, const void* Vcodes, const void* Vscales, void* K, void* V,
+                   const int32_t* seqlens_k, const int32_t* block_table, const int32_t* first, const int32_t* cu_seqlens, int B, int Hkv, int N,
+                   int Nk, int d, int k_bits, int v_bits, int page_size, int pages_per_seq, int type, void* stream);
+
+/*
+ * Forward against such a cache: fa_kvcache_fwd over the values that codes and scales stand for. Q, O [B, Nq, Hq, d], LSE [B, Hq, Nq],
+ * lengths, causal rule (query r at position r + seqlens_k[b] - Nq) and rows that see no key (O = 0, LSE = -inf) as there; any Nq. Keys and
+ * values that a query does not see do not touch its result, also where their blocks are NaN (e = 255); E4M3's own NaN codes, which
+ * fa_qcache_append never writes, have to lie in keys that all queries of the sequence see. NaN in a query, in a key that it sees or in
+ * that key's value reaches the row's result. d in {64, 128}; B * Nq * Hq at most 2^26, Hkv at most 2^16 (FA_ERR_SHAPE beyond). How the keys are cut
+ * over workgroups goes by the sizes alone, so results are the same bits in every run; `workspace` (partial results, float32; 16-byte
+ * aligned) needs fa_qcache_fwd_workspace_bytes() bytes, undefined on entry and return; where that is 0 it may be NULL. type: of Q and O, FA_TYPE_BF16
+ * or FA_TYPE_F16. Forward only, as fa_kvcache_fwd.
+ */
+size_t fa_qcache_fwd_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int d);
+int fa_qcache_fwd(const void* Q, const void* Kcodes, const void* Kscales, const void* Vcodes, const void* Vscales, const int32_t* seqlens_k,
+                  const int32_t* block_table, void* O, float* LSE, void* workspace, size_t workspace_bytes, int B, int Hq, int Hkv, int Nq,
+                  int Nk, int d, int k_bits, int v_bits, int page_size, int pages_per_seq, float scale, int causal, int type, void* stream);
+
+/*
+ * Rotary positions, of one axis (text) or several (rows and columns of images, time too for video). Pair i of a row's channels,
+ * i < pairs: channels i and i + pairs, or with `neighbours` 2 i and 2 i + 1, become
+ *     (x1 cos a - x2 sin a, x1 sin a + x2 cos a),  a = position[axis[i]] * inv_freq[i]
+ * and channels 2 * pairs .. d - 1 pass through. a is the exact product (reduced in float64), sine and cosine are good to float32, the rotation is
+ * float32. fa_rope_bwd is the gradient, the same with -a: it takes dQout, dKout and leaves dQ, dK.
+ * Q [B, N, Hq, d] -> Qout, and in the same launch K [B, N, Hkv, d] -> Kout (K NULL: Q alone; Hkv is ignored): element (b, i, h, t) at b *
+ * batch_stride + i * token_stride + h * head_stride + t, `strides` (HOST array, elements) holding those three of Q, Qout, K, Kout in turn.
+ * An output may be its input (the same strides). positions: DEVICE int32, axis x, sequence b, token i at positions[x * axis_stride + b * batch_stride + i];
+ * any values, negative ones too. inv_freq: DEVICE float32 [pairs], finite. axis: DEVICE int32 [pairs] (clamped into 0 .. axes - 1; nullptr: 0). type:
+ * FA_TYPE_*. Tensors aligned to their elements (16 bytes, with strides of as many, is fastest). d a multiple of 8 up to 256, 1 <= pairs,
+ * 2 * pairs <= d, 1 <= axes; B * N below 2^31, Hq + Hkv at most 2^20. Packed batches: B = 1, N the tokens of all sequences.
+ */
+int fa_rope_fwd(const void* Q, const void* K, void* Qout, void* Kout, const int32_t* positions, const float* inv_freq, const int32_t* axis,
+                int B, int N, int Hq, int Hkv, int d, int pairs, int axes, int neighbours, const long long* strides,
+                long long axis_stride, long long batch_stride, int type, void* stream);
+int fa_rope_bwd(const void* dQout, const void* dKout, void* dQ, void* dK, const int32_t* positions, const float* inv_freq, const int32_t* axis,
+                int B, int N, int Hq, int Hkv, int d, int pairs, int axes, int neighbours, const long long* strides,
+                long long axis_stride, long long batch_stride, int type, void* stream);
+
+/*
  * The packed ragged entry points (one and two lengths, with dropout, with a window), the split-key
  * forward, the key/value cache forward, the shared-prefix forward and the weights of cached keys for IEEE half precision (fp16) elements: each is its bfloat16 namesake with every
  * 16-bit tensor holding fp16, as fa_cross_fwd_f16 / fa_cross_bwd_f16 are to fa_cross_fwd /

@@ -10,7 +10,7 @@ import ctypes
 import importlib
 import os
 import warnings
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libfa_gfx950.so")
@@ -114,6 +114,12 @@ SIGNATURES = {
     "fa_verify_drafts_workspace_bytes": (_c_size_t, [_c_int] * 3),
     "fa_verify_drafts": (_c_int, [_c_void_p] * 6 + [_c_void_p, _c_size_t] + [_c_int] * 3 + [ctypes.c_longlong] * 2 + [_c_int] * 3 +
                          [_c_float, _c_void_p]),
+    "fa_qcache_append": (_c_int, [_c_void_p] * 10 + [_c_int] * 9 + [ctypes.c_longlong] * 6 + [_c_int, _c_void_p]),
+    "fa_qcache_read": (_c_int, [_c_void_p] * 10 + [_c_int] * 10 + [_c_void_p]),
+    "fa_qcache_fwd_workspace_bytes": (_c_size_t, [_c_int] * 6),
+    "fa_qcache_fwd": (_c_int, [_c_void_p] * 10 + [_c_size_t] + [_c_int] * 10 + [_c_float, _c_int, _c_int, _c_void_p]),
+    "fa_rope_fwd": (_c_int, [_c_void_p] * 7 + [_c_int] * 8 + [_c_void_p] + [ctypes.c_longlong] * 2 + [_c_int, _c_void_p]),
+    "fa_rope_bwd": (_c_int, [_c_void_p] * 7 + [_c_int] * 8 + [_c_void_p] + [ctypes.c_longlong] * 2 + [_c_int, _c_void_p]),
     "fa_mfma_probe_scratch_bytes": (_c_size_t, []),
     "fa_mfma_probe": (_c_int, [_c_int, _c_int, _c_void_p, _c_void_p]),
 }
@@ -412,6 +418,37 @@ def fa_verify_drafts_raw(draft_tokens, draft_probs, target, uniform, tokens, acc
                          target_stride, draft_type, target_type, logits, inv_temperature, stream=0) -> int:
     return load().fa_verify_drafts(draft_tokens, draft_probs, target, uniform, tokens, accepted, ws, ws_bytes, B, k, V, draft_stride,
                                    target_stride, draft_type, target_type, int(logits), inv_temperature, stream)
+
+
+def fa_qcache_append_raw(Knew, Vnew, Kcodes, Kscales, Vcodes, Vscales, Kout, Vout, seqlens_k, block_table, B, Hkv, Nq, Nk, d, k_bits, v_bits,
+                         page_size, pages_per_seq, k_strides, v_strides, type, stream=0) -> int:
+    return load().fa_qcache_append(Knew, Vnew, Kcodes, Kscales, Vcodes, Vscales, Kout, Vout, seqlens_k, block_table, B, Hkv, Nq, Nk, d,
+                                   k_bits, v_bits, page_size, pages_per_seq, *k_strides, *v_strides, type, stream)
+
+
+def fa_qcache_read_raw(Kcodes, Kscales, Vcodes, Vscales, K, V, seqlens_k, block_table, first, cu_seqlens, B, Hkv, N, Nk, d, k_bits, v_bits,
+                       page_size, pages_per_seq, type, stream=0) -> int:
+    return load().fa_qcache_read(Kcodes, Kscales, Vcodes, Vscales, K, V, seqlens_k, block_table, first, cu_seqlens, B, Hkv, N, Nk, d,
+                                 k_bits, v_bits, page_size, pages_per_seq, type, stream)
+
+
+def fa_qcache_fwd_workspace_bytes(B, Hq, Hkv, Nq, Nk, d) -> int:
+    return load().fa_qcache_fwd_workspace_bytes(B, Hq, Hkv, Nq, Nk, d)
+
+
+def fa_qcache_fwd_raw(Q, Kcodes, Kscales, Vcodes, Vscales, seqlens_k, block_table, O, LSE, ws, ws_bytes, B, Hq, Hkv, Nq, Nk, d, k_bits,
+                      v_bits, page_size, pages_per_seq, scale, causal, type, stream=0) -> int:
+    return load().fa_qcache_fwd(Q, Kcodes, Kscales, Vcodes, Vscales, seqlens_k, block_table, O, LSE, ws, ws_bytes, B, Hq, Hkv, Nq, Nk, d,
+                                k_bits, v_bits, page_size, pages_per_seq, scale, int(causal), type, stream)
+
+
+def fa_rope_raw(inverse, Q, K, Qout, Kout, positions, inv_freq, axis, B, N, Hq, Hkv, d, pairs, axes, neighbours, strides, axis_stride,
+                batch_stride, type, stream=0) -> int:
+    """fa_rope_fwd, or with `inverse` fa_rope_bwd; strides: twelve numbers (None: NULL)"""
+    fn = load().fa_rope_bwd if inverse else load().fa_rope_fwd
+    held = (ctypes.c_longlong * 12)(*strides) if strides is not None else None
+    return fn(Q, K, Qout, Kout, positions, inv_freq, axis, B, N, Hq, Hkv, d, pairs, axes, int(neighbours), held, axis_stride, batch_stride,
+              type, stream)
 
 
 def fa_mfma_probe_scratch_bytes() -> int:
@@ -1300,6 +1337,246 @@ def fa_verify_drafts(draft_tokens, draft_probs, target, uniform, logits: bool = 
                                 _wsbytes(ws), B, k, V, draft_stride, target_stride, draft_type, target_type, logits, inv_temperature,
                                 _stream()))
     return tokens, accepted
+
+
+# ---- caches held in 4 or 8 bits
+
+class QCache(NamedTuple):
+    """Keys and values in 4 or 8 bits: codes uint8 [B,Hkv,Nk,d*bits/8] (4 bits: two a byte, the even channel in the low half) and scales
+    uint8 [B,Hkv,Nk,d/32], or pools of pages [pages,Hkv,page_size,..]. Any four such tensors will do."""
+    Kcodes: "torch.Tensor"
+    Kscales: "torch.Tensor"
+    Vcodes: "torch.Tensor"
+    Vscales: "torch.Tensor"
+
+
+def qcache(n: int, Hkv: int, slots: int, d: int, k_bits: int = 4, v_bits: int = 4, device="cuda") -> QCache:
+    """An empty cache of n sequences with `slots` slots each, or of n pages of `slots` (page_size)."""
+    import torch
+    if k_bits not in (4, 8) or v_bits not in (4, 8) or d % 32:
+        raise ValueError("a cache holds 4 or 8 bits an element, in blocks of 32 channels")
+    return QCache(*(torch.zeros((n, Hkv, slots, w), dtype=torch.uint8, device=device)
+                    for w in (d * k_bits // 8, d // 32, d * v_bits // 8, d // 32)))
+
+
+def _current(dev) -> None:
+    """The calls go to the current device's stream."""
+    import torch
+    if dev.type == "cuda" and dev.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {dev}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _qcache(cache, B, Nk, table, dev):
+    """The four tensors of a cache -> their dimensions: x.Hkv, x.d, x.Nk, x.page, x.pages, x.k_bits, x.v_bits. Nk (0: all there are) says how many
+    slots are meant."""
+    import torch
+    if len(cache) != 4:
+        raise ValueError("a cache is (Kcodes, Kscales, Vcodes, Vscales)")
+    Kc, Ks, Vc, Vs = cache
+    x = _Dims()
+    if Kc.dim() != 4 or Ks.dim() != 4:
+        raise ValueError("codes and scales must be [B, Hkv, Nk, bytes] or [pages, Hkv, page_size, bytes]")
+    x.d = 32 * Ks.shape[3]
+    lead = tuple(Kc.shape[:3])
+    bits = {x.d // 2: 4, x.d: 8}
+    for t, nm in ((Kc, "Kcodes"), (Vc, "Vcodes")):
+        if t.shape[-1] not in bits:
+            raise ValueError(f"{nm} must hold 4 or 8 bits for each of the scales' {x.d} channels")
+        _need(t, nm, torch.uint8, (*lead, t.shape[-1]), dev)
+    for t, nm in ((Ks, "Kscales"), (Vs, "Vscales")):
+        _need(t, nm, torch.uint8, (*lead, x.d // 32), dev)
+    x.Hkv, x.k_bits, x.v_bits = lead[1], bits[Kc.shape[3]], bits[Vc.shape[3]]
+    if table is None:
+        if lead[0] != B:
+            raise ValueError("a cache without a block_table must be of [B, Hkv, Nk, ..]")
+        if Nk not in (0, lead[2]):
+            raise ValueError(f"the slots of a contiguous cache are its {lead[2]} rows a sequence, not {Nk}")
+        x.Nk, x.page, x.pages = lead[2], 0, 0
+        return x
+    _need(table, "block_table", torch.int32, None, dev)
+    if table.dim() != 2 or table.shape[0] != B:
+        raise ValueError("block_table must be [B, pages_per_seq]")
+    x.page, x.pages = lead[2], table.shape[1]
+    if not 0 <= Nk <= x.page * x.pages:
+        raise ValueError(f"the pages of block_table hold {x.page * x.pages} slots a sequence, not {Nk}")
+    x.Nk = Nk or x.page * x.pages
+    return x
+
+
+def _type16(t, name):
+    import torch
+    if t.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"{name} must be bfloat16 or float16")
+    return FA_TYPE_BF16 if t.dtype == torch.bfloat16 else FA_TYPE_F16
+
+
+def _row_strides(t, name, shape, dtype, dev, unit):
+    """Strides of a tensor [B, N, H, d] whose rows are dense and lie a multiple of `unit` elements apart."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != dev:
+        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)} on {dev}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    # (a dimension of one has no say)
+    s = [0 if n == 1 else v for n, v in zip(t.shape[:3], t.stride()[:3])]
+    if t.stride(3) != 1 and t.shape[3] > 1 or any(v % unit for v in s) or any(v < 0 for v in s):
+        raise ValueError(f"the rows of {name} must be dense, and lie a multiple of {unit} elements apart")
+    return s
+
+
+def fa_qcache_append(Knew, Vnew, cache, seqlens_k=None, block_table=None, max_seqlen_k: int = 0, Kout=None, Vout=None):
+    """New keys and values Knew, Vnew [B,Nq,Hkv,d] (bf16 or fp16; slices of a projection's output will do) quantised into the slots
+    seqlens_k[b] - Nq .. of every sequence's cache (a QCache; slabs, or pages with block_table [B,pages_per_seq]; seqlens_k int32 [B] counts
+    the new keys already; max_seqlen_k bounds the slots of paged sequences). Kout, Vout [B,Nq,Hkv,d], where given, receive the values that the new
+    slots stand for; they may be Knew, Vnew. Returns the cache."""
+    if _host and _host.qcache_append(Knew, Vnew, cache, seqlens_k, block_table, max_seqlen_k, Kout, Vout):
+        return cache
+    import torch
+    type = _type16(Knew, "Knew")
+    if Knew.dim() != 4:
+        raise ValueError("Knew must be [B, Nq, Hkv, d]")
+    shape, dev = tuple(Knew.shape), Knew.device
+    B, Nq, Hkv, d = shape
+    x = _qcache(cache, B, max_seqlen_k, block_table, dev)
+    if (x.Hkv, x.d) != (Hkv, d):
+        raise ValueError(f"the cache holds {x.Hkv} heads of {x.d}, Knew {Hkv} of {d}")
+    ks, vs = (_row_strides(t, nm, shape, Knew.dtype, dev, 8) for t, nm in ((Knew, "Knew"), (Vnew, "Vnew")))
+    for t, nm in ((Kout, "Kout"), (Vout, "Vout")):
+        if t is not None:
+            _need(t, nm, Knew.dtype, shape, dev)
+    if seqlens_k is not None:
+        _need(seqlens_k, "seqlens_k", torch.int32, (B,), dev)
+    _current(dev)
+    _check(fa_qcache_append_raw(_ptr(Knew), _ptr(Vnew), *map(_ptr, cache), _ptr(Kout), _ptr(Vout), _ptr(seqlens_k), _ptr(block_table), B, Hkv,
+                                Nq, x.Nk, d, x.k_bits, x.v_bits, x.page, x.pages, ks, vs, type, _stream()))
+    return cache
+
+
+def fa_qcache_read(cache, K, V, seqlens_k=None, block_table=None, max_seqlen_k: int = 0, first=None, cu_seqlens=None):
+    """Slots of a cache (fa_qcache_append) back in 16 bits, into K, V (bf16 or fp16): [B,N,Hkv,d], row i of sequence b being slot first[b] + i
+    (int32 [B]; None: 0), or with cu_seqlens (int32 [B+1]) packed [T,Hkv,d], sequence b from its slot 0 on. Rows past a sequence's length are left
+    as they were. Returns K, V."""
+    if _host and _host.qcache_read(cache, K, V, seqlens_k, block_table, max_seqlen_k, first, cu_seqlens):
+        return K, V
+    import torch
+    type = _type16(K, "K")
+    dev = K.device
+    if cu_seqlens is None:
+        if K.dim() != 4:
+            raise ValueError("K must be [B, N, Hkv, d], or [T, Hkv, d] with cu_seqlens")
+        B = K.shape[0]
+    else:
+        if first is not None:
+            raise ValueError("packed rows begin at slot 0: first and cu_seqlens exclude each other")
+        if K.dim() != 3 or cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
+            raise ValueError("with cu_seqlens [B + 1] K must be [T, Hkv, d]")
+        B = cu_seqlens.numel() - 1
+        _need(cu_seqlens, "cu_seqlens", torch.int32, None, dev)
+    x = _qcache(cache, B, max_seqlen_k, block_table, dev)
+    if tuple(K.shape[-2:]) != (x.Hkv, x.d):
+        raise ValueError(f"the cache holds {x.Hkv} heads of {x.d}, K is {tuple(K.shape)}")
+    _need(K, "K", K.dtype)
+    _need(V, "V", K.dtype, tuple(K.shape), dev)
+    for t, nm in ((seqlens_k, "seqlens_k"), (first, "first")):
+        if t is not None:
+            _need(t, nm, torch.int32, (B,), dev)
+    _current(dev)
+    _check(fa_qcache_read_raw(*map(_ptr, cache), _ptr(K), _ptr(V), _ptr(seqlens_k), _ptr(block_table), _ptr(first), _ptr(cu_seqlens), B, x.Hkv,
+                              K.shape[-3], x.Nk, x.d, x.k_bits, x.v_bits, x.page, x.pages, type, _stream()))
+    return K, V
+
+
+def fa_qcache_fwd(Q, cache, scale: float, causal: bool, seqlens_k=None, block_table=None, max_seqlen_k: int = 0, O=None, LSE=None,
+                  workspace=None):
+    """fa_kvcache_fwd against a cache held in 4 or 8 bits (a QCache): Nq new queries per sequence, Q [B,Nq,Hq,d] bf16 or fp16, attend to the first
+    seqlens_k[b] keys. Returns O [B,Nq,Hq,d] of that type and LSE [B,Hq,Nq] fp32."""
+    if _host and O is None and LSE is None and workspace is None:
+        r = _host.qcache_fwd(Q, cache, scale, causal, seqlens_k, block_table, max_seqlen_k)
+        if r is not None:
+            return r
+    import torch
+    type = _type16(Q, "Q")
+    _need(Q, "Q")
+    if Q.dim() != 4:
+        raise ValueError("Q must be [B, Nq, Hq, d]")
+    B, Nq, Hq, d = Q.shape
+    dev = Q.device
+    x = _qcache(cache, B, max_seqlen_k, block_table, dev)
+    if x.d != d:
+        raise ValueError("the cache must have the head dimension of Q")
+    if seqlens_k is not None:
+        _need(seqlens_k, "seqlens_k", torch.int32, (B,), dev)
+    _current(dev)
+    O = _out(O, "O", (B, Nq, Hq, d), Q.dtype, dev)
+    LSE = _out(LSE, "LSE", (B, Hq, Nq), torch.float32, dev)
+    ws = _workspace(workspace, fa_qcache_fwd_workspace_bytes(B, Hq, x.Hkv, Nq, x.Nk, d), dev)
+    _check(fa_qcache_fwd_raw(_ptr(Q), *map(_ptr, cache), _ptr(seqlens_k), _ptr(block_table), _ptr(O), _ptr(LSE), _ptr(ws), _wsbytes(ws), B, Hq,
+                             x.Hkv, Nq, x.Nk, d, x.k_bits, x.v_bits, x.page, x.pages, scale, causal, type, _stream()))
+    return O, LSE
+
+
+# ---- rotary positions
+
+def _rope(inverse, Q, K, positions, inv_freq, axis, neighbours, Qout, Kout):
+    if _host and Qout is None and Kout is None:
+        r = _host.rope(inverse, Q, K, positions, inv_freq, axis, neighbours)
+        if r is not None:
+            return r
+    import torch
+    types = {torch.float32: FA_TYPE_F32, torch.bfloat16: FA_TYPE_BF16, torch.float16: FA_TYPE_F16}
+    if Q.dtype not in types:
+        raise ValueError("Q must be float32, bfloat16 or float16")
+    packed = Q.dim() == 3
+    if not packed and Q.dim() != 4:
+        raise ValueError("Q must be [B, N, Hq, d] or packed [T, Hq, d]")
+    dev, lead = Q.device, tuple(Q.shape[:-2])
+    if K is not None and (K.dim() != Q.dim() or tuple(K.shape[:-2]) != lead or K.shape[-1] != Q.shape[-1]):
+        raise ValueError("K must be [B, N, Hkv, d] with the B, N and d of Q")
+    if positions.dim() == len(lead):
+        positions = positions[None]
+    if positions.dtype != torch.int32 or tuple(positions.shape[1:]) != lead or positions.dim() != len(lead) + 1 or positions.device != dev:
+        raise ValueError(f"positions must be int32 of [axes, {', '.join(map(str, lead))}] on the device of Q")
+    if positions.shape[-1] > 1 and positions.stride(-1) != 1 or min(positions.stride()) < 0:
+        raise ValueError("the positions of a sequence must be dense")
+    _need(inv_freq, "inv_freq", torch.float32, None, dev)
+    pairs = inv_freq.numel()
+    if inv_freq.dim() != 1 or not 1 <= pairs <= Q.shape[-1] // 2:
+        raise ValueError("inv_freq must have one value for each pair of channels, half of d at most")
+    if axis is not None:
+        _need(axis, "axis", torch.int32, (pairs,), dev)
+    outs, strides = [], []
+    for x, y, nm in ((Q, Qout, "Q"), (K, Kout, "K")):
+        if x is None:
+            if y is not None:
+                raise ValueError("Kout without K")
+            outs.append(None)
+            strides += [0] * 6
+            continue
+        y = torch.empty(x.shape, dtype=x.dtype, device=dev) if y is None else y
+        outs.append(y)
+        for t, n in ((x, nm), (y, nm + "out")):
+            full = t[None] if packed else t
+            own = _row_strides(full, n, (1, *x.shape) if packed else x.shape, Q.dtype, dev, 1)
+            if t is y and any(v == 0 and size > 1 for v, size in zip(own, full.shape)):
+                raise ValueError(f"the rows of {n} must be places of their own")
+            strides += own
+    _current(dev)
+    B, N = (1, lead[0]) if packed else lead
+    pb = 0 if packed or positions.shape[1] == 1 else positions.stride(1)
+    _check(fa_rope_raw(inverse, _ptr(Q), _ptr(K), _ptr(outs[0]), _ptr(outs[1]), _ptr(positions), _ptr(inv_freq), _ptr(axis), B, N, Q.shape[-2],
+                       K.shape[-2] if K is not None else 0, Q.shape[-1], pairs, positions.shape[0], neighbours, strides,
+                       0 if positions.shape[0] == 1 else positions.stride(0), pb, types[Q.dtype], _stream()))
+    return outs[0], outs[1]
+
+
+def fa_rope_fwd(Q, K, positions, inv_freq, axis=None, neighbours: bool = False, Qout=None, Kout=None):
+    """Rotate queries Q [B,N,Hq,d] and keys K [B,N,Hkv,d] (None: Q alone), or packed [T,H,d], bf16, fp16 or fp32, by their positions: int32
+    [axes,B,N] ([axes,T]; one axis: [B,N]). Pair i of a row's channels (i and i + pairs; neighbours=True: 2i and 2i + 1) turns by
+    positions[axis[i]] * inv_freq[i]: inv_freq fp32 [pairs], axis int32 [pairs] (None: axis 0). Channels past the pairs pass through. Inputs
+    may be slices of a projection's output; an output may be its input. Returns Qout, Kout (contiguous unless given)."""
+    return _rope(False, Q, K, positions, inv_freq, axis, neighbours, Qout, Kout)
+
+
+def fa_rope_bwd(dQout, dKout, positions, inv_freq, axis=None, neighbours: bool = False, dQ=None, dK=None):
+    """The gradient of fa_rope_fwd: rotation by the opposite angles. Returns dQ, dK."""
+    return _rope(True, dQout, dKout, positions, inv_freq, axis, neighbours, dQ, dK)
 
 
 def fa_mfma_probe(iters: int, random_operands: bool):

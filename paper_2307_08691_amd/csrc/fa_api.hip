@@ -1250,6 +1250,183 @@ int fa_verify_drafts(const int32_t* draft_tokens, const void* draft_probs, const
   return launched(fa::launch_verify(a, (hipStream_t)stream));
 }
 
+// ---- caches held in 4 or 8 bits, rotary positions
+
+static int set_qcache(fa::QCacheView& c, const void* Kc, const void* Ks, const void* Vc, const void* Vs, const int32_t* lens, const int32_t* table,
+                      int B, int Hkv, int Nk, int d, int k_bits, int v_bits, int page_size, int pages_per_seq) {
+  if ((k_bits != 4 && k_bits != 8) || (v_bits != 4 && v_bits != 8)) return FA_ERR_UNSUPPORTED;
+  if (int e = set_cache(c.c, lens, table, B, Hkv, Nk, d, page_size, pages_per_seq)) return e;
+  if (!aligned16(Kc) || !aligned16(Vc) || !aligned4(Ks) || !aligned4(Vs)) return FA_ERR_ALIGN;
+  c.Kc = (uint8_t*)Kc;
+  c.Ks = (uint8_t*)Ks;
+  c.Vc = (uint8_t*)Vc;
+  c.Vs = (uint8_t*)Vs;
+  c.k_bits = k_bits;
+  c.v_bits = v_bits;
+  return FA_OK;
+}
+static int check_blocks(int d) { return d <= 0 ? FA_ERR_SHAPE : (d % 32 || d > 256 ? FA_ERR_UNSUPPORTED : FA_OK); }
+static int check_16bit(int type) { return type == FA_TYPE_BF16 || type == FA_TYPE_F16 ? FA_OK : FA_ERR_UNSUPPORTED; }
+
+int fa_qcache_append(const void* Knew, const void* Vnew, void* Kcodes, void* Kscales, void* Vcodes, void* Vscales, void* Kout, void* Vout,
+                     const int32_t* seqlens_k, const int32_t* block_table, int B, int Hkv, int Nq, int Nk, int d, int k_bits, int v_bits,
+                     int page_size, int pages_per_seq, long long k_batch_stride, long long k_token_stride, long long k_head_stride,
+                     long long v_batch_stride, long long v_token_stride, long long v_head_stride, int type, void* stream) {
+  if (!Knew || !Vnew || !Kcodes || !Kscales || !Vcodes || !Vscales) return FA_ERR_NULL;
+  if (Nq <= 0) return FA_ERR_SHAPE;
+  if (int e = check_blocks(d)) return e;
+  if (int e = check_16bit(type)) return e;
+  fa::QAppendArgs a;
+  if (int e = set_qcache(a.c, Kcodes, Kscales, Vcodes, Vscales, seqlens_k, block_table, B, Hkv, Nk, d, k_bits, v_bits, page_size, pages_per_seq))
+    return e;
+  if ((double)B * Nq * Hkv * (d / 8) > (double)(1u << 30)) return FA_ERR_SHAPE;
+  for (long long x : {k_batch_stride, k_token_stride, k_head_stride, v_batch_stride, v_token_stride, v_head_stride})
+    if (x < 0 || x % 8) return FA_ERR_SHAPE;
+  if (!aligned16(Knew) || !aligned16(Vnew) || !aligned16(Kout) || !aligned16(Vout)) return FA_ERR_ALIGN;
+  a.Kn = (const __bf16*)Knew;
+  a.Vn = (const __bf16*)Vnew;
+  a.Kout = (__bf16*)Kout;
+  a.Vout = (__bf16*)Vout;
+  a.k_bs = (long)k_batch_stride;
+  a.k_ts = (long)k_token_stride;
+  a.k_hs = (long)k_head_stride;
+  a.v_bs = (long)v_batch_stride;
+  a.v_ts = (long)v_token_stride;
+  a.v_hs = (long)v_head_stride;
+  a.nseq = B;
+  a.Nq = Nq;
+  a.f16 = type == FA_TYPE_F16;
+  return launched(fa::launch_qappend(a, (hipStream_t)stream));
+}
+
+int fa_qcache_read(const void* Kcodes, const void* Kscales, const void* Vcodes, const void* Vscales, void* K, void* V,
+                   const int32_t* seqlens_k, const int32_t* block_table, const int32_t* first, const int32_t* cu_seqlens, int B, int Hkv, int N,
+                   int Nk, int d, int k_bits, int v_bits, int page_size, int pages_per_seq, int type, void* stream) {
+  if (!Kcodes || !Kscales || !Vcodes || !Vscales || !K || !V) return FA_ERR_NULL;
+  if (N <= 0 || (first && cu_seqlens)) return FA_ERR_SHAPE;
+  if (int e = check_blocks(d)) return e;
+  if (int e = check_16bit(type)) return e;
+  fa::QReadArgs a;
+  if (int e = set_qcache(a.c, Kcodes, Kscales, Vcodes, Vscales, seqlens_k, block_table, B, Hkv, Nk, d, k_bits, v_bits, page_size, pages_per_seq))
+    return e;
+  const long rows = cu_seqlens && Nk < N ? Nk : N;  // (of one sequence, at most)
+  if ((double)B * Hkv * ((rows + 63) / 64) >= (double)(1u << 24)) return FA_ERR_SHAPE;  // (threads of a grid are counted in 32 bits)
+  if (!aligned16(K) || !aligned16(V) || !aligned4(first) || !aligned4(cu_seqlens)) return FA_ERR_ALIGN;
+  a.K = (__bf16*)K;
+  a.V = (__bf16*)V;
+  a.first = first;
+  a.cu = cu_seqlens;
+  a.nseq = B;
+  a.N = N;
+  a.total = N;
+  a.f16 = type == FA_TYPE_F16;
+  return launched(fa::launch_qread(a, (hipStream_t)stream));
+}
+
+static bool qcache_fwd_sizes(int B, int Hq, int Hkv, int Nq, int Nk) {
+  return B > 0 && Hq > 0 && Hkv > 0 && Hq % Hkv == 0 && Nq > 0 && Nk > 0 && Nk <= FA_CACHE_MAX_SLOTS && Hkv <= (1 << 16) &&
+         (double)B * Nq * Hq <= (1 << 26);
+}
+
+size_t fa_qcache_fwd_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int d) {
+  if (!qcache_fwd_sizes(B, Hq, Hkv, Nq, Nk) || (d != 64 && d != 128)) return 0;
+  const fa::QAttendPlan p = fa::qattend_plan(B, Hq, Hkv, Nq, Nk, d);
+  return p.shares == 1 ? 0 : round_up((size_t)p.shares * B * Nq * Hq * (d + 1) * sizeof(float), 256);
+}
+
+int fa_qcache_fwd(const void* Q, const void* Kcodes, const void* Kscales, const void* Vcodes, const void* Vscales, const int32_t* seqlens_k,
+                  const int32_t* block_table, void* O, float* LSE, void* workspace, size_t workspace_bytes, int B, int Hq, int Hkv, int Nq,
+                  int Nk, int d, int k_bits, int v_bits, int page_size, int pages_per_seq, float scale, int causal, int type, void* stream) {
+  if (!Q || !Kcodes || !Kscales || !Vcodes || !Vscales || !O || !LSE) return FA_ERR_NULL;
+  if (int e = check_common(Hq, Hkv, d, scale, false)) return e;
+  if (!qcache_fwd_sizes(B, Hq, Hkv, Nq, Nk)) return FA_ERR_SHAPE;
+  if (int e = check_16bit(type)) return e;
+  fa::QAttendArgs a;
+  if (int e = set_qcache(a.c, Kcodes, Kscales, Vcodes, Vscales, seqlens_k, block_table, B, Hkv, Nk, d, k_bits, v_bits, page_size, pages_per_seq))
+    return e;
+  if (!aligned16(Q) || !aligned16(O) || !aligned4(LSE) || !aligned16(workspace)) return FA_ERR_ALIGN;
+  const size_t need = fa_qcache_fwd_workspace_bytes(B, Hq, Hkv, Nq, Nk, d);
+  if (need && !workspace) return FA_ERR_NULL;
+  if (workspace_bytes < need) return FA_ERR_WORKSPACE;
+  const fa::QAttendPlan p = fa::qattend_plan(B, Hq, Hkv, Nq, Nk, d);
+  a.Q = (const __bf16*)Q;
+  a.O = (__bf16*)O;
+  a.LSE = LSE;
+  a.Opart = (float*)workspace;
+  a.Lpart = a.Opart + (p.shares == 1 ? 0 : (size_t)p.shares * B * Nq * Hq * d);
+  a.nseq = B;
+  a.Nq = Nq;
+  a.Hq = Hq;
+  a.G = Hq / Hkv;
+  a.f16 = type == FA_TYPE_F16;
+  a.causal = causal != 0;
+  a.scale = scale;
+  a.scale_log2e = scale * fa::kLog2e;
+  return launched(fa::launch_qattend(a, (hipStream_t)stream));
+}
+
+static int rope_any(int inverse, const void* Q, const void* K, void* Qout, void* Kout, const int32_t* positions, const float* inv_freq,
+                    const int32_t* axis, int B, int N, int Hq, int Hkv, int d, int pairs, int axes, int neighbours, const long long* strides,
+                    long long axis_stride, long long batch_stride, int type, void* stream) {
+  if (!Q || !Qout || !positions || !inv_freq || !strides || (K && !Kout)) return FA_ERR_NULL;
+  if (type < FA_TYPE_F32 || type > FA_TYPE_F16) return FA_ERR_UNSUPPORTED;
+  if (d <= 0) return FA_ERR_SHAPE;
+  if (d % 8 || d > 256) return FA_ERR_UNSUPPORTED;
+  if (B <= 0 || N <= 0 || (double)B * N > (double)0x7fffffff || Hq <= 0 || (K && Hkv <= 0) || (long)Hq + (K ? Hkv : 0) > (1 << 20) || pairs <= 0 ||
+      2 * (long)pairs > d || axes <= 0 || axis_stride < 0 || batch_stride < 0)
+    return FA_ERR_SHAPE;
+  const int size = type == FA_TYPE_F32 ? 4 : 2;
+  const void* at[4] = {Q, Qout, K, Kout};
+  // as many elements at once as divide the pairs, the strides and the addresses, 16 bytes at most
+  int vec = 16 / size;
+  while (pairs % vec) vec /= 2;
+  for (int i = 0; i < (K ? 4 : 2); ++i) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(at[i]);
+    if (p % size) return FA_ERR_ALIGN;
+    while (p % (vec * size)) vec /= 2;
+    for (int j = 0; j < 3; ++j) {
+      if (strides[3 * i + j] < 0) return FA_ERR_SHAPE;
+      while (strides[3 * i + j] % vec) vec /= 2;
+    }
+  }
+  if (!aligned4(positions) || !aligned4(inv_freq) || !aligned4(axis)) return FA_ERR_ALIGN;
+  fa::RopeArgs a;
+  for (int i = 0; i < 2; ++i) {
+    const long long* s = strides + 6 * i;
+    if (i && !K) a.t[i] = {nullptr, nullptr, 0, 0, 0, 0, 0, 0, 0};
+    else a.t[i] = {at[2 * i], (void*)at[2 * i + 1], i ? Hkv : Hq, (long)s[0], (long)s[1], (long)s[2], (long)s[3], (long)s[4], (long)s[5]};
+  }
+  a.positions = positions;
+  a.inv_freq = inv_freq;
+  a.axis = axis;
+  a.p_as = (long)axis_stride;
+  a.p_bs = (long)batch_stride;
+  a.nseq = B;
+  a.N = N;
+  a.d = d;
+  a.pairs = pairs;
+  a.axes = axes;
+  a.type = type;
+  a.neighbours = neighbours != 0;
+  a.inverse = inverse;
+  a.vec = vec;
+  return launched(fa::launch_rope(a, (hipStream_t)stream));
+}
+
+int fa_rope_fwd(const void* Q, const void* K, void* Qout, void* Kout, const int32_t* positions, const float* inv_freq, const int32_t* axis,
+                int B, int N, int Hq, int Hkv, int d, int pairs, int axes, int neighbours, const long long* strides,
+                long long axis_stride, long long batch_stride, int type, void* stream) {
+  return rope_any(0, Q, K, Qout, Kout, positions, inv_freq, axis, B, N, Hq, Hkv, d, pairs, axes, neighbours, strides, axis_stride,
+                  batch_stride, type, stream);
+}
+
+int fa_rope_bwd(const void* dQout, const void* dKout, void* dQ, void* dK, const int32_t* positions, const float* inv_freq, const int32_t* axis,
+                int B, int N, int Hq, int Hkv, int d, int pairs, int axes, int neighbours, const long long* strides,
+                long long axis_stride, long long batch_stride, int type, void* stream) {
+  return rope_any(1, dQout, dKout, dQ, dK, positions, inv_freq, axis, B, N, Hq, Hkv, d, pairs, axes, neighbours, strides, axis_stride,
+                  batch_stride, type, stream);
+}
+
 size_t fa_mfma_probe_scratch_bytes(void) { return 16 + (size_t)256 * 512 * sizeof(float); }
 
 int fa_mfma_probe(int iters, int random_operands, void* scratch, void* stream) {

@@ -34,7 +34,8 @@ namespace {
   X(fa_varlen_bwd) X(fa_varlen_bwd_f16) X(fa_varlen_bwd_workspace_bytes) X(fa_kvcache_fwd) X(fa_kvcache_fwd_f16)        \
   X(fa_splitkv_fwd_workspace_bytes) X(fa_prefix_fwd) X(fa_prefix_fwd_f16) X(fa_prefix_fwd_workspace_bytes) X(fa_cache_append)      \
   X(fa_cache_weights) X(fa_cache_weights_f16) X(fa_cache_evict) X(fa_cache_evict_workspace_bytes) X(fa_verify_drafts)             \
-  X(fa_verify_drafts_workspace_bytes)
+  X(fa_verify_drafts_workspace_bytes) X(fa_qcache_append) X(fa_qcache_read) X(fa_qcache_fwd) X(fa_qcache_fwd_workspace_bytes)      \
+  X(fa_rope_fwd) X(fa_rope_bwd)
 struct Entries {
 #define X(name) decltype(&::name) name;
   FA_HOST_ENTRIES(X)
@@ -591,6 +592,231 @@ PyObject* verify_drafts(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- caches held in 4 or 8 bits, rotary positions
+
+// (for these the tensors' device has to be the current one)
+bool current_stream_of(c10::Device dev, void*& st) {
+  PyObject* d = PyObject_CallNoArgs(get_device);
+  if (!d) return false;
+  const long index = PyLong_AsLong(d);
+  PyObject* s = PyObject_CallOneArg(get_stream, d);
+  Py_DECREF(d);
+  if (!s) return false;
+  st = index == dev.index() ? PyLong_AsVoidPtr(s) : nullptr;
+  Py_DECREF(s);
+  if (PyErr_Occurred()) return false;
+  return index == dev.index();
+}
+int type16(at::ScalarType t) { return t == at::kBFloat16 ? FA_TYPE_BF16 : (t == at::kHalf ? FA_TYPE_F16 : -1); }
+
+// (Kcodes, Kscales, Vcodes, Vscales) and a table: as binding._qcache
+struct QCache {
+  const at::Tensor *t[4], *table = nullptr;
+  int Hkv, d, slots, k_bits, v_bits, page = 0, pages = 0;
+  bool parse(PyObject* cache, PyObject* table_arg, PyObject* most, int B, c10::Device dev) {
+    int Nk;
+    if (!PyTuple_Check(cache) || PyTuple_GET_SIZE(cache) != 4 || !integer(most, Nk) || Nk < 0) return false;
+    for (int i = 0; i < 4; ++i) {
+      t[i] = plain(PyTuple_GET_ITEM(cache, i));
+      if (!t[i] || t[i]->dim() != 4 || t[i]->scalar_type() != at::kByte || t[i]->device() != dev) return false;
+    }
+    if (t[1]->size(3) > 1 << 20) return false;
+    d = 32 * (int)t[1]->size(3), Hkv = (int)t[0]->size(1);
+    k_bits = t[0]->size(3) == d ? 8 : 4, v_bits = t[2]->size(3) == d ? 8 : 4;
+    const int64_t n = t[0]->size(0), rows = t[0]->size(2), width[4] = {(int64_t)d * k_bits / 8, d / 32, (int64_t)d * v_bits / 8, d / 32};
+    for (int i = 0; i < 4; ++i)
+      if (t[i]->sizes() != at::IntArrayRef({n, (int64_t)Hkv, rows, width[i]})) return false;
+    if (table_arg == Py_None) {
+      if (n != B || (Nk && Nk != rows)) return false;
+      slots = (int)rows;
+      return true;
+    }
+    table = plain(table_arg);
+    if (!table || table->dim() != 2 || !is(table, at::kInt, dev, {B, table->size(1)})) return false;
+    page = (int)rows, pages = (int)table->size(1);
+    const long all = (long)page * pages;
+    if (all > INT_MAX || Nk > all) return false;
+    slots = Nk ? Nk : (int)all;
+    return true;
+  }
+  const int32_t* pages_of() const { return table ? (const int32_t*)in(table) : nullptr; }
+};
+// Strides of a tensor of dense rows, a multiple of `unit` elements apart (a dimension of one has no say)
+bool row_strides(const at::Tensor* t, int64_t unit, long long* s) {
+  const int n = (int)t->dim();
+  if (t->stride(n - 1) != 1 && t->size(n - 1) > 1) return false;
+  for (int i = 0; i < 3; ++i) {
+    const int j = i + n - 4;
+    s[i] = j < 0 || t->size(j) == 1 ? 0 : t->stride(j);
+    if (s[i] < 0 || s[i] % unit) return false;
+  }
+  return true;
+}
+
+// Knew, Vnew, cache, seqlens_k, block_table, max_seqlen_k, Kout, Vout -> True
+PyObject* qcache_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 8 || !plain_context()) Py_RETURN_NONE;
+  const at::Tensor *K = strided(args[0]), *V = strided(args[1]), *Ko = nullptr, *Vo = nullptr;
+  if (!K || !V || K->dim() != 4) Py_RETURN_NONE;
+  const at::ScalarType et = K->scalar_type();
+  const c10::Device dev = K->device();
+  const int type = type16(et), B = (int)K->size(0), Nq = (int)K->size(1), Hkv = (int)K->size(2), d = (int)K->size(3);
+  long long ks[3], vs[3];
+  const int32_t* lens;
+  QCache c;
+  void* st;
+  if (type < 0 || !is(V, et, dev, K->sizes()) || !row_strides(K, 8, ks) || !row_strides(V, 8, vs) || !c.parse(args[2], args[4], args[5], B, dev) ||
+      c.Hkv != Hkv || c.d != d || !lengths(args[3], B, dev, lens))
+    Py_RETURN_NONE;
+  if (args[6] != Py_None && (!(Ko = plain(args[6])) || !is(Ko, et, dev, K->sizes()))) Py_RETURN_NONE;
+  if (args[7] != Py_None && (!(Vo = plain(args[7])) || !is(Vo, et, dev, K->sizes()))) Py_RETURN_NONE;
+  if (!current_stream_of(dev, st)) {
+    if (PyErr_Occurred()) return nullptr;
+    Py_RETURN_NONE;
+  }
+  const void *k = in(K), *v = in(V);
+  void *ko = Ko ? Ko->mutable_data_ptr() : nullptr, *vo = Vo ? Vo->mutable_data_ptr() : nullptr;
+  void* p[4];
+  for (int i = 0; i < 4; ++i) p[i] = c.t[i]->mutable_data_ptr();
+  const int32_t* tb = c.pages_of();
+  const int e = without_gil([&] {
+    return lib.fa_qcache_append(k, v, p[0], p[1], p[2], p[3], ko, vo, lens, tb, B, Hkv, Nq, c.slots, d, c.k_bits, c.v_bits, c.page, c.pages, ks[0],
+                                ks[1], ks[2], vs[0], vs[1], vs[2], type, st);
+  });
+  if (e) Py_RETURN_NONE;
+  Py_RETURN_TRUE;
+  END_HANDLE_TH_ERRORS
+}
+
+// cache, K, V, seqlens_k, block_table, max_seqlen_k, first, cu_seqlens -> True
+PyObject* qcache_read(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 8 || !plain_context()) Py_RETURN_NONE;
+  const at::Tensor *K = plain(args[1]), *V = plain(args[2]), *cu = nullptr;
+  if (!K || K->dim() < 3) Py_RETURN_NONE;
+  const at::ScalarType et = K->scalar_type();
+  const c10::Device dev = K->device();
+  const int type = type16(et), dims = args[7] == Py_None ? 4 : 3;
+  if (type < 0 || K->dim() != dims || !is(V, et, dev, K->sizes())) Py_RETURN_NONE;
+  int B = (int)K->size(0);
+  if (dims == 3) {
+    cu = plain(args[7]);
+    if (!cu || cu->dim() != 1 || cu->size(0) < 2 || !is(cu, at::kInt, dev, cu->sizes()) || args[6] != Py_None) Py_RETURN_NONE;
+    B = (int)cu->size(0) - 1;
+  }
+  const int32_t *lens, *first;
+  QCache c;
+  void* st;
+  if (!c.parse(args[0], args[4], args[5], B, dev) || K->size(dims - 2) != c.Hkv || K->size(dims - 1) != c.d || !lengths(args[3], B, dev, lens) ||
+      !lengths(args[6], B, dev, first))
+    Py_RETURN_NONE;
+  if (!current_stream_of(dev, st)) {
+    if (PyErr_Occurred()) return nullptr;
+    Py_RETURN_NONE;
+  }
+  const int N = (int)K->size(dims - 3);
+  void *k = K->mutable_data_ptr(), *v = V->mutable_data_ptr();
+  const int32_t *tb = c.pages_of(), *cs = cu ? (const int32_t*)in(cu) : nullptr;
+  const int e = without_gil([&] {
+    return lib.fa_qcache_read(in(c.t[0]), in(c.t[1]), in(c.t[2]), in(c.t[3]), k, v, lens, tb, first, cs, B, c.Hkv, N, c.slots, c.d, c.k_bits, c.v_bits,
+                              c.page, c.pages, type, st);
+  });
+  if (e) Py_RETURN_NONE;
+  Py_RETURN_TRUE;
+  END_HANDLE_TH_ERRORS
+}
+
+// Q, cache, scale, causal, seqlens_k, block_table, max_seqlen_k
+PyObject* qcache_fwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 7 || !plain_context()) Py_RETURN_NONE;
+  const at::Tensor* Q = plain(args[0]);
+  float scale;
+  int causal;
+  if (!Q || Q->dim() != 4 || !number(args[2], scale) || !flag(args[3], causal)) Py_RETURN_NONE;
+  const at::ScalarType et = Q->scalar_type();
+  const c10::Device dev = Q->device();
+  const int type = type16(et), B = (int)Q->size(0), Nq = (int)Q->size(1), Hq = (int)Q->size(2), d = (int)Q->size(3);
+  const int32_t* lens;
+  QCache c;
+  void* st;
+  if (type < 0 || !c.parse(args[1], args[5], args[6], B, dev) || c.d != d || !lengths(args[4], B, dev, lens)) Py_RETURN_NONE;
+  if (!current_stream_of(dev, st)) {
+    if (PyErr_Occurred()) return nullptr;
+    Py_RETURN_NONE;
+  }
+  const size_t nb = lib.fa_qcache_fwd_workspace_bytes(B, Hq, c.Hkv, Nq, c.slots, d);
+  at::Tensor O = make(Q->sizes(), et, dev), L = make({B, Hq, Nq}, at::kFloat, dev), W;
+  if (nb) W = make({(int64_t)nb}, at::kByte, dev);
+  const void* q = in(Q);
+  void *o = O.mutable_data_ptr(), *w = nb ? W.mutable_data_ptr() : nullptr;
+  float* l = (float*)L.mutable_data_ptr();
+  const int32_t* tb = c.pages_of();
+  const int e = without_gil([&] {
+    return lib.fa_qcache_fwd(q, in(c.t[0]), in(c.t[1]), in(c.t[2]), in(c.t[3]), lens, tb, o, l, w, nb, B, Hq, c.Hkv, Nq, c.slots, d, c.k_bits, c.v_bits,
+                             c.page, c.pages, scale, causal, type, st);
+  });
+  if (e) Py_RETURN_NONE;
+  return pack({O, L});
+  END_HANDLE_TH_ERRORS
+}
+
+// inverse, Q, K, positions, inv_freq, axis, neighbours -> (Qout, Kout), contiguous
+PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 7 || !plain_context()) Py_RETURN_NONE;
+  const at::Tensor *Q = strided(args[1]), *K = nullptr, *pos = strided(args[3]), *f = plain(args[4]), *ax = nullptr;
+  int inverse, neighbours;
+  if (!Q || !pos || !f || f->dim() != 1 || !flag(args[0], inverse) || !flag(args[6], neighbours)) Py_RETURN_NONE;
+  const at::ScalarType et = Q->scalar_type();
+  const c10::Device dev = Q->device();
+  const int n = (int)Q->dim(), lead = n - 2, type = value_type(Q);
+  if (type < 0 || (n != 3 && n != 4)) Py_RETURN_NONE;
+  const int d = (int)Q->size(n - 1), Hq = (int)Q->size(n - 2), N = (int)Q->size(n - 3), B = n == 4 ? (int)Q->size(0) : 1, pairs = (int)f->size(0);
+  int Hkv = 0;
+  if (args[2] != Py_None) {
+    K = strided(args[2]);
+    if (!K || K->dim() != n || K->scalar_type() != et || K->device() != dev || K->size(n - 1) != d || K->size(n - 3) != N ||
+        (n == 4 && K->size(0) != B))
+      Py_RETURN_NONE;
+    Hkv = (int)K->size(n - 2);
+  }
+  // positions [axes, B, N], [axes, T], or without the first dimension
+  const int p = (int)pos->dim() - lead;
+  if (p < 0 || p > 1 || pos->scalar_type() != at::kInt || pos->device() != dev || pos->size(p + lead - 1) != N || (lead == 2 && pos->size(p) != B) ||
+      (N > 1 && pos->stride(p + lead - 1) != 1))
+    Py_RETURN_NONE;
+  const int axes = p ? (int)pos->size(0) : 1;
+  const long long as = axes > 1 ? pos->stride(0) : 0, bs = lead == 2 && B > 1 ? pos->stride(p) : 0;
+  if (!is(f, at::kFloat, dev, {pairs}) || 2 * (long)pairs > d) Py_RETURN_NONE;
+  if (args[5] != Py_None && (!(ax = plain(args[5])) || !is(ax, at::kInt, dev, {pairs}))) Py_RETURN_NONE;
+  void* st;
+  if (!current_stream_of(dev, st)) {
+    if (PyErr_Occurred()) return nullptr;
+    Py_RETURN_NONE;
+  }
+  at::Tensor Qo = make(Q->sizes(), et, dev), Ko;
+  if (K) Ko = make(K->sizes(), et, dev);
+  long long s[12] = {0};
+  if (!row_strides(Q, 1, s) || !row_strides(&Qo, 1, s + 3) || (K && (!row_strides(K, 1, s + 6) || !row_strides(&Ko, 1, s + 9)))) Py_RETURN_NONE;
+  const void *q = in(Q), *k = K ? in(K) : nullptr;
+  void *qo = Qo.mutable_data_ptr(), *ko = K ? Ko.mutable_data_ptr() : nullptr;
+  const int32_t *ps = (const int32_t*)in(pos), *as32 = ax ? (const int32_t*)in(ax) : nullptr;
+  const float* fr = stat(f);
+  const int e = without_gil([&] {
+    return (inverse ? lib.fa_rope_bwd : lib.fa_rope_fwd)(q, k, qo, ko, ps, fr, as32, B, N, Hq, Hkv, d, pairs, axes, neighbours, s, as, bs, type, st);
+  });
+  if (e) Py_RETURN_NONE;
+  if (K) return pack({Qo, Ko});
+  PyObject* o = THPVariable_Wrap(Qo);
+  if (!o) return nullptr;
+  PyObject* r = PyTuple_Pack(2, o, Py_None);
+  Py_DECREF(o);
+  return r;
+  END_HANDLE_TH_ERRORS
+}
+
 PyObject* cache_splits(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   int v[6], ragged;
   for (int i = 0; i < 6; ++i)
@@ -636,7 +862,8 @@ PyObject* entry_names(PyObject*, PyObject*) {
 
 #define FAST(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(dense_fwd), FAST(dense_bwd), FAST(varlen_fwd), FAST(varlen_bwd), FAST(kvcache_fwd), FAST(cache_splits),
-                         FAST(prefix_fwd), FAST(cache_append), FAST(cache_weights), FAST(cache_evict), FAST(verify_drafts),
+                         FAST(prefix_fwd), FAST(cache_append), FAST(cache_weights), FAST(cache_evict), FAST(verify_drafts), FAST(qcache_append),
+                         FAST(qcache_read), FAST(qcache_fwd), FAST(rope),
                          {"init", init, METH_VARARGS, nullptr}, {"entry_names", entry_names, METH_NOARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -228,6 +228,64 @@ struct VerifyArgs {
 size_t verify_workspace(int B, int k, int V);
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t st);
 
+// A cache held in 4 or 8 bits (fa_mx.h): c says where the slots are, codes and scales hold them.
+struct QCacheView {
+  CacheView c;
+  uint8_t *Kc, *Ks, *Vc, *Vs;
+  int k_bits, v_bits;
+};
+// New rows into it, and slots back in 16 bits (fa_qcache.hip)
+struct QAppendArgs {
+  QCacheView c;
+  const __bf16 *Kn, *Vn;
+  __bf16 *Kout, *Vout;  // the values that the new slots stand for, [nseq, Nq, Hkv, d], or nullptr
+  long k_bs, k_ts, k_hs, v_bs, v_ts, v_hs;  // strides of Kn, Vn: sequence, token, head
+  int nseq, Nq, f16;
+};
+hipError_t launch_qappend(const QAppendArgs& a, hipStream_t st);
+struct QReadArgs {
+  QCacheView c;
+  __bf16 *K, *V;         // [nseq, N, Hkv, d], or with cu [total, Hkv, d]
+  const int32_t* first;  // slot of each sequence's row 0 (nullptr: 0); not with cu
+  const int32_t* cu;     // [nseq + 1]: sequence s fills rows cu[s] .. cu[s + 1] from its slot 0 on
+  int nseq, N, f16;
+  long total;
+};
+hipError_t launch_qread(const QReadArgs& a, hipStream_t st);
+// Attention over it (fa_qattend.hip)
+struct QAttendArgs {
+  QCacheView c;
+  const __bf16* Q;
+  __bf16* O;
+  float* LSE;
+  float *Opart, *Lpart;  // [share][token][Hq][d], [share][token][Hq]; unused with one share
+  int nseq, Nq, Hq, G, f16, causal;
+  float scale, scale_log2e;
+};
+struct QAttendPlan {  // how rows and keys are cut (a function of the sizes alone)
+  int rows;           // packed rows (query * G + head of the group) of an item
+  int keys, shares;   // keys of a share, a multiple of 64, and how many that makes
+};
+QAttendPlan qattend_plan(int B, int Hq, int Hkv, int Nq, int Nk, int d);
+hipError_t launch_qattend(const QAttendArgs& a, hipStream_t st);
+
+// Queries and keys rotated by their positions (fa_rope.hip)
+struct RopeTensor {
+  const void* x;
+  void* y;
+  int heads;
+  long x_bs, x_ts, x_hs, y_bs, y_ts, y_hs;  // strides: sequence, token, head
+};
+struct RopeArgs {
+  RopeTensor t[2];  // t[1].heads = 0: one tensor
+  const int32_t* positions;  // axis a, sequence s, token i at positions[a * p_as + s * p_bs + i]
+  const float* inv_freq;     // [pairs]
+  const int32_t* axis;       // [pairs] or nullptr (axis 0)
+  long p_as, p_bs;
+  int nseq, N, d, pairs, axes, type, neighbours, inverse, vec;  // vec: elements moved at once
+};
+hipError_t launch_rope(const RopeArgs& a, hipStream_t st);
+
 hipError_t launch_fwd(const FwdArgs& a, int d, int causal, hipStream_t st);
 // forward in workgroups of four wavefronts for grids that leave wavefront slots empty (fa_stream.hip); d in {64, 128}
 hipError_t launch_fwd_stream(const FwdArgs& a, int d, int causal, hipStream_t st);

@@ -20,6 +20,7 @@
 
 #include "fa_kernels.h"
 #include "fa_lds.h"
+#include "fa_merge.h"
 
 namespace fa {
 
@@ -406,55 +407,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   else wide_item<D, F16>(a, it, smem);
 }
 
-// One thread per four elements of a (token, head) row. Few threads a row and a handful of slots: the time is the chain of loads, so
-// the logsumexps and partial rows of FLY slots are requested together, and where there are no more than that none is read twice.
-// (A slot without keys for this row has written no partial O: what is read in its place is not used.)
 template <int D, bool F16, int FLY>
 __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixArgs a, int slots) {
-  constexpr int TPR = D / 4;
-  const long all = (long)a.nseq * a.Nq * a.Hq, r = (long)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
-  if (r >= all) return;
-  const int c = threadIdx.x % TPR;
-  float l[FLY], mx = -INFINITY;
-  f32x4 o[FLY];
-  auto request = [&](int k0) {
-#pragma unroll
-    for (int u = 0; u < FLY; ++u) l[u] = a.Lpart[(k0 + u < slots ? k0 + u : slots - 1) * all + r];
-#pragma unroll
-    for (int u = 0; u < FLY; ++u) o[u] = *(const f32x4*)(a.Opart + ((k0 + u < slots ? k0 + u : slots - 1) * all + r) * D + 4 * c);
-  };
-  request(0);
-  for (int k = FLY; k < slots; ++k) mx = max_or_nan(mx, a.Lpart[k * all + r]);
-#pragma unroll
-  for (int u = 0; u < FLY; ++u) mx = max_or_nan(mx, l[u]);
-  const long tok = r / a.Hq;
-  const int h = (int)(r - tok * a.Hq);
-  const long s = tok / a.Nq;
-  float* lse = a.LSE + (s * a.Hq + h) * a.Nq + (tok - s * a.Nq);
-  if (mx == -INFINITY) {  // no key anywhere
-    *(u32x2*)(a.O + r * D + 4 * c) = (u32x2){0u, 0u};
-    if (c == 0) *lse = -INFINITY;
-    return;
-  }
-  float z = 0.f;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int k0 = 0;;) {
-#pragma unroll
-    for (int u = 0; u < FLY; ++u) {
-      if (k0 + u >= slots || l[u] == -INFINITY) continue;
-      const float wgt = __expf(l[u] - mx);
-      z += wgt;
-      acc += o[u] * wgt;
-    }
-    if ((k0 += FLY) >= slots) break;
-    request(k0);
-  }
-  const float inv = 1.f / z;
-  u32x2 x;
-  x[0] = pack2<F16>(acc[0] * inv, acc[1] * inv);
-  x[1] = pack2<F16>(acc[2] * inv, acc[3] * inv);
-  *(u32x2*)(a.O + r * D + 4 * c) = x;
-  if (c == 0) *lse = mx + __logf(z);
+  merge_slots<D, F16, FLY>(a.Opart, a.Lpart, a.O, a.LSE, (long)a.nseq * a.Nq * a.Hq, a.Hq, a.Nq, slots);
 }
 
 template <int D, bool F16>
