@@ -16,7 +16,7 @@
 
 #include "fa_lds.h"
 #include "fa_merge.h"
-#include "fa_mx.h"
+#include "fa_qattend.h"
 
 namespace fa {
 
@@ -47,16 +47,6 @@ __device__ __forceinline__ int v_swizzle(int k) {
   const int k0 = k & 1, k1 = (k >> 1) & 1, k2 = (k >> 2) & 1;
   if (D == 128) return VB == 4 ? (k0 << 1 | k1 | k1 << 2 | k2 << 3) : (k0 | k0 << 1 | k1 << 2 | k2 << 3);
   return VB == 4 ? (k2 | k1 << 1 | k2 << 2) : (k1 | k1 << 1 | k2 << 2);  // (two rows of 128 bytes share a line of the banks)
-}
-
-struct QItem {
-  int s, g, nk, begin, end;  // keys in all, and the share [begin, end)
-  long tok0;                 // token of packed row 0
-  int row0, rows, off, slot;
-};
-__device__ __forceinline__ long out_row(const QAttendArgs& a, const QItem& it, int r) {  // token * Hq + head of packed row r of the item
-  const int row = it.row0 + r, q = row / a.G;
-  return (it.tok0 + q) * a.Hq + it.g * a.G + (row - q * a.G);
 }
 
 template <int D, int KB, int VB, int RT>
@@ -303,8 +293,7 @@ __device__ __forceinline__ void narrow_item(const QAttendArgs& a, const QItem& i
       x[0] = pack2<F16>(o[0] * inv, o[1] * inv);
       x[1] = pack2<F16>(o[2] * inv, o[3] * inv);
       *(u32x2*)(a.O + at * D + 4 * c) = x;
-      const long tok = at / a.Hq, s = tok / a.Nq;
-      if (c == 0) a.LSE[(s * a.Hq + (at - tok * a.Hq)) * a.Nq + (tok - s * a.Nq)] = lse;
+      if (c == 0) *lse_at(a, at) = lse;
     } else {
       const long all = (long)a.nseq * a.Nq * a.Hq;
       *(f32x4*)(a.Opart + (it.slot * all + at) * D + 4 * c) = o * inv;
@@ -313,38 +302,16 @@ __device__ __forceinline__ void narrow_item(const QAttendArgs& a, const QItem& i
   }
 }
 
+// Wavefronts of a SIMD: what registers allow
+constexpr int narrow_waves(int D, int bits, int RT) { return D == 64 ? (RT == 1 ? 4 : 3) : (RT == 1 && bits == 8 ? 3 : 2); }
 template <int D, bool F16, int KB, int VB, int RT>
-__global__ __launch_bounds__(256) void qattend_narrow_kernel(QAttendArgs a, QAttendPlan plan) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(narrow_waves(D, KB + VB, RT), narrow_waves(D, KB + VB, RT)))) void qattend_narrow_kernel(QAttendArgs a, QAttendPlan plan) {
   __shared__ __attribute__((aligned(1024))) char smem[Narrow<D, KB, VB, RT>::LDS];
   const int blocks = (a.Nq * a.G + plan.rows - 1) / plan.rows, per = blocks * plan.shares;
-  // (sequences of uneven lengths: longest first)
-  const int pair = blockIdx.x / (unsigned)per, in = blockIdx.x - (unsigned)pair * per, rank = pair / a.c.c.Hkv;
-  const CacheSequence cs = cache_sequence(a.c.c.lens, a.c.c.Nk, a.nseq, rank);
-  QItem it;
-  it.s = cs.s;
-  it.g = pair - rank * a.c.c.Hkv;
-  it.slot = in % plan.shares;
-  it.row0 = in / plan.shares * plan.rows;
-  it.rows = a.Nq * a.G - it.row0 < plan.rows ? a.Nq * a.G - it.row0 : plan.rows;
-  it.tok0 = (long)it.s * a.Nq;
-  it.nk = cs.len;
-  it.off = it.nk - a.Nq;
-  const long begin = (long)it.slot * plan.keys;
-  it.begin = begin < it.nk ? (int)begin : it.nk;
-  it.end = it.nk - it.begin < plan.keys ? it.nk : it.begin + plan.keys;
+  const int pair = blockIdx.x / (unsigned)per, in = blockIdx.x - (unsigned)pair * per;
+  const QItem it = make_item(a, plan, pair, in / plan.shares, in % plan.shares);
   const bool direct = plan.shares == 1;
-  if (it.begin >= it.end) {  // no key: L = -inf, and with one share O = 0
-    const long all = (long)a.nseq * a.Nq * a.Hq;
-    for (int i = threadIdx.x; i < it.rows * (D / 4); i += 256) {
-      const int r = i / (D / 4), c = i % (D / 4);
-      const long at = out_row(a, it, r), tok = at / a.Hq, s = tok / a.Nq;
-      if (direct) *(u32x2*)(a.O + at * D + 4 * c) = (u32x2){0u, 0u};
-      if (c) continue;
-      if (direct) a.LSE[(s * a.Hq + (at - tok * a.Hq)) * a.Nq + (tok - s * a.Nq)] = -INFINITY;
-      else a.Lpart[it.slot * all + at] = -INFINITY;
-    }
-    return;
-  }
+  if (it.begin >= it.end) return empty_item<D>(a, it, direct);
   narrow_item<D, F16, KB, VB, RT>(a, it, direct, smem);
 }
 
@@ -354,8 +321,7 @@ __global__ __launch_bounds__(256) void qattend_merge_kernel(QAttendArgs a, int s
 }
 
 template <int D, bool F16, int KB, int VB>
-hipError_t launch_bits(const QAttendArgs& a, hipStream_t st) {
-  const QAttendPlan plan = qattend_plan(a.nseq, a.Hq, a.c.c.Hkv, a.Nq, a.c.c.Nk, D);
+hipError_t launch_bits(const QAttendArgs& a, const QAttendPlan& plan, hipStream_t st) {
   const long items = (long)a.nseq * a.c.c.Hkv * (((long)a.Nq * a.G + plan.rows - 1) / plan.rows) * plan.shares;
   if (items > 0x7fffffffL) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)items), block(256);
@@ -365,9 +331,10 @@ hipError_t launch_bits(const QAttendArgs& a, hipStream_t st) {
 }
 template <int D, bool F16>
 hipError_t launch_type(const QAttendArgs& a, hipStream_t st) {
-  const hipError_t e = a.c.k_bits == 4 ? (a.c.v_bits == 4 ? launch_bits<D, F16, 4, 4>(a, st) : launch_bits<D, F16, 4, 8>(a, st))
-                                       : (a.c.v_bits == 4 ? launch_bits<D, F16, 8, 4>(a, st) : launch_bits<D, F16, 8, 8>(a, st));
-  const int slots = qattend_plan(a.nseq, a.Hq, a.c.c.Hkv, a.Nq, a.c.c.Nk, D).shares;
+  const QAttendPlan plan = qattend_plan(a.nseq, a.Hq, a.c.c.Hkv, a.Nq, a.c.c.Nk, D);
+  const hipError_t e = plan.rows == 128 ? launch_qattend_wide(a, plan, st) : a.c.k_bits == 4 ? (a.c.v_bits == 4 ? launch_bits<D, F16, 4, 4>(a, plan, st) : launch_bits<D, F16, 4, 8>(a, plan, st))
+                                       : (a.c.v_bits == 4 ? launch_bits<D, F16, 8, 4>(a, plan, st) : launch_bits<D, F16, 8, 8>(a, plan, st));
+  const int slots = plan.shares;
   if (e || slots == 1) return e;
   constexpr int RPB = 256 / (D / 4);
   const dim3 grid((unsigned)(((long)a.nseq * a.Nq * a.Hq + RPB - 1) / RPB));
@@ -381,9 +348,9 @@ hipError_t launch_type(const QAttendArgs& a, hipStream_t st) {
 QAttendPlan qattend_plan(int B, int Hq, int Hkv, int Nq, int Nk, int d) {
   QAttendPlan p;
   const long rows = (long)Nq * (Hq / Hkv);
-  p.rows = rows <= 16 ? 16 : 32;
+  p.rows = rows <= 16 ? 16 : (rows <= 64 ? 32 : 128);
   const long items = (long)B * Hkv * ((rows + p.rows - 1) / p.rows), blocks = ((long)Nk + 63) / 64;
-  long shares = 768 / items;
+  long shares = (p.rows == 128 ? 512 : 768) / items;
   shares = std::max(1l, std::min(std::min(shares, 128l), blocks / 4));
   const long per = (blocks + shares - 1) / shares;
   p.keys = (int)(64 * per);

@@ -7,7 +7,7 @@ import re
 from paper_2307_08691_amd import build as fa_build
 from test_kernel_resources import resource_remarks
 
-SOURCES = ["fa_qcache.hip", "fa_qattend.hip", "fa_rope.hip"]
+SOURCES = ["fa_qcache.hip", "fa_qattend.hip", "fa_qattend_wide.hip", "fa_rope.hip"]
 
 
 def test_every_kernel_is_built_and_needs_no_scratch():
