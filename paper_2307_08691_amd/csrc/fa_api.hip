@@ -1325,13 +1325,14 @@ int fa_qcache_read(const void* Kcodes, const void* Kscales, const void* Vcodes, 
 
 static bool qcache_fwd_sizes(int B, int Hq, int Hkv, int Nq, int Nk) {
   return B > 0 && Hq > 0 && Hkv > 0 && Hq % Hkv == 0 && Nq > 0 && Nk > 0 && Nk <= FA_CACHE_MAX_SLOTS && Hkv <= (1 << 16) &&
-         (double)B * Nq * Hq <= (1 << 26);
+         (double)B * Nq * Hq <= (1 << 26) && (double)B * Hkv * (((double)Nq * (Hq / Hkv)) / 16 + 1) * (Nk / 128 + 1) < (double)0x7fffffff;
 }
 
 size_t fa_qcache_fwd_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int d) {
   if (!qcache_fwd_sizes(B, Hq, Hkv, Nq, Nk) || (d != 64 && d != 128)) return 0;
   const fa::QAttendPlan p = fa::qattend_plan(B, Hq, Hkv, Nq, Nk, d);
-  return p.shares == 1 ? 0 : round_up((size_t)p.shares * B * Nq * Hq * (d + 1) * sizeof(float), 256);
+  if (p.slots == 0) return 0;
+  return round_up((size_t)p.slots * p.rows * (d + 1) * sizeof(float) + (size_t)B * Hkv * p.blocks * sizeof(fa::QAttendArgs::Unit), 256);
 }
 
 int fa_qcache_fwd(const void* Q, const void* Kcodes, const void* Kscales, const void* Vcodes, const void* Vscales, const int32_t* seqlens_k,
@@ -1353,7 +1354,8 @@ int fa_qcache_fwd(const void* Q, const void* Kcodes, const void* Kscales, const 
   a.O = (__bf16*)O;
   a.LSE = LSE;
   a.Opart = (float*)workspace;
-  a.Lpart = a.Opart + (p.shares == 1 ? 0 : (size_t)p.shares * B * Nq * Hq * d);
+  a.Lpart = a.Opart + (size_t)p.slots * p.rows * d;
+  a.units = (fa::QAttendArgs::Unit*)(a.Lpart + (size_t)p.slots * p.rows);
   a.nseq = B;
   a.Nq = Nq;
   a.Hq = Hq;

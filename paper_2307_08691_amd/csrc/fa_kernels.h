@@ -258,13 +258,19 @@ struct QAttendArgs {
   const __bf16* Q;
   __bf16* O;
   float* LSE;
-  float *Opart, *Lpart;  // [share][token][Hq][d], [share][token][Hq]; unused with one share
+  float *Opart, *Lpart;  // [slot][plan.rows][d], [slot][plan.rows] (fa_qattend.h)
+  struct Unit {
+    int first, parts;    // of a unit: the workgroup that has its first keys, and how many have parts of it (0: it is finished)
+  };
+  Unit* units;           // [nseq][Hkv][plan.blocks]
   int nseq, Nq, Hq, G, f16, causal;
   float scale, scale_log2e;
 };
-struct QAttendPlan {  // how rows and keys are cut (a function of the sizes alone)
-  int rows;           // packed rows (query * G + head of the group) of an item
-  int keys, shares;   // keys of a share, a multiple of 64, and how many that makes
+struct QAttendPlan {      // how the work is cut (a function of the sizes alone)
+  int rows, blocks;       // packed rows (query * G + head of the group) of a block, blocks of a key/value head
+  int chunk_log2;         // keys that are dealt together
+  int groups, least;      // workgroups, and the fewest chunks that one is started for
+  int slots;              // places for partial results
 };
 QAttendPlan qattend_plan(int B, int Hq, int Hkv, int Nq, int Nk, int d);
 hipError_t launch_qattend(const QAttendArgs& a, hipStream_t st);

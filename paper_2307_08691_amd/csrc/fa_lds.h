@@ -62,6 +62,16 @@ __device__ __forceinline__ void dma16_uniform(const void* gbase, unsigned voff, 
                : "memory");
 }
 
+// ... for data that is read once (nt: it does not displace what the caches hold)
+__device__ __forceinline__ void dma16_uniform_once(const void* gbase, unsigned voff, const void* lds) {
+  const unsigned long long b = (unsigned long long)gbase;
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)b), hi = __builtin_amdgcn_readfirstlane((unsigned)(b >> 32));
+  gbase = (const void*)(((unsigned long long)hi << 32) | lo);
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(voff), "s"(gbase),
+               "s"(__builtin_amdgcn_readfirstlane(lds_address(lds)))
+               : "memory");
+}
+
 // Copy `nrows` rows of D bf16 elements (row pitch `gstride` elements, first row
 // `row_first`, rows clamped to `row_last`) from global memory straight into a
 // swizzled LDS tile, 16 bytes per lane, without passing through registers. Each

@@ -1,17 +1,19 @@
 // Attention over a key/value cache held in 4 or 8 bits (fa_mx.h): Algorithm 1 over what the codes stand for, with the parallelism of
-// decoding. The rows of one (sequence, key/value head), query * G + head of the group, are cut into items of up to 32 of them against a
-// share of the keys; the four wavefronts of a workgroup take tiles of 32 keys in turn, each with a running softmax of its own, no barrier
-// in the loop, and join through LDS at the end. Shares are joined by a second launch (fa_merge.h).
+// decoding. The rows of one (sequence, key/value head), query * G + head of the group, come in blocks of up to 32; the four wavefronts of
+// a workgroup take tiles of 32 keys (64 of 64 channels) of a segment (fa_qattend.h) in turn, each with a running softmax of its own, no barrier in the loop, and
+// join through LDS at the segment's end.
 //
 // Codes become 16-bit elements in registers, two an instruction, and every product is a 16x16x32 MFMA of those:
-//   * S^T = K Q^T: a lane holds a quarter of a key's channels, D / 4 consecutive ones of one or two blocks, as they lie in memory. The
-//     order in which channels are summed is free, so step s of the contraction takes eight of each lane's own, and Q is held alike.
-//   * O^T += V^T P^T needs keys along a lane's operand, so V goes through LDS once: read in whole rows, converted, written as 16-bit rows and
+//   * S^T = K Q^T: a lane holds a quarter of a key's channels, D / 4 consecutive ones of one block. The order in which channels are summed is
+//     free, so step s of the contraction takes eight of each lane's own, and Q is held alike.
+//   * O^T += V^T P^T needs keys along a lane's operand, so V goes through LDS again as 16-bit elements, 64 channels at a time, and is
 //     read back transposed. P^T is in place already: the keys of a lane's eight operand elements are those whose scores it has.
-// Bound by HBM, which hands a compute unit 24 bytes a ns: 136 bytes a key of 128 channels in 4 bits.
+// Tiles come by direct copies to LDS, whole rows a request, several tiles ahead (NLOADS), and go to registers at once when they are
+// there, so that their place is requested again. Bound by HBM, which hands a compute unit 24 bytes a ns: 136 bytes a key of 128 channels in 4 bits.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cstdlib>
 #include <type_traits>
 
 #include "fa_lds.h"
@@ -39,88 +41,148 @@ __device__ __forceinline__ float sum_of_four(float x) {
   return sum_with_partner32(__builtin_bit_cast(float, (int)sw[0]) + __builtin_bit_cast(float, (int)sw[1]));
 }
 
-// Where chunk c (16 bytes) of key k lies in a wavefront's V tile, 32 rows of 2 D bytes: XOR-ed with a function of the key chosen so that the
-// transposing reads (8 keys x 32 bytes at a time) and the writes (16 lanes x 16 bytes: PIECE chunks a lane, 2 (VB = 8) or 4) are both free
-// of bank conflicts.
-template <int D, int VB>
-__device__ __forceinline__ int v_swizzle(int k) {
-  const int k0 = k & 1, k1 = (k >> 1) & 1, k2 = (k >> 2) & 1;
-  if (D == 128) return VB == 4 ? (k0 << 1 | k1 | k1 << 2 | k2 << 3) : (k0 | k0 << 1 | k1 << 2 | k2 << 3);
-  return VB == 4 ? (k2 | k1 << 1 | k2 << 2) : (k1 | k1 << 1 | k2 << 2);  // (two rows of 128 bytes share a line of the banks)
+// Tiles of codes in LDS, 32 rows of ROW bytes in pieces of 16: piece c of key k lies at place c ^ mix(k) of its row, so that 16 keys' pieces c
+// lie in different banks.
+template <int ROW>
+__device__ __forceinline__ int code_mix(int k) {
+  return ROW == 128 ? (k >> 1) & 7 : (ROW == 64 ? (k >> 2) & 3 : (k >> 3) & 1);
+}
+// What lane `lane` fetches with request u of a tile: from its first row on, keys past `last` repeating that one
+template <int ROW>
+__device__ __forceinline__ unsigned code_offset(int u, int lane, int last) {
+  const int k = (64 * u + lane) / (ROW / 16), c = (lane % (ROW / 16)) ^ code_mix<ROW>(k);
+  return (unsigned)((k < last ? k : last) * ROW + 16 * c);
+}
+// V as 16-bit elements: 32 rows of 64 channels (128 bytes). Free of conflicts for the writes (16 keys at one piece) and the transposing reads
+// (8 keys x 32 bytes; two rows share a line of the banks).
+__device__ __forceinline__ int v_mix(int k) { return (k & 6) | ((k >> 3) & 1); }
+
+// 2 bytes a lane from global memory into LDS, a word each (see dma16)
+__device__ __forceinline__ void dma2(const void* gaddr, const void* lds) {
+  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_ushort %0, off" ::"v"(gaddr), "s"(__builtin_amdgcn_readfirstlane(lds_address(lds))) : "memory");
 }
 
 template <int D, int KB, int VB, int RT>
 struct Narrow {
-  static constexpr int NW = 4, KT = 32, ROWS = 16 * RT, ROWB = 2 * D, VTILE = KT * ROWB, PART = ROWS * 4 * D, WAVEB = VTILE > PART ? VTILE : PART;
+  static constexpr int NW = 4, KT = 4096 / D, ROWS = 16 * RT, KROW = D * KB / 8, VROW = D * VB / 8, SROW = D / 32;  // bytes of a row of codes, of scales
+  static constexpr int KN = KT * KROW / 1024, VN = KT * VROW / 1024, SN = KT / 32, REQUESTS = KN + VN + SN;  // of a tile
+  static constexpr int STAGEB = KT * (KROW + VROW + 8), VTILE = 32 * 128, PART = ROWS * 4 * D;
+  // wavefronts of a SIMD by the registers, and what LDS a wavefront then has
+  static constexpr int WAVES = RT == 1 ? 3 : 2, ROOM = 160 * 1024 / (4 * WAVES) - 2 * ROWS * 4 - 64;
+  static constexpr int STAGES = (ROOM - VTILE) / STAGEB < 1 ? 1 : ((ROOM - VTILE) / STAGEB > 4 ? 4 : (ROOM - VTILE) / STAGEB);
+  static constexpr int WAVEB = STAGES * STAGEB + VTILE > PART ? STAGES * STAGEB + VTILE : PART;
   static constexpr int STAT_OFF = NW * WAVEB, LDS = STAT_OFF + 2 * NW * ROWS * 4;
 };
 
 template <int D, bool F16, int KB, int VB, int RT>
-__device__ __forceinline__ void narrow_item(const QAttendArgs& a, const QItem& it, bool direct, char* smem) {
+__device__ __forceinline__ void narrow_segment(const QAttendArgs& a, const QAttendPlan& plan, const QSegment& it, char* smem) {
   typedef Narrow<D, KB, VB, RT> N;
-  constexpr int NW = N::NW, KT = N::KT, ROWS = N::ROWS, ROWB = N::ROWB, WAVEB = N::WAVEB;
-  constexpr int KS = D / 32, CT = D / 16;              // steps of the first product, tiles of channels of the second
-  constexpr int KROW = D * KB / 8, VROW = D * VB / 8, SROW = D / 32;  // bytes of a row
-  constexpr int KW = KROW / 16;                        // words of a key that a lane holds
-  constexpr int VPR = VROW / 16, VN = KT * VPR / 64, VCH = D / VPR;  // pieces of 16 bytes of a row, of a lane, and channels of one
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, l4 = lane >> 4;
+  constexpr int NW = N::NW, KT = N::KT, ROWS = N::ROWS, WAVEB = N::WAVEB, STAGES = N::STAGES, KROW = N::KROW, VROW = N::VROW, SROW = N::SROW;
+  constexpr int KS = D / 32, CT = D / 16, KU = KT / 16;  // steps of the first product, tiles of 16 channels, of 16 keys
+  constexpr int HG = D / 64, PK = KT / 32, GROUPS = HG * PK;  // V: groups of 64 channels, of 32 keys, and of both
+  constexpr int KW = KROW / 16, VW = VB;                // words that a lane holds of a key's quarter, of 32 channels of V
+  constexpr int V_OFF = KT * KROW, S_OFF = V_OFF + KT * VROW;  // in a stage: codes of K, of V, a word of scales a key of each
+  int tid = threadIdx.x;  // (hidden from the compiler: nothing that follows from it is to live across segments)
+  asm volatile("" : "+v"(tid));
+  const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, l4 = lane >> 4;
   const CacheView& cv = a.c.c;
+  char* const ring = smem + w * WAVEB;
+  char* const vt = ring + STAGES * N::STAGEB;
 
   bf16x8 Qf[RT][KS];
-  int lim_row[RT];  // the last key of this lane's row in the share
+  int lim_row[RT];  // the last key of this lane's row in the segment
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int r = 16 * rt + l16 < it.rows ? 16 * rt + l16 : it.rows - 1;  // (lanes past the end compute on a copy and store nothing)
-    const int q = (it.row0 + r) / a.G, lim = a.causal ? q + it.off : it.nk - 1;
+    const int q = (it.row0 + r) / a.G, lim = a.causal ? q + it.off : it.len - 1;
     lim_row[rt] = lim < it.end - 1 ? lim : it.end - 1;
-    const __bf16* qp = a.Q + out_row(a, it, r) * D + (D / 4) * l4;
+    const __bf16* qp = a.Q + out_row(a, it, r).at * D + (D / 4) * l4;
 #pragma unroll
     for (int s = 0; s < KS; ++s) Qf[rt][s] = *(const bf16x8*)(qp + 8 * s);
   }
-  const int lim_least = a.causal ? it.row0 / a.G + it.off : it.nk - 1;  // keys up to here: seen by all rows
+  const int lim_least = a.causal ? it.row0 / a.G + it.off : it.len - 1;  // keys up to here: seen by all rows
 
-  struct Raw {
-    uint32_t K[2][KW];
-    u32x4 V[VN];
-    uint32_t ks[2], vs[VN];
-  };
-  // Pages of this wavefront's tiles: lane i has the one of tile i of the next 64.
+  // ---- requests of a tile
+  const int t0 = it.begin + KT * w, tiles = t0 < it.end ? (it.end - t0 + NW * KT - 1) / (NW * KT) : 0;
   const int mask = (1 << cv.page_log2) - 1;
-  int pages = 0;
-  auto load = [&](int key0, Raw& x) {
+  int pages = 0;  // of this wavefront's tiles: lane i has the one of tile i of the next 64
+  unsigned koff[N::KN], voff[N::VN];  // where this lane's pieces of a whole tile are
+#pragma unroll
+  for (int u = 0; u < N::KN; ++u) koff[u] = code_offset<KROW>(u, lane, KT - 1);
+#pragma unroll
+  for (int u = 0; u < N::VN; ++u) voff[u] = code_offset<VROW>(u, lane, KT - 1);
+  auto request = [&](int i, int stage) {
+    const int key0 = t0 + i * (NW * KT);
     long row = ((long)it.s * cv.Hkv + it.g) * cv.Nk + key0;
     if (cv.table) {
-      const int i = (key0 - it.begin) / (NW * KT) & 63;
-      if (i == 0) {
+      if ((i & 63) == 0) {
         const int t = key0 + lane * (NW * KT);
         pages = cv.table[(long)it.s * cv.table_stride + ((t < it.end ? t : key0) >> cv.page_log2)];
+        touch(pages);
       }
-      row = (((long)__builtin_amdgcn_readlane(pages, i) * cv.Hkv + it.g) << cv.page_log2) + (key0 & mask);
+      row = (((long)__builtin_amdgcn_readlane(pages, i & 63) * cv.Hkv + it.g) << cv.page_log2) + (key0 & mask);
     }
     const int last = it.end - 1 - key0;  // (keys past the end repeat the last one)
-    const uint8_t *kc = a.c.Kc + row * KROW, *ks = a.c.Ks + row * SROW, *vc = a.c.Vc + row * VROW, *vs = a.c.Vs + row * SROW;
+    char* const to = ring + stage * N::STAGEB;
+    unsigned ko[N::KN], vo[N::VN];
+    int k = lane & (KT - 1);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int k = 16 * u + l16 < last ? 16 * u + l16 : last;
-      const uint32_t* from = (const uint32_t*)(kc + k * KROW + 4 * KW * l4);
+    for (int u = 0; u < N::KN; ++u) ko[u] = koff[u];
+#pragma unroll
+    for (int u = 0; u < N::VN; ++u) vo[u] = voff[u];
+    if (last < KT - 1) {
+      asm volatile("; keep this a branch" ::);
+#pragma unroll
+      for (int u = 0; u < N::KN; ++u) ko[u] = code_offset<KROW>(u, lane, last);
+#pragma unroll
+      for (int u = 0; u < N::VN; ++u) vo[u] = code_offset<VROW>(u, lane, last);
+      k = k < last ? k : last;
+    }
+    const uint8_t *kc = a.c.Kc + row * KROW, *vc = a.c.Vc + row * VROW;
+#pragma unroll
+    for (int u = 0; u < N::KN; ++u) dma16_uniform_once(kc, ko[u], to + 1024 * u);
+#pragma unroll
+    for (int u = 0; u < N::VN; ++u) dma16_uniform_once(vc, vo[u], to + V_OFF + 1024 * u);
+    if constexpr (SROW == 4) {
+      dma4((lane < 32 ? a.c.Ks : a.c.Vs) + row * SROW + k * SROW, to + S_OFF);
+    } else {
+      dma2(a.c.Ks + row * SROW + k * SROW, to + S_OFF);
+      dma2(a.c.Vs + row * SROW + k * SROW, to + S_OFF + 4 * KT);
+    }
+  };
+
+  // ---- a tile in registers: of keys 16 u + l16 quarter l4 of the channels of K; of V, group (b, h), of key 32 b + lane % 32 the channels
+  // 64 h + 32 (lane / 32) ..
+  uint32_t Kr[KU][KW], Vr[GROUPS][VW], ks[KU], vs[PK];
+  auto take = [&](int stage) {
+    const char* st = ring + stage * N::STAGEB;
+#pragma unroll
+    for (int u = 0; u < KU; ++u) {
+      const int k = 16 * u + l16;
       if constexpr (KW == 2) {
-        const u32x2 y = *(const u32x2*)from;
-        x.K[u][0] = y[0], x.K[u][1] = y[1];
+        const u32x2 y = *(const u32x2*)(st + k * KROW + 16 * ((l4 >> 1) ^ code_mix<KROW>(k)) + 8 * (l4 & 1));
+        Kr[u][0] = y[0], Kr[u][1] = y[1];
       } else {
 #pragma unroll
-        for (int j = 0; j < KW; j += 4) {
-          const u32x4 y = *(const u32x4*)(from + j);
-          x.K[u][j] = y[0], x.K[u][j + 1] = y[1], x.K[u][j + 2] = y[2], x.K[u][j + 3] = y[3];
+        for (int j = 0; j < KW / 4; ++j) {
+          const u32x4 y = *(const u32x4*)(st + k * KROW + 16 * ((l4 * (KW / 4) + j) ^ code_mix<KROW>(k)));
+          Kr[u][4 * j] = y[0], Kr[u][4 * j + 1] = y[1], Kr[u][4 * j + 2] = y[2], Kr[u][4 * j + 3] = y[3];
         }
       }
-      x.ks[u] = ks[k * SROW + l4 * SROW / 4];
+      ks[u] = *(const uint32_t*)(st + S_OFF + 4 * k);
     }
+    const int sub = lane >> 5;
 #pragma unroll
-    for (int u = 0; u < VN; ++u) {
-      const int i = 64 * u + lane, c = i % VPR, k = i / VPR < last ? i / VPR : last;
-      x.V[u] = *(const u32x4*)(vc + k * VROW + 16 * c);
-      x.vs[u] = vs[k * SROW + c * VCH / 32];
+    for (int v = 0; v < GROUPS; ++v) {
+      const int k = 32 * (v / HG) + (lane & 31);
+#pragma unroll
+      for (int j = 0; j < VW / 4; ++j) {
+        const u32x4 y = *(const u32x4*)(st + V_OFF + k * VROW + 16 * (((2 * (v % HG) + sub) * (VW / 4) + j) ^ code_mix<VROW>(k)));
+        Vr[v][4 * j] = y[0], Vr[v][4 * j + 1] = y[1], Vr[v][4 * j + 2] = y[2], Vr[v][4 * j + 3] = y[3];
+      }
+      if (v % HG == 0) vs[v / HG] = *(const uint32_t*)(st + S_OFF + 4 * (KT + k));
     }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   };
 
   f32x4 O[RT][CT];
@@ -133,35 +195,47 @@ __device__ __forceinline__ void narrow_item(const QAttendArgs& a, const QItem& i
     l[rt] = 0.f;
   }
   const float c2 = a.scale_log2e;
-  char* const vt = smem + w * WAVEB;
-  // this lane's places: writes of V, transposing reads
   const int vread = 4 * l4 + (l16 >> 2), vcol = (l16 & 3) >> 1, vhalf = 8 * (l16 & 1);
 
-  auto compute = [&](int key0, const Raw& x) {
+  auto compute = [&](int key0) {
     const bool edge = key0 + KT - 1 > lim_least || key0 + KT > it.end;
-    // ---- V through LDS. (Where some rows do not see a key that is NaN, its blocks go in as zeros and the rows that do see it get their NaN below.)
-    bool none[VN];
+    // (Where some rows do not see a key of V that is NaN, its blocks go in as zeros, and the rows that do see it get their NaN below.)
+    unsigned long long none[GROUPS];
+    uint32_t e[GROUPS];
 #pragma unroll
-    for (int u = 0; u < VN; ++u) {
-      const int i = 64 * u + lane, c = i % VPR, k = i / VPR, f = v_swizzle<D, VB>(k);
-      none[u] = edge && x.vs[u] == 255u;
-      const float s = mx_scale(none[u] ? 127u : x.vs[u]);
+    for (int v = 0; v < GROUPS; ++v) {
+      none[v] = 0ull;
+      e[v] = (vs[v / HG] >> (8 * (2 * (v % HG) + (lane >> 5)))) & 0xffu;
+    }
+    if (edge) {
 #pragma unroll
-      for (int j = 0; j < VCH / 8; ++j) {
-        const uint32_t w0 = VB == 4 ? x.V[u][j] : x.V[u][(2 * j) & 3], w1 = VB == 4 ? 0u : x.V[u][(2 * j + 1) & 3];
-        *(bf16x8*)(vt + k * ROWB + 16 * ((c * (VCH / 8) + j) ^ f)) = mx_decode8<VB, F16>(none[u] ? 0u : w0, none[u] ? 0u : w1, s);
+      for (int v = 0; v < GROUPS; ++v) {
+        const bool nan = e[v] == 255u;
+        none[v] = __builtin_amdgcn_ballot_w64(nan);
+        e[v] = nan ? 127u : e[v];
+#pragma unroll
+        for (int j = 0; j < VW; ++j) Vr[v][j] = nan ? 0u : Vr[v][j];
       }
     }
-    // ---- S^T = K Q^T
-    f32x4 S[RT][2];
+    auto put_v = [&](int v) {
+      const int k = lane & 31, sub = lane >> 5;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const float s = mx_scale(x.ks[u]);
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t w0 = VB == 4 ? Vr[v][j] : Vr[v][(2 * j) % VW], w1 = VB == 4 ? 0u : Vr[v][(2 * j + 1) % VW];
+        *(bf16x8*)(vt + k * 128 + 16 * ((4 * sub + j) ^ v_mix(k))) = mx_decode8<VB, F16>(w0, w1, mx_scale(e[v]));
+      }
+    };
+    put_v(0);
+    // ---- S^T = K Q^T
+    f32x4 S[RT][KU];
+#pragma unroll
+    for (int u = 0; u < KU; ++u) {
+      const float s = mx_scale((ks[u] >> (8 * (D == 128 ? l4 : l4 >> 1))) & 0xffu);
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) S[rt][u] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int t = 0; t < KS; ++t) {
-        const bf16x8 k = KB == 4 ? mx_decode8<KB, F16>(x.K[u][t], 0u, s) : mx_decode8<KB, F16>(x.K[u][(2 * t) % KW], x.K[u][(2 * t + 1) % KW], s);
+        const bf16x8 k = KB == 4 ? mx_decode8<KB, F16>(Kr[u][t], 0u, s) : mx_decode8<KB, F16>(Kr[u][(2 * t) % KW], Kr[u][(2 * t + 1) % KW], s);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) S[rt][u] = mfma16<F16>(k, Qf[rt][t], S[rt][u]);
       }
@@ -170,18 +244,18 @@ __device__ __forceinline__ void narrow_item(const QAttendArgs& a, const QItem& i
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < KU; ++u)
 #pragma unroll
           for (int r = 0; r < 4; ++r) S[rt][u][r] = key0 + 16 * u + 4 * l4 + r > lim_row[rt] ? -INFINITY : S[rt][u][r];
     }
     // ---- online softmax
-    bf16x8 P[RT];
+    bf16x8 P[RT][PK];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       auto advance = [&]() {
         float mx = S[rt][0][0];
 #pragma unroll
-        for (int i = 1; i < 8; ++i) mx = fmaxf(mx, S[rt][i / 4][i % 4]);
+        for (int i = 1; i < 4 * KU; ++i) mx = fmaxf(mx, S[rt][i / 4][i % 4]);
         const float m_new = fmaxf(m[rt], max_of_four(mx));
         const float alpha = m_new == -INFINITY ? 1.f : fast_exp2((m[rt] - m_new) * c2);
         l[rt] *= alpha;
@@ -189,13 +263,13 @@ __device__ __forceinline__ void narrow_item(const QAttendArgs& a, const QItem& i
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) O[rt][ct] *= alpha;
       };
-      f32x4 E[2];
+      f32x4 E[KU];
       float rs;
       auto exponentials = [&]() {
         const float ref = m[rt] == -INFINITY ? 0.f : m[rt] * c2;
         rs = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4 * KU; ++i) {
           E[i / 4][i % 4] = fast_exp2(__builtin_fmaf(S[rt][i / 4][i % 4], c2, -ref));
           rs += E[i / 4][i % 4];
         }
@@ -207,29 +281,40 @@ __device__ __forceinline__ void narrow_item(const QAttendArgs& a, const QItem& i
         exponentials();
       }
       l[rt] += rs;
-      u32x4 p;
-      p[0] = pack2<F16>(E[0][0], E[0][1]);
-      p[1] = pack2<F16>(E[0][2], E[0][3]);
-      p[2] = pack2<F16>(E[1][0], E[1][1]);
-      p[3] = pack2<F16>(E[1][2], E[1][3]);
-      P[rt] = __builtin_bit_cast(bf16x8, p);
+#pragma unroll
+      for (int b = 0; b < PK; ++b) {
+        u32x4 p;
+        p[0] = pack2<F16>(E[2 * b][0], E[2 * b][1]);
+        p[1] = pack2<F16>(E[2 * b][2], E[2 * b][3]);
+        p[2] = pack2<F16>(E[2 * b + 1][0], E[2 * b + 1][1]);
+        p[3] = pack2<F16>(E[2 * b + 1][2], E[2 * b + 1][3]);
+        P[rt][b] = __builtin_bit_cast(bf16x8, p);
+      }
     }
-    // ---- O^T += V^T P^T
-    asm volatile("" ::: "memory");
-    const int f = v_swizzle<D, VB>(vread);  // (keys 16 further on have the same)
+    // ---- O^T += V^T P^T, 64 channels of 32 keys at a time (LDS keeps a wavefront's order: the next ones are written behind the reads)
+    const int f = v_mix(vread);  // (keys 16 further on have the same)
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-      const int at = vread * ROWB + 16 * ((2 * ct + vcol) ^ f) + vhalf;
-      const bf16x8 v = lds_tr_pair(vt, at, at + 16 * ROWB);
+    for (int v = 0; v < GROUPS; ++v) {
+      asm volatile("" ::: "memory");
+      bf16x8 x[4];
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) O[rt][ct] = mfma16<F16>(v, P[rt], O[rt][ct]);
+      for (int c = 0; c < 4; ++c) {
+        const int at = vread * 128 + 16 * ((2 * c + vcol) ^ f) + vhalf;
+        x[c] = lds_tr_pair(vt, at, at + 16 * 128);
+      }
+      asm volatile("" ::: "memory");
+      if (v + 1 < GROUPS) put_v(v + 1);
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) O[rt][4 * (v % HG) + c] = mfma16<F16>(x[c], P[rt][v / HG], O[rt][4 * (v % HG) + c]);
     }
     asm volatile("" ::: "memory");
     if (edge) {
 #pragma unroll
-      for (int u = 0; u < VN; ++u)
-        for (unsigned long long b = __builtin_amdgcn_ballot_w64(none[u]); b; b &= b - 1) {
-          const int i = 64 * u + __builtin_ctzll(b), k = key0 + i / VPR, blk = i % VPR * VCH / 32;
+      for (int v = 0; v < GROUPS; ++v)
+        for (unsigned long long b = none[v]; b; b &= b - 1) {
+          const int i = __builtin_ctzll(b), k = key0 + 32 * (v / HG) + (i & 31), blk = 2 * (v % HG) + (i >> 5);
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -239,30 +324,33 @@ __device__ __forceinline__ void narrow_item(const QAttendArgs& a, const QItem& i
     }
   };
 
-  Raw A, B;
-  int t = it.begin + KT * w;
-  if (t < it.end) {
-    load(t, A);
-    while (true) {
-      if (t + NW * KT < it.end) load(t + NW * KT, B);
-      compute(t, A);
-      if ((t += NW * KT) >= it.end) break;
-      if (t + NW * KT < it.end) load(t + NW * KT, A);
-      compute(t, B);
-      if ((t += NW * KT) >= it.end) break;
+  if (tiles > 0) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int s = 0; s < KS; ++s) touch(Qf[rt][s]);
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i)
+      if (i < tiles) request(i, i);
+    for (int i = 0, stage = 0; i < tiles; ++i) {
+      if (STAGES > 1 && i + STAGES <= tiles) wait_vmem_upto<(STAGES - 1) * N::REQUESTS>();  // (all that are on their way but this one's)
+      else wait_vmem();
+      take(stage);
+      if (i + STAGES < tiles) request(i + STAGES, stage);
+      compute(t0 + i * (NW * KT));
+      stage = stage + 1 < STAGES ? stage + 1 : 0;
     }
   }
 
-  // ---- the wavefronts' partial results become the item's: rows of pieces of four channels, their places XOR-ed with the row
+  // ---- the wavefronts' partial results become the segment's: rows of pieces of four channels, their places XOR-ed with the row
   constexpr int CPR = D / 4;
   float lsum[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) lsum[rt] = sum_of_four(l[rt]);
-  __syncthreads();
   float* stat = (float*)(smem + N::STAT_OFF);
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    char* const mine = smem + w * WAVEB + (16 * rt + l16) * (4 * D);
+    char* const mine = ring + (16 * rt + l16) * (4 * D);
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) *(f32x4*)(mine + 16 * ((4 * ct + l4) ^ l16)) = O[rt][ct];
     if (l4 == 0) {
@@ -284,47 +372,51 @@ __device__ __forceinline__ void narrow_item(const QAttendArgs& a, const QItem& i
       den += wgt * stat[NW * ROWS + u * ROWS + r];
       o += *(const f32x4*)(smem + u * WAVEB + r * (4 * D) + 16 * (c ^ (r & 15))) * wgt;
     }
-    const float inv = den == 0.f ? 0.f : 1.f / den;  // (no visible key: L = -inf; a NaN stays one)
-    const float lse = den == 0.f ? -INFINITY : mm * a.scale + fast_log2(den) * kLn2;
-    const long at = out_row(a, it, r);
-    if (direct) {
-      if (den == 0.f) o = (f32x4){0.f, 0.f, 0.f, 0.f};
-      u32x2 x;
-      x[0] = pack2<F16>(o[0] * inv, o[1] * inv);
-      x[1] = pack2<F16>(o[2] * inv, o[3] * inv);
-      *(u32x2*)(a.O + at * D + 4 * c) = x;
-      if (c == 0) *lse_at(a, at) = lse;
-    } else {
-      const long all = (long)a.nseq * a.Nq * a.Hq;
-      *(f32x4*)(a.Opart + (it.slot * all + at) * D + 4 * c) = o * inv;
-      if (c == 0) a.Lpart[it.slot * all + at] = lse;
-    }
+    const float inv = den == 0.f ? 0.f : 1.f / den;  // (no visible key: O = 0, L = -inf; a NaN stays one)
+    put_row<F16>(a, plan, it, r, c, o * inv, den == 0.f ? -INFINITY : mm * a.scale + fast_log2(den) * kLn2);
   }
+  __syncthreads();
 }
 
-// Wavefronts of a SIMD: what registers allow
-constexpr int narrow_waves(int D, int bits, int RT) { return D == 64 ? (RT == 1 ? 4 : 3) : (RT == 1 && bits == 8 ? 3 : 2); }
 template <int D, bool F16, int KB, int VB, int RT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(narrow_waves(D, KB + VB, RT), narrow_waves(D, KB + VB, RT)))) void qattend_narrow_kernel(QAttendArgs a, QAttendPlan plan) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(Narrow<D, KB, VB, RT>::WAVES, Narrow<D, KB, VB, RT>::WAVES))) void qattend_narrow_kernel(
+    QAttendArgs a, QAttendPlan plan) {
   __shared__ __attribute__((aligned(1024))) char smem[Narrow<D, KB, VB, RT>::LDS];
-  const int blocks = (a.Nq * a.G + plan.rows - 1) / plan.rows, per = blocks * plan.shares;
-  const int pair = blockIdx.x / (unsigned)per, in = blockIdx.x - (unsigned)pair * per;
-  const QItem it = make_item(a, plan, pair, in / plan.shares, in % plan.shares);
-  const bool direct = plan.shares == 1;
-  if (it.begin >= it.end) return empty_item<D>(a, it, direct);
-  narrow_item<D, F16, KB, VB, RT>(a, it, direct, smem);
+  for_segments(a, plan, smem, [&](const QSegment& it) { narrow_segment<D, F16, KB, VB, RT>(a, plan, it, smem); });
 }
 
-template <int D, bool F16, int FLY>
-__global__ __launch_bounds__(256) void qattend_merge_kernel(QAttendArgs a, int slots) {
-  merge_slots<D, F16, FLY>(a.Opart, a.Lpart, a.O, a.LSE, (long)a.nseq * a.Nq * a.Hq, a.Hq, a.Nq, slots);
+// Units that several workgroups have parts of. ONE: a workgroup a row, for few units with many parts; else one for as many rows as it has
+// threads for.
+template <int D, bool F16, bool ONE>
+__global__ __launch_bounds__(256) void qattend_merge_kernel(QAttendArgs a, QAttendPlan p) {
+  __shared__ __attribute__((aligned(16))) char parts[ONE ? merge_split_lds<D>() : 16];
+  constexpr int AT_ONCE = 256 / (D / 4);
+  const int here = ONE ? p.rows : p.rows / AT_ONCE, unit = blockIdx.x / (unsigned)here, part = blockIdx.x % (unsigned)here;
+  const int pair = unit / p.blocks, row0 = (unit - pair * p.blocks) * p.rows;
+  const int rows = a.Nq * a.G - row0 < p.rows ? a.Nq * a.G - row0 : p.rows;
+  const QAttendArgs::Unit u = a.units[unit];
+  if (u.parts == 0) return;
+  auto slot = [&](int k) { return k == 0 ? 2 * u.first + 1 : 2 * (u.first + k); };
+  auto o_at = [&](int k, int r) { return (const float*)part_o(a, p, slot(k), r); };
+  auto l_at = [&](int k, int r) { return a.Lpart[(long)slot(k) * p.rows + r]; };
+  auto done = [&](int r, int c4, f32x4 o, float lse) {
+    QSegment it;
+    const int s = pair / a.c.c.Hkv;
+    it.s = s, it.g = pair - s * a.c.c.Hkv, it.tok0 = (long)s * a.Nq, it.row0 = row0, it.slot = -1;
+    put_row<F16>(a, p, it, r, c4, o, lse);
+  };
+  const int r = ONE ? part : part * AT_ONCE + (int)threadIdx.x / (D / 4);
+  if (r >= rows) return;
+  auto partial = [&](int k) { return o_at(k, r); };
+  auto logsum = [&](int k) { return l_at(k, r); };
+  auto finish = [&](int c4, f32x4 o, float lse) { done(r, c4, o, lse); };
+  if constexpr (ONE) merge_split<D>(parts, u.parts, partial, logsum, finish);
+  else merge_few<D, 4>(u.parts, partial, logsum, finish);
 }
 
 template <int D, bool F16, int KB, int VB>
 hipError_t launch_bits(const QAttendArgs& a, const QAttendPlan& plan, hipStream_t st) {
-  const long items = (long)a.nseq * a.c.c.Hkv * (((long)a.Nq * a.G + plan.rows - 1) / plan.rows) * plan.shares;
-  if (items > 0x7fffffffL) return hipErrorInvalidConfiguration;
-  const dim3 grid((unsigned)items), block(256);
+  const dim3 grid((unsigned)plan.groups), block(256);
   if (plan.rows == 16) hipLaunchKernelGGL((qattend_narrow_kernel<D, F16, KB, VB, 1>), grid, block, 0, st, a, plan);
   else hipLaunchKernelGGL((qattend_narrow_kernel<D, F16, KB, VB, 2>), grid, block, 0, st, a, plan);
   return hipGetLastError();
@@ -332,14 +424,13 @@ hipError_t launch_bits(const QAttendArgs& a, const QAttendPlan& plan, hipStream_
 template <int D, bool F16>
 hipError_t launch_type(const QAttendArgs& a, hipStream_t st) {
   const QAttendPlan plan = qattend_plan(a.nseq, a.Hq, a.c.c.Hkv, a.Nq, a.c.c.Nk, D);
-  const hipError_t e = plan.rows == 128 ? launch_qattend_wide(a, plan, st) : a.c.k_bits == 4 ? (a.c.v_bits == 4 ? launch_bits<D, F16, 4, 4>(a, plan, st) : launch_bits<D, F16, 4, 8>(a, plan, st))
-                                       : (a.c.v_bits == 4 ? launch_bits<D, F16, 8, 4>(a, plan, st) : launch_bits<D, F16, 8, 8>(a, plan, st));
-  const int slots = plan.shares;
-  if (e || slots == 1) return e;
-  constexpr int RPB = 256 / (D / 4);
-  const dim3 grid((unsigned)(((long)a.nseq * a.Nq * a.Hq + RPB - 1) / RPB));
-  if (slots <= 4) hipLaunchKernelGGL((qattend_merge_kernel<D, F16, 4>), grid, dim3(256), 0, st, a, slots);
-  else hipLaunchKernelGGL((qattend_merge_kernel<D, F16, 16>), grid, dim3(256), 0, st, a, slots);
+  const hipError_t e = plan.rows == 128 ? launch_qattend_wide(a, plan, st)
+                       : a.c.k_bits == 4 ? (a.c.v_bits == 4 ? launch_bits<D, F16, 4, 4>(a, plan, st) : launch_bits<D, F16, 4, 8>(a, plan, st))
+                                         : (a.c.v_bits == 4 ? launch_bits<D, F16, 8, 4>(a, plan, st) : launch_bits<D, F16, 8, 8>(a, plan, st));
+  if (e || plan.slots == 0) return e;
+  const long units = (long)a.nseq * a.c.c.Hkv * plan.blocks;
+  if (units * plan.rows <= 4 * plan.groups) hipLaunchKernelGGL((qattend_merge_kernel<D, F16, true>), dim3((unsigned)(units * plan.rows)), dim3(256), 0, st, a, plan);
+  else hipLaunchKernelGGL((qattend_merge_kernel<D, F16, false>), dim3((unsigned)(units * (plan.rows / (1024 / D)))), dim3(256), 0, st, a, plan);
   return hipGetLastError();
 }
 
@@ -349,12 +440,17 @@ QAttendPlan qattend_plan(int B, int Hq, int Hkv, int Nq, int Nk, int d) {
   QAttendPlan p;
   const long rows = (long)Nq * (Hq / Hkv);
   p.rows = rows <= 16 ? 16 : (rows <= 64 ? 32 : 128);
-  const long items = (long)B * Hkv * ((rows + p.rows - 1) / p.rows), blocks = ((long)Nk + 63) / 64;
-  long shares = (p.rows == 128 ? 512 : 768) / items;
-  shares = std::max(1l, std::min(std::min(shares, 128l), blocks / 4));
-  const long per = (blocks + shares - 1) / shares;
-  p.keys = (int)(64 * per);
-  p.shares = (int)((blocks + per - 1) / per);
+  p.blocks = (int)((rows + p.rows - 1) / p.rows);
+  const int chunk = p.rows == 128 ? 128 : 16384 / d;  // (narrow: a tile for each of four wavefronts)
+  p.chunk_log2 = chunk == 128 ? 7 : 8;
+  p.least = 256 / chunk;
+  p.groups = p.rows == 16 ? 768 : 512;
+  static const char *qt = getenv("QTOT"), *qm = getenv("QMIN");  // SWEEP
+  if (qt) p.groups = atoi(qt);
+  if (qm) p.least = atoi(qm);
+  const double units = (double)B * Hkv * p.blocks, chunks = units * ((Nk + chunk - 1) / chunk);
+  if (chunks < p.groups) p.groups = (int)chunks;
+  p.slots = Nk <= chunk ? 0 : 2 * p.groups;  // (a unit of one chunk is never shared)
   return p;
 }
 

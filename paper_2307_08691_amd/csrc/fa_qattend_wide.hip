@@ -1,5 +1,5 @@
-// Attention over a key/value cache held in 4 or 8 bits (fa_mx.h) for many rows a key/value head: chunks of prompts. An item is 128 packed rows
-// against a share of the keys; each of the four wavefronts has 32 rows, and they share tiles of 64 keys in LDS, which hold 16-bit elements:
+// Attention over a key/value cache held in 4 or 8 bits (fa_mx.h) for many rows a key/value head: chunks of prompts. A block is 128 packed rows,
+// against a segment of the keys (fa_qattend.h); each of the four wavefronts has 32 rows, and they share tiles of 64 keys in LDS, which hold 16-bit elements:
 // every thread converts a quarter of a key's channels of K and of V on the way from memory (one block of 32, or half of one), requested an
 // iteration earlier. The loop is that of the shared prefix's wide items (fa_prefix.hip): scores of the next tile beside the exponentials of
 // this one, then O^T += V^T P^T, operands requested a few products ahead. Two workgroups share a compute unit. Bound by the matrix units
@@ -21,12 +21,14 @@ struct Wide {
 };
 
 template <int D, bool F16, int KB, int VB>
-__device__ __forceinline__ void wide_item(const QAttendArgs& a, const QItem& it, bool direct, char* smem) {
+__device__ __forceinline__ void wide_segment(const QAttendArgs& a, const QAttendPlan& plan, const QSegment& it, char* smem) {
   typedef Wide<D> W;
   constexpr int BC = W::BC, ROWB = W::ROWB, TILEB = W::TILEB, V_OFF = W::V_OFF, KS = D / 16, DT = D / 32, AHEAD = 4;
   constexpr int CH = D / 4, CHUNKS = CH / 8, KW = CH * KB / 32, VW = CH * VB / 32;  // of a thread and tile: channels, 16-byte pieces of 16-bit ones, words
   const CacheView& cv = a.c.c;
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane & 31, hh = lane >> 5;
+  int tid = threadIdx.x;  // (hidden from the compiler: nothing that follows from it is to live across segments)
+  asm volatile("" : "+v"(tid));
+  const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane & 31, hh = lane >> 5;
   const int r0 = 32 * w, mine = r0 + lq;  // this lane's row of the item
   const int prow = mine < it.rows ? mine : it.rows - 1, q = (it.row0 + prow) / a.G;
   // this thread's part of a tile: 16 keys beside each other in 16 lanes, whose pieces then lie in different banks
@@ -38,19 +40,30 @@ __device__ __forceinline__ void wide_item(const QAttendArgs& a, const QItem& it,
     asm volatile("" : "+v"(ln));
     return Part{16 * w + (ln & 15), ln >> 4};
   };
-  const int lim = a.causal ? q + it.off : it.nk - 1, lim_end = lim < it.end - 1 ? lim : it.end - 1;
-  const int lim_least = a.causal ? (it.row0 + r0) / a.G + it.off : it.nk - 1;  // keys up to here: seen by all rows of the wavefront
-  const int lim_item = a.causal ? it.row0 / a.G + it.off : it.nk - 1;          // ... of the item
+  const int lim = a.causal ? q + it.off : it.len - 1, lim_end = lim < it.end - 1 ? lim : it.end - 1;
+  const int lim_least = a.causal ? (it.row0 + r0) / a.G + it.off : it.len - 1;  // keys up to here: seen by all rows of the wavefront
+  const int lim_item = a.causal ? it.row0 / a.G + it.off : it.len - 1;          // ... of the item
 
   const Part at = part();
   struct Raw {
     uint32_t k[KW], v[VW], ks, vs;
   };
   const int mask = (1 << cv.page_log2) - 1;
-  auto row_of = [&](int key0) {
-    if (!cv.table) return ((long)it.s * cv.Hkv + it.g) * cv.Nk + key0;
-    const int page = cv.table[(long)it.s * cv.table_stride + (key0 >> cv.page_log2)];
-    return (((long)page * cv.Hkv + it.g) << cv.page_log2) + (key0 & mask);
+  // Row in which the tile that K was last requested of begins; V of it is requested next. Pages: lane i has that of tile i of the next 64.
+  long row_k = 0;
+  int pages = 0;
+  auto next_row = [&](int key0) {
+    if (!cv.table) {
+      row_k = ((long)it.s * cv.Hkv + it.g) * cv.Nk + key0;
+      return;
+    }
+    const int i = (key0 - it.begin) / BC & 63;
+    if (i == 0) {
+      const int t = key0 + lane * BC;
+      pages = cv.table[(long)it.s * cv.table_stride + ((t < it.end ? t : key0) >> cv.page_log2)];
+      touch(pages);
+    }
+    row_k = (((long)__builtin_amdgcn_readlane(pages, i) * cv.Hkv + it.g) << cv.page_log2) + (key0 & mask);
   };
   auto words = [&](auto N, const uint8_t* from, uint32_t* to) {
     if constexpr (decltype(N)::value == 2) {
@@ -66,13 +79,14 @@ __device__ __forceinline__ void wide_item(const QAttendArgs& a, const QItem& it,
   };
   auto request_k = [&](int key0, Raw& x) {  // (keys past the end repeat the last one)
     const auto [tk, quarter] = part();
-    const long row = row_of(key0) + (tk < it.end - 1 - key0 ? tk : it.end - 1 - key0);
+    next_row(key0);
+    const long row = row_k + (tk < it.end - 1 - key0 ? tk : it.end - 1 - key0);
     words(std::integral_constant<int, KW>{}, a.c.Kc + row * (D * KB / 8) + quarter * (4 * KW), x.k);
     x.ks = a.c.Ks[row * (D / 32) + quarter * D / 128];
   };
   auto request_v = [&](int key0, Raw& x) {
     const auto [tk, quarter] = part();
-    const long row = row_of(key0) + (tk < it.end - 1 - key0 ? tk : it.end - 1 - key0);
+    const long row = row_k + (tk < it.end - 1 - key0 ? tk : it.end - 1 - key0);
     words(std::integral_constant<int, VW>{}, a.c.Vc + row * (D * VB / 8) + quarter * (4 * VW), x.v);
     x.vs = a.c.Vs[row * (D / 32) + quarter * D / 128];
   };
@@ -86,17 +100,21 @@ __device__ __forceinline__ void wide_item(const QAttendArgs& a, const QItem& it,
     }
   };
   // (Where some row does not see a key of the tile, blocks that are NaN go in as zeros, and the rows that see them get their NaN after the product.)
-  auto put_v = [&](const Raw& x, int key0, int stage) {
+  auto put_v = [&](Raw& x, int key0, int stage) {
     const int tk = at.key, quarter = at.quarter;
-    const bool none = (key0 + BC - 1 > lim_item || key0 + BC > it.end) && x.vs == 255u;
-    const float s = mx_scale(none ? 127u : x.vs);
+    if (key0 + BC - 1 > lim_item || key0 + BC > it.end) {
+      const bool none = x.vs == 255u;
+      x.vs = none ? 127u : x.vs;
+#pragma unroll
+      for (int j = 0; j < VW; ++j) x.v[j] = none ? 0u : x.v[j];
+      smem[W::FLAGS_OFF + stage * 4 * BC + 4 * tk + quarter] = none;
+    }
+    const float s = mx_scale(x.vs);
 #pragma unroll
     for (int j = 0; j < CHUNKS; ++j) {
-      const bf16x8 y = VB == 4 ? mx_decode8<VB, F16>(none ? 0u : x.v[j % VW], 0u, s)
-                               : mx_decode8<VB, F16>(none ? 0u : x.v[(2 * j) % VW], none ? 0u : x.v[(2 * j + 1) % VW], s);
+      const bf16x8 y = VB == 4 ? mx_decode8<VB, F16>(x.v[j % VW], 0u, s) : mx_decode8<VB, F16>(x.v[(2 * j) % VW], x.v[(2 * j + 1) % VW], s);
       *(bf16x8*)(smem + V_OFF + stage * TILEB + swz_off<ROWB>(tk, quarter * CHUNKS + j)) = y;
     }
-    smem[W::FLAGS_OFF + stage * 4 * BC + 4 * tk + quarter] = none;
   };
 
   Raw next;
@@ -104,7 +122,7 @@ __device__ __forceinline__ void wide_item(const QAttendArgs& a, const QItem& it,
   request_v(it.begin, next);
   bf16x8 Qf[KS];
   {
-    const __bf16* qp = a.Q + out_row(a, it, prow) * D + 8 * hh;
+    const __bf16* qp = a.Q + out_row(a, it, prow).at * D + 8 * hh;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) Qf[ks] = *(const bf16x8*)(qp + 16 * ks);
   }
@@ -218,53 +236,42 @@ __device__ __forceinline__ void wide_item(const QAttendArgs& a, const QItem& it,
   const float lsum = sum_with_partner32(l);
   const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
   const float lse = lsum == 0.f ? -INFINITY : m * a.scale + fast_log2(lsum) * kLn2;
-  const long all = (long)a.nseq * a.Nq * a.Hq;
   __syncthreads();  // everyone has read the last tiles
   char* const stage = smem + w * (32 * 4 * D);
-  if (direct) {
-    store_rows_via_lds<DT, F16>(stage, O, inv, [&](int r) { return a.O + out_row(a, it, r0 + r) * D; }, it.rows - r0, D, lane);
-    if (hh == 0 && mine < it.rows) *lse_at(a, out_row(a, it, mine)) = lse;
-    return;
-  }
-  constexpr int CPR = D / 4;  // 16-byte chunks of a row
+  if (it.slot < 0) {
+    store_rows_via_lds<DT, F16>(stage, O, inv, [&](int r) { return a.O + out_row(a, it, r0 + r).at * D; }, it.rows - r0, D, lane);
+    if (hh == 0 && mine < it.rows) a.LSE[out_row(a, it, mine).lse] = lse;
+  } else {
+    constexpr int CPR = D / 4;  // 16-byte chunks of a row
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) {
-      f32x4 o;
+      for (int r4 = 0; r4 < 4; ++r4) {
+        f32x4 o;
 #pragma unroll
-      for (int v = 0; v < 4; ++v) o[v] = O[dt][4 * r4 + v] * inv;
-      *(f32x4*)(stage + lq * (4 * D) + 16 * ((8 * dt + 2 * r4 + hh) ^ (lq & (CPR - 1)))) = o;
-    }
+        for (int v = 0; v < 4; ++v) o[v] = O[dt][4 * r4 + v] * inv;
+        *(f32x4*)(stage + lq * (4 * D) + 16 * ((8 * dt + 2 * r4 + hh) ^ (lq & (CPR - 1)))) = o;
+      }
 #pragma unroll 4
-  for (int i = 0; i < CPR / 2; ++i) {
-    const int r = (64 * i + lane) / CPR, c = lane & (CPR - 1);
-    const f32x4 o = *(const f32x4*)(stage + r * (4 * D) + 16 * (c ^ (r & (CPR - 1))));
-    if (r0 + r < it.rows) *(f32x4*)(a.Opart + (it.slot * all + out_row(a, it, r0 + r)) * D + 4 * c) = o;
+    for (int i = 0; i < CPR / 2; ++i) {
+      const int r = (64 * i + lane) / CPR, c = lane & (CPR - 1);
+      const f32x4 o = *(const f32x4*)(stage + r * (4 * D) + 16 * (c ^ (r & (CPR - 1))));
+      if (r0 + r < it.rows) *(f32x4*)(part_o(a, plan, it.slot, r0 + r) + 4 * c) = o;
+    }
+    if (hh == 0 && mine < it.rows) a.Lpart[(long)it.slot * plan.rows + mine] = lse;
   }
-  if (hh == 0 && mine < it.rows) a.Lpart[it.slot * all + out_row(a, it, mine)] = lse;
+  __syncthreads();
 }
 
 template <int D, bool F16, int KB, int VB>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void qattend_wide_kernel(QAttendArgs a, QAttendPlan plan) {
   __shared__ __attribute__((aligned(1024))) char smem[Wide<D>::LDS];
-  // The blocks of rows of one pair and share go to one XCD, whose L2 then holds their keys.
-  const int blocks = (a.Nq * a.G + plan.rows - 1) / plan.rows;
-  const int unit = blockIdx.x / (unsigned)blocks / kXcds * kXcds + blockIdx.x % kXcds, blk = blockIdx.x / kXcds % (unsigned)blocks;
-  if (unit >= a.nseq * a.c.c.Hkv * plan.shares) return;
-  const int pair = unit / plan.shares;
-  const QItem it = make_item(a, plan, pair, blk, unit - pair * plan.shares);
-  const bool direct = plan.shares == 1;
-  if (it.begin >= it.end) return empty_item<D>(a, it, direct);
-  wide_item<D, F16, KB, VB>(a, it, direct, smem);
+  for_segments(a, plan, smem, [&](const QSegment& it) { wide_segment<D, F16, KB, VB>(a, plan, it, smem); });
 }
 
 template <int D, bool F16>
 hipError_t launch_type(const QAttendArgs& a, const QAttendPlan& plan, hipStream_t st) {
-  const long blocks = ((long)a.Nq * a.G + plan.rows - 1) / plan.rows, units = (long)a.nseq * a.c.c.Hkv * plan.shares;
-  const long items = (units + kXcds - 1) / kXcds * kXcds * blocks;
-  if (items >= 1l << 24) return hipErrorInvalidConfiguration;
-  const dim3 grid((unsigned)items), block(256);
+  const dim3 grid((unsigned)plan.groups), block(256);
   if (a.c.k_bits == 4 && a.c.v_bits == 4) hipLaunchKernelGGL((qattend_wide_kernel<D, F16, 4, 4>), grid, block, 0, st, a, plan);
   else if (a.c.k_bits == 4) hipLaunchKernelGGL((qattend_wide_kernel<D, F16, 4, 8>), grid, block, 0, st, a, plan);
   else if (a.c.v_bits == 4) hipLaunchKernelGGL((qattend_wide_kernel<D, F16, 8, 4>), grid, block, 0, st, a, plan);

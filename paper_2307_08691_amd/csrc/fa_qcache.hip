@@ -67,21 +67,30 @@ hipError_t launch_qappend(const QAppendArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// ---- read. A workgroup takes kReadRows slots of a (sequence, head) pair; a thread eight channels of K and V at a time.
-constexpr int kReadRows = 64;
-template <int BITS, bool F16>
-__device__ __forceinline__ void read_piece(const uint8_t* codes, const uint8_t* scales, long row, int piece, int d, __bf16* out) {
-  const uint8_t* from = codes + (row * d + 8 * piece) * BITS / 8;
-  u32x2 w = {0u, 0u};
-  if constexpr (BITS == 4) w[0] = *(const uint32_t*)from;
-  else w = *(const u32x2*)from;
-  *(bf16x8*)out = mx_decode8<BITS, F16>(w[0], w[1], mx_scale(scales[row * (d / 32) + piece / 4]));
-}
-template <int KB, int VB, bool F16>
+// ---- read. A workgroup takes kReadRows slots of a (sequence, head) pair, a thread eight channels of K and V at a time and kFly of those on
+// their way together. (16 sequences of up to 4096 slots, 8 heads of 128, 4 bits, packed: READ_OLD us one by one, READ_NEW so.)
+constexpr int kReadRows = 64, kFly = 4;
+template <int BITS>
+struct Codes {
+  u32x2 w;
+  uint8_t e;
+  __device__ __forceinline__ void request(const uint8_t* codes, const uint8_t* scales, long row, int piece, int d) {
+    const uint8_t* from = codes + (row * d + 8 * piece) * BITS / 8;
+    if constexpr (BITS == 4) w[0] = *(const uint32_t*)from;
+    else w = *(const u32x2*)from;
+    e = scales[row * (d / 32) + piece / 4];
+  }
+  template <bool F16>
+  __device__ __forceinline__ bf16x8 values() const { return mx_decode8<BITS, F16>(w[0], BITS == 4 ? 0u : w[1], mx_scale(e)); }
+};
+// ONCE: results past the caches (kReadOnce bytes and more) are stored around them: READ_CACHED us through them, READ_NEW so.
+constexpr long kReadOnce = 32l << 20;
+template <int KB, int VB, bool F16, bool ONCE>
 __global__ __launch_bounds__(256) void qread_kernel(QReadArgs a, int tiles) {
   const CacheView& c = a.c.c;
-  const unsigned pair = blockIdx.x / (unsigned)tiles;
-  const int tile = (int)(blockIdx.x - pair * (unsigned)tiles), s = (int)(pair / (unsigned)c.Hkv), g = (int)pair - s * c.Hkv;
+  // (the heads of the same slots beside each other: their rows are neighbours in the output)
+  const unsigned part = blockIdx.x / (unsigned)c.Hkv;
+  const int g = (int)(blockIdx.x - part * (unsigned)c.Hkv), s = (int)(part / (unsigned)tiles), tile = (int)(part - (unsigned)s * (unsigned)tiles);
   long first = 0, row0, rows;  // the first slot, where its row goes, and how many rows there are room for
   if (a.cu) {
     row0 = a.cu[s];
@@ -93,29 +102,54 @@ __global__ __launch_bounds__(256) void qread_kernel(QReadArgs a, int tiles) {
     row0 = (long)s * a.N;
     rows = a.N;
   }
-  const int n = held_keys(c, s), cpr = c.d / 8;
-  const int i0 = tile * kReadRows;
-  for (int j = threadIdx.x; j < kReadRows * cpr; j += 256) {
-    const int i = i0 + j / cpr, piece = j % cpr;
-    const long slot = first + i;
-    if (i >= rows || slot < 0 || slot >= n) continue;
-    const long row = mx_row(c, s, g, (int)slot), at = ((row0 + i) * c.Hkv + g) * c.d + 8 * piece;
-    read_piece<KB, F16>(a.c.Kc, a.c.Ks, row, piece, c.d, a.K + at);
-    read_piece<VB, F16>(a.c.Vc, a.c.Vs, row, piece, c.d, a.V + at);
+  // rows of the tile that have a slot: lo .. hi - 1
+  const long i0 = (long)tile * kReadRows, n = held_keys(c, s);
+  const long lo = i0 > -first ? i0 : -first;
+  long hi = i0 + kReadRows < rows ? i0 + kReadRows : rows;
+  hi = hi < n - first ? hi : n - first;
+  if (lo >= hi) return;
+  const int cpr = c.d / 8, pieces = (int)(hi - lo) * cpr;
+  for (int j0 = threadIdx.x; j0 < pieces; j0 += 256 * kFly) {
+    Codes<KB> k[kFly];
+    Codes<VB> v[kFly];
+    long at[kFly];
+#pragma unroll
+    for (int u = 0; u < kFly; ++u) {
+      const int j = j0 + 256 * u < pieces ? j0 + 256 * u : j0, i = j / cpr, piece = j - i * cpr;
+      const long row = mx_row(c, s, g, (int)(first + lo + i));
+      k[u].request(a.c.Kc, a.c.Ks, row, piece, c.d);
+      v[u].request(a.c.Vc, a.c.Vs, row, piece, c.d);
+      at[u] = ((row0 + lo + i) * c.Hkv + g) * c.d + 8 * piece;
+    }
+#pragma unroll
+    for (int u = 0; u < kFly; ++u) {
+      if (j0 + 256 * u >= pieces) break;
+      const u32x4 x = __builtin_bit_cast(u32x4, k[u].template values<F16>()), y = __builtin_bit_cast(u32x4, v[u].template values<F16>());
+      if constexpr (ONCE) {
+        __builtin_nontemporal_store(x, (u32x4*)(a.K + at[u]));
+        __builtin_nontemporal_store(y, (u32x4*)(a.V + at[u]));
+      } else {
+        *(u32x4*)(a.K + at[u]) = x;
+        *(u32x4*)(a.V + at[u]) = y;
+      }
+    }
   }
 }
-template <bool F16>
-static hipError_t launch_qread_t(const QReadArgs& a, hipStream_t st) {
+template <int KB, int VB>
+static hipError_t launch_qread_b(const QReadArgs& a, hipStream_t st) {
   const long most = a.cu ? (a.total < a.c.c.Nk ? a.total : a.c.c.Nk) : a.N;
   const long tiles = (most + kReadRows - 1) / kReadRows, all = (long)a.nseq * a.c.c.Hkv * tiles;
-  if (all > 0x7fffffffL) return hipErrorInvalidConfiguration;
+  const bool once = (a.cu ? a.total : (long)a.nseq * a.N) * a.c.c.Hkv * a.c.c.d * 4 >= kReadOnce;
   const dim3 grid((unsigned)all), block(256);
-  if (a.c.k_bits == 4 && a.c.v_bits == 4) hipLaunchKernelGGL((qread_kernel<4, 4, F16>), grid, block, 0, st, a, (int)tiles);
-  else if (a.c.k_bits == 4) hipLaunchKernelGGL((qread_kernel<4, 8, F16>), grid, block, 0, st, a, (int)tiles);
-  else if (a.c.v_bits == 4) hipLaunchKernelGGL((qread_kernel<8, 4, F16>), grid, block, 0, st, a, (int)tiles);
-  else hipLaunchKernelGGL((qread_kernel<8, 8, F16>), grid, block, 0, st, a, (int)tiles);
+  if (a.f16 && once) hipLaunchKernelGGL((qread_kernel<KB, VB, true, true>), grid, block, 0, st, a, (int)tiles);
+  else if (a.f16) hipLaunchKernelGGL((qread_kernel<KB, VB, true, false>), grid, block, 0, st, a, (int)tiles);
+  else if (once) hipLaunchKernelGGL((qread_kernel<KB, VB, false, true>), grid, block, 0, st, a, (int)tiles);
+  else hipLaunchKernelGGL((qread_kernel<KB, VB, false, false>), grid, block, 0, st, a, (int)tiles);
   return hipGetLastError();
 }
-hipError_t launch_qread(const QReadArgs& a, hipStream_t st) { return a.f16 ? launch_qread_t<true>(a, st) : launch_qread_t<false>(a, st); }
+hipError_t launch_qread(const QReadArgs& a, hipStream_t st) {
+  if (a.c.k_bits == 4) return a.c.v_bits == 4 ? launch_qread_b<4, 4>(a, st) : launch_qread_b<4, 8>(a, st);
+  return a.c.v_bits == 4 ? launch_qread_b<8, 4>(a, st) : launch_qread_b<8, 8>(a, st);
+}
 
 }  // namespace fa
