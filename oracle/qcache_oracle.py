@@ -19,7 +19,9 @@ def quantise(x, bits):
     whole = np.isfinite(blocks).all(-1)
     top = np.abs(np.where(whole[..., None], blocks, 0)).max(-1)
     e = np.full(top.shape, 16)
-    for b in range(17, 255):  # the smallest power of two that is large enough
+    some = top[top > LARGEST[bits] * 2.0**(16 - 127)]
+    lo, hi = (int(np.floor(np.log2(x / LARGEST[bits]))) + 127 for x in (some.min(), some.max())) if some.size else (0, 0)
+    for b in range(max(17, lo), min(254, hi + 2) + 1):  # the smallest power of two that is large enough
         e = np.where(top > LARGEST[bits] * 2.0**(e - 127), b, e)
     y = np.where(whole[..., None], blocks / 2.0**(e[..., None] - 127), 0.0)
     g, a = grid(bits), np.abs(y)

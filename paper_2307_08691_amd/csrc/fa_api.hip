@@ -1330,7 +1330,7 @@ static bool qcache_fwd_sizes(int B, int Hq, int Hkv, int Nq, int Nk) {
 
 size_t fa_qcache_fwd_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int d) {
   if (!qcache_fwd_sizes(B, Hq, Hkv, Nq, Nk) || (d != 64 && d != 128)) return 0;
-  const fa::QAttendPlan p = fa::qattend_plan(B, Hq, Hkv, Nq, Nk, d);
+  const fa::QAttendPlan p = fa::qattend_plan(B, Hq, Hkv, Nq, Nk, d, 0);
   if (p.slots == 0) return 0;
   return round_up((size_t)p.slots * p.rows * (d + 1) * sizeof(float) + (size_t)B * Hkv * p.blocks * sizeof(fa::QAttendArgs::Unit), 256);
 }
@@ -1349,7 +1349,7 @@ int fa_qcache_fwd(const void* Q, const void* Kcodes, const void* Kscales, const 
   const size_t need = fa_qcache_fwd_workspace_bytes(B, Hq, Hkv, Nq, Nk, d);
   if (need && !workspace) return FA_ERR_NULL;
   if (workspace_bytes < need) return FA_ERR_WORKSPACE;
-  const fa::QAttendPlan p = fa::qattend_plan(B, Hq, Hkv, Nq, Nk, d);
+  const fa::QAttendPlan p = fa::qattend_plan(B, Hq, Hkv, Nq, Nk, d, 0);
   a.Q = (const __bf16*)Q;
   a.O = (__bf16*)O;
   a.LSE = LSE;

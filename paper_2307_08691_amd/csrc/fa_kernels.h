@@ -272,7 +272,7 @@ struct QAttendPlan {      // how the work is cut (a function of the sizes alone)
   int groups, least;      // workgroups, and the fewest chunks that one is started for
   int slots;              // places for partial results
 };
-QAttendPlan qattend_plan(int B, int Hq, int Hkv, int Nq, int Nk, int d);
+QAttendPlan qattend_plan(int B, int Hq, int Hkv, int Nq, int Nk, int d, int bits);  // bits: of K and V together (0: room for any)
 hipError_t launch_qattend(const QAttendArgs& a, hipStream_t st);
 
 // Queries and keys rotated by their positions (fa_rope.hip)

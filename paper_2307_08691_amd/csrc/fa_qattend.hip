@@ -13,7 +13,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cstdlib>
 #include <type_traits>
 
 #include "fa_lds.h"
@@ -62,10 +61,14 @@ __device__ __forceinline__ void dma2(const void* gaddr, const void* lds) {
   asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_ushort %0, off" ::"v"(gaddr), "s"(__builtin_amdgcn_readfirstlane(lds_address(lds))) : "memory");
 }
 
+// Keys of a tile: 64 where 32 would be 2 KB (their instructions beside the elements' own: 64 sequences of up to 4096 keys of 64, 4 bits, 29.4 us with
+// tiles of 32, 28.0 so; with 8 bits 16 x 16 heads of up to 4096: 17.2 and 18.9)
+constexpr int narrow_keys(int d, int bits) { return d == 64 && bits == 8 ? 64 : 32; }
 template <int D, int KB, int VB, int RT>
 struct Narrow {
-  static constexpr int NW = 4, KT = 4096 / D, ROWS = 16 * RT, KROW = D * KB / 8, VROW = D * VB / 8, SROW = D / 32;  // bytes of a row of codes, of scales
+  static constexpr int NW = 4, KT = narrow_keys(D, KB + VB), ROWS = 16 * RT, KROW = D * KB / 8, VROW = D * VB / 8, SROW = D / 32;  // bytes of a row of codes, of scales
   static constexpr int KN = KT * KROW / 1024, VN = KT * VROW / 1024, SN = KT / 32, REQUESTS = KN + VN + SN;  // of a tile
+  static_assert(KT == 32 || D == 64, "the scales of a tile: 64 words a request");
   static constexpr int STAGEB = KT * (KROW + VROW + 8), VTILE = 32 * 128, PART = ROWS * 4 * D;
   // wavefronts of a SIMD by the registers, and what LDS a wavefront then has
   static constexpr int WAVES = RT == 1 ? 3 : 2, ROOM = 160 * 1024 / (4 * WAVES) - 2 * ROWS * 4 - 64;
@@ -143,12 +146,11 @@ __device__ __forceinline__ void narrow_segment(const QAttendArgs& a, const QAtte
     for (int u = 0; u < N::KN; ++u) dma16_uniform_once(kc, ko[u], to + 1024 * u);
 #pragma unroll
     for (int u = 0; u < N::VN; ++u) dma16_uniform_once(vc, vo[u], to + V_OFF + 1024 * u);
-    if constexpr (SROW == 4) {
-      dma4((lane < 32 ? a.c.Ks : a.c.Vs) + row * SROW + k * SROW, to + S_OFF);
-    } else {
-      dma2(a.c.Ks + row * SROW + k * SROW, to + S_OFF);
-      dma2(a.c.Vs + row * SROW + k * SROW, to + S_OFF + 4 * KT);
-    }
+    // (scales: a word a key of K, then of V)
+    const uint8_t* const sc = (KT == 32 && lane >= 32 ? a.c.Vs : a.c.Ks) + row * SROW + k * SROW;
+    if constexpr (SROW == 4) dma4(sc, to + S_OFF);
+    else dma2(sc, to + S_OFF);
+    if constexpr (KT == 64) dma2(a.c.Vs + row * SROW + k * SROW, to + S_OFF + 4 * KT);
   };
 
   // ---- a tile in registers: of keys 16 u + l16 quarter l4 of the channels of K; of V, group (b, h), of key 32 b + lane % 32 the channels
@@ -423,7 +425,7 @@ hipError_t launch_bits(const QAttendArgs& a, const QAttendPlan& plan, hipStream_
 }
 template <int D, bool F16>
 hipError_t launch_type(const QAttendArgs& a, hipStream_t st) {
-  const QAttendPlan plan = qattend_plan(a.nseq, a.Hq, a.c.c.Hkv, a.Nq, a.c.c.Nk, D);
+  const QAttendPlan plan = qattend_plan(a.nseq, a.Hq, a.c.c.Hkv, a.Nq, a.c.c.Nk, D, a.c.k_bits + a.c.v_bits);
   const hipError_t e = plan.rows == 128 ? launch_qattend_wide(a, plan, st)
                        : a.c.k_bits == 4 ? (a.c.v_bits == 4 ? launch_bits<D, F16, 4, 4>(a, plan, st) : launch_bits<D, F16, 4, 8>(a, plan, st))
                                          : (a.c.v_bits == 4 ? launch_bits<D, F16, 8, 4>(a, plan, st) : launch_bits<D, F16, 8, 8>(a, plan, st));
@@ -436,21 +438,26 @@ hipError_t launch_type(const QAttendArgs& a, hipStream_t st) {
 
 }  // namespace
 
-QAttendPlan qattend_plan(int B, int Hq, int Hkv, int Nq, int Nk, int d) {
+// Short caches whose units all have a workgroup: nothing is cut, and no merge is launched (us, cut and whole: 96 sequences of up to 1024
+// keys, 16 heads on 4 of 64: 15.1 and 11.1; 8 of up to 1024, 8 on 2: 11.1 and 8.2; but 4 of up to 2048, 32 on 8 of 128: 10.9 and 17.2)
+constexpr int kWhole = 1024;
+QAttendPlan qattend_plan(int B, int Hq, int Hkv, int Nq, int Nk, int d, int bits) {
   QAttendPlan p;
   const long rows = (long)Nq * (Hq / Hkv);
   p.rows = rows <= 16 ? 16 : (rows <= 64 ? 32 : 128);
   p.blocks = (int)((rows + p.rows - 1) / p.rows);
-  const int chunk = p.rows == 128 ? 128 : 16384 / d;  // (narrow: a tile for each of four wavefronts)
-  p.chunk_log2 = chunk == 128 ? 7 : 8;
-  p.least = 256 / chunk;
-  p.groups = p.rows == 16 ? 768 : 512;
-  static const char *qt = getenv("QTOT"), *qm = getenv("QMIN");  // SWEEP
-  if (qt) p.groups = atoi(qt);
-  if (qm) p.least = atoi(qm);
-  const double units = (double)B * Hkv * p.blocks, chunks = units * ((Nk + chunk - 1) / chunk);
+  // As many workgroups as fit: three a compute unit, or two. Two stream as fast as three where a tile has 6 KB and more, and leave fewer
+  // parts to the merge (us at 512 and 768: 131072 keys of 128, 8 and 4 bits, one sequence, 32 heads on 8: 42.2 and 45.3; 16 sequences of up to
+  // 8192, 8 and 8: 35.0 and 35.5; but 64 of up to 8192, 4 and 4: 76.5 and 66.0; 64 of up to 4096 of 64 channels, 8 and 8: 39.3 and 34.7)
+  p.groups = p.rows == 16 && !(d == 128 && bits > 8) ? 768 : 512;
+  p.least = 1;
+  p.chunk_log2 = p.rows != 128 && bits && narrow_keys(d, bits) == 64 ? 8 : 7;  // (narrow: a tile for each of four wavefronts)
+  const double units = (double)B * Hkv * p.blocks;
+  if (p.rows != 128 && units <= 512 && Nk <= kWhole)  // (whatever the bits: the workspace is sized without them)
+    while ((1 << p.chunk_log2) < Nk) ++p.chunk_log2;
+  const double chunks = units * (((Nk - 1) >> p.chunk_log2) + 1);
   if (chunks < p.groups) p.groups = (int)chunks;
-  p.slots = Nk <= chunk ? 0 : 2 * p.groups;  // (a unit of one chunk is never shared)
+  p.slots = Nk <= 1 << p.chunk_log2 ? 0 : 2 * p.groups;  // (a unit of one chunk is never shared)
   return p;
 }
 

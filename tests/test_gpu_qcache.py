@@ -196,7 +196,10 @@ SHAPES = [
     (2, 5, 8, 2, 700, 256, [700, 33]),                        # 20 rows: the second tile of rows partly empty
     (2, 9, 8, 2, 200, 0, [200, 9]),                           # 36 rows: a block of 32 and one of four
     (2, 70, 4, 1, 500, 128, [500, 70]),                       # 280 rows under the causal rule
-    (150, 1, 2, 1, 70, 0, [(11 * i) % 71 for i in range(150)]),  # more sequences than are ranked by length
+    (150, 1, 2, 1, 70, 0, [(11 * i) % 71 for i in range(150)]),  # many short sequences, some of them empty
+    (3, 1, 4, 2, 1100, 64, [1100, 0, 1]),                     # caches that are cut, one of them empty
+    (300, 1, 2, 2, 300, 0, [(37 * i) % 300 * (i % 7 > 0) for i in range(300)]),  # more sequences than a workgroup has threads, runs over several
+    (2, 130, 4, 2, 1200, 64, [1200, 64]),                     # wide blocks, some of which see no key at all
 ]
 
 
@@ -292,14 +295,15 @@ def test_a_nan_in_a_query_stays_in_its_row():
 
 def test_nothing_behind_the_rows_is_written_and_the_workspace_is_as_large_as_it_says():
     r = rng(12)
-    for nq, slots in ((1, 2000), (5, 600), (40, 900), (1, 64)):
-        c = Cache(r, 2, slots, 2, 64, 0, [slots, 40], 4, 4)
-        Q = gpu(r.normal(size=(2, nq, 8, 64)), torch.bfloat16)
-        need = binding.fa_qcache_fwd_workspace_bytes(2, 8, 2, nq, slots, 64)
+    for B, nq, hq, hkv, slots, d, bits in ((2, 1, 8, 2, 2000, 64, 4), (2, 5, 8, 2, 1100, 64, 8), (2, 40, 8, 2, 900, 64, 4), (2, 1, 8, 2, 64, 64, 4),
+                                           (75, 1, 8, 8, 300, 128, 8), (75, 1, 8, 8, 300, 64, 4), (90, 1, 8, 8, 260, 128, 4), (3, 9, 4, 4, 3000, 128, 8)):
+        c = Cache(r, B, slots, hkv, d, 0, [slots, 40] + [slots - i for i in range(B - 2)], bits, bits)
+        Q = gpu(r.normal(size=(B, nq, hq, d)), torch.bfloat16)
+        need = binding.fa_qcache_fwd_workspace_bytes(B, hq, hkv, nq, slots, d)
         ws = torch.full((need + 4096,), 0x5a, dtype=torch.uint8, device="cuda")
-        O = torch.full((2 * nq * 8 * 64 + 512,), 3.0, dtype=torch.bfloat16, device="cuda")
-        L = torch.full((2 * nq * 8 + 512,), 3.0, device="cuda")
-        o, l = O[:-512].view(2, nq, 8, 64), L[:-512].view(2, 8, nq)
+        O = torch.full((B * nq * hq * d + 512,), 3.0, dtype=torch.bfloat16, device="cuda")
+        L = torch.full((B * nq * hq + 512,), 3.0, device="cuda")
+        o, l = O[:-512].view(B, nq, hq, d), L[:-512].view(B, hq, nq)
         binding.fa_qcache_fwd(Q, c.q, 0.125, True, O=o, LSE=l, workspace=ws, **c.more)
         eO, eL = binding.fa_qcache_fwd(Q, c.q, 0.125, True, **c.more)
         assert torch.equal(o, eO) and torch.equal(l, eL)
@@ -354,3 +358,71 @@ def test_past_two_gigabytes():
     c = Cache.__new__(Cache)
     c.q, c.rows, c.more = q, rows, dict(seqlens_k=ints(lens), block_table=table)
     check("bf16", d, 2, 1, 4, hkv, 512, page, lens, 8, 4, cache=c)
+
+
+def test_a_layer_of_a_decoding_batch_in_a_graph():
+    """Rotate, quantise into the cache, attend, read back: captured once and replayed with other work between the replays, a step further each
+    time. Every replay is the eager run of the same state."""
+    r = rng(18)
+    B, hq, hkv, d, page, per = 3, 8, 2, 64, 64, 24
+    table = ints(r.permutation(B * per).reshape(B, per).tolist())
+    lens, pos = ints([1400, 63, 1]), ints([[1399], [62], [0]])
+    f = torch.tensor([10000.0**(-i / 32) for i in range(32)], device="cuda")
+    cache = binding.qcache(B * per, hkv, page, d, 8, 4)
+    prompt = [gpu(r.normal(size=(B, 1400, hkv, d)), torch.bfloat16) for _ in range(2)]
+    binding.fa_qcache_append(*prompt, cache, seqlens_k=lens, block_table=table)
+    qkv = gpu(r.normal(size=(B, 1, hq + 2 * hkv, d)), torch.bfloat16)
+    back = [torch.zeros((B, 16, hkv, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    first = ints([0, 0, 0])
+
+    def step(cache):
+        q, k = binding.fa_rope_fwd(qkv[:, :, :hq], qkv[:, :, hq:hq + hkv], pos, f)
+        kr, vr = torch.empty_like(k), torch.empty_like(k)
+        binding.fa_qcache_append(k, qkv[:, :, hq + hkv:], cache, seqlens_k=lens, block_table=table, Kout=kr, Vout=vr)
+        O, L = binding.fa_qcache_fwd(q, cache, 0.125, True, seqlens_k=lens, block_table=table)
+        binding.fa_qcache_read(cache, *back, seqlens_k=lens, block_table=table, first=first)
+        return q, kr, vr, O, L
+
+    twin = binding.QCache(*(t.clone() for t in cache))
+    step(binding.QCache(*(t.clone() for t in cache)))
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = step(cache)
+    for t, was in zip(cache, twin):  # (capturing runs nothing; the graph's cache is as it was)
+        assert torch.equal(t, was)
+    for i in range(4):
+        qkv.copy_(gpu(r.normal(size=tuple(qkv.shape)), torch.bfloat16))
+        lens += 1
+        pos += 1
+        first.copy_(lens - 16)
+        g.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (*out, *cache, *back)]
+        want = [*step(twin), *twin, *back]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+
+
+@pytest.mark.parametrize("k_bits,v_bits", [(4, 4), (8, 8)])
+def test_a_prompt_sees_what_later_steps_see(k_bits, v_bits):
+    """The values that append returns are those that attention over the cache uses: a prompt through fa_fwd on them, its cache through
+    fa_qcache_fwd, and its cache read back through fa_varlen_cross_fwd, agree to the rounding of O and P (e of |O| twice, e of p |v| twice)."""
+    r = rng(19)
+    B, n, hq, hkv, d = 2, 300, 8, 2, 64
+    Q = gpu(r.normal(size=(B, n, hq, d)), torch.bfloat16)
+    K, V = (gpu(r.normal(size=(B, n, hkv, d)), torch.bfloat16) for _ in range(2))
+    cache = binding.qcache(B, hkv, n, d, k_bits, v_bits)
+    binding.fa_qcache_append(K, V, cache, Kout=K, Vout=V)
+    O, L = binding.fa_qcache_fwd(Q, cache, 0.125, True)
+    O2, L2 = binding.fa_fwd(Q, K, V, 0.125, True)
+    k, v = (torch.zeros((B * n, hkv, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    cu = ints([0, n, 2 * n])
+    binding.fa_qcache_read(cache, k, v, cu_seqlens=cu)
+    assert torch.equal(k.view(B, n, hkv, d), K) and torch.equal(v.view(B, n, hkv, d), V)
+    O3, L3 = binding.fa_varlen_cross_fwd(Q.view(B * n, hq, d), k, v, cu, cu, n, n, 0.125, True)
+    _, _, A, M = dec.prefix_forward(f64(Q), np.zeros((0, hkv, d)), np.zeros((0, hkv, d)), f64(K), f64(V), [n, n], 0.125, True)
+    for o, l in ((O2, L2), (O3.view(B, n, hq, d), L3.view(hq, B, n).transpose(0, 1))):
+        score = 2 * (M * d / 2**24 + (M + np.abs(f64(L)) + 8) / 2**21)
+        assert (np.abs(f64(l) - f64(L)) <= score).all()
+        assert (np.abs(f64(o) - f64(O)) <= 2 * 2.0**-8 * (A + np.abs(f64(O))) * (1 + 2.0**-7) + A * 8 * score.transpose(0, 2, 1)[..., None]).all()

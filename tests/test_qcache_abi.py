@@ -21,7 +21,7 @@ def read(Kc=P, Ks=P, Vc=P, Vs=P, K=P, V=P, lens=P, tab=0, first=0, cu=0, B=2, Hk
     return fa.fa_qcache_read_raw(Kc, Ks, Vc, Vs, K, V, lens, tab, first, cu, B, Hkv, N, Nk, d, kb, vb, page, pages, type)
 
 
-def attend(Q=P, Kc=P, Ks=P, Vc=P, Vs=P, lens=P, tab=0, O=P, L=P, ws=P, nb=BIG, B=2, Hq=8, Hkv=2, Nq=1, Nk=1000, d=64, kb=4, vb=8, page=0,
+def attend(Q=P, Kc=P, Ks=P, Vc=P, Vs=P, lens=P, tab=0, O=P, L=P, ws=P, nb=BIG, B=2, Hq=8, Hkv=2, Nq=1, Nk=4000, d=64, kb=4, vb=8, page=0,
            pages=0, scale=0.1, type=fa.FA_TYPE_BF16):
     return fa.fa_qcache_fwd_raw(Q, Kc, Ks, Vc, Vs, lens, tab, O, L, ws, nb, B, Hq, Hkv, Nq, Nk, d, kb, vb, page, pages, scale, True, type)
 
@@ -77,8 +77,26 @@ def test_attend_refusals():
         assert attend(**bad) == fa.FA_ERR_SHAPE, bad
     for bad in PAGES + [dict(d=96), dict(d=256), dict(d=32), dict(type=fa.FA_TYPE_F32), dict(type=-1)]:
         assert attend(**bad) == fa.FA_ERR_UNSUPPORTED, bad
-    need = fa.fa_qcache_fwd_workspace_bytes(2, 8, 2, 1, 1000, 64)
+    need = fa.fa_qcache_fwd_workspace_bytes(2, 8, 2, 1, 4000, 64)
     assert need > 0 and attend(nb=need - 1) == fa.FA_ERR_WORKSPACE and attend(ws=0) == fa.FA_ERR_NULL
+    for bad in (dict(B=0), dict(Hq=7), dict(Nq=0), dict(Nk=0), dict(d=96), dict(Nk=(1 << 30) + 1), dict(B=1 << 20, Nq=64)):
+        x = dict(B=2, Hq=8, Hkv=2, Nq=1, Nk=4000, d=64, **{k: v for k, v in bad.items() if k not in ("B", "Hq", "Nq", "Nk", "d")})
+        x.update(bad)
+        assert fa.fa_qcache_fwd_workspace_bytes(*x.values()) == 0, bad
+    # more chunks of keys than are counted in 31 bits
+    assert attend(B=64, Hq=1 << 10, Hkv=1 << 4, Nq=1 << 10, Nk=1 << 30) == fa.FA_ERR_SHAPE
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_workspace_needs(d):
+    """None where nothing can be cut: caches of a chunk, and of up to 1024 keys while every head of every sequence has a workgroup of its own;
+    else places for two parts of each workgroup, however long the caches are."""
+    need = lambda B, Hkv, Nq, Nk: fa.fa_qcache_fwd_workspace_bytes(B, Hkv, Hkv, Nq, Nk, d)  # noqa: E731
+    assert need(4, 8, 1, 1024) == need(64, 8, 1, 1024) == need(1000, 8, 1, 128) == need(1, 1, 200, 128) == 0
+    assert need(4, 8, 1, 1025) > 0 and need(65, 8, 1, 1024) > 0 and need(1, 1, 200, 129) > 0
+    assert need(64, 8, 1, 1 << 20) - need(64, 8, 1, 8192) == 0
+    assert need(64, 8, 1, 1 << 20) <= 2 * 768 * 16 * (d + 1) * 4 + 64 * 8 * 8 + 256
+    assert need(64, 8, 200, 1 << 20) <= 2 * 512 * 128 * (d + 1) * 4 + 2 * 64 * 8 * 8 + 256
 
 
 @pytest.mark.parametrize("inverse", [False, True])
