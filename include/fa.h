@@ -664,11 +664,13 @@ int fa_qcache_read(const void* Kcodes, const void* Kscales, const void* Vcodes, 
  * Forward against such a cache: fa_kvcache_fwd over the values that codes and scales stand for. Q, O [B, Nq, Hq, d], LSE [B, Hq, Nq],
  * lengths, causal rule (query r at position r + seqlens_k[b] - Nq) and rows that see no key (O = 0, LSE = -inf) as there; any Nq. Keys and
  * values that a query does not see do not touch its result, also where their blocks are NaN (e = 255); E4M3's own NaN codes, which
- * fa_qcache_append never writes, have to lie in keys that all queries of the sequence see. NaN in a query, in a key that it sees or in
- * that key's value reaches the row's result. d in {64, 128}; B * Nq * Hq at most 2^26, Hkv at most 2^16 (FA_ERR_SHAPE beyond). How the keys are cut
- * over workgroups goes by the sizes alone, so results are the same bits in every run; `workspace` (partial results, float32; 16-byte
- * aligned) needs fa_qcache_fwd_workspace_bytes() bytes, undefined on entry and return; where that is 0 it may be NULL. type: of Q and O, FA_TYPE_BF16
- * or FA_TYPE_F16. Forward only, as fa_kvcache_fwd.
+ * fa_qcache_append never writes, and values past half precision's range have to lie in keys that all queries of the sequence see. NaN in a
+ * query, in a key that it sees or in that key's value reaches the row's result. d in {64, 128}; B * Nq * Hq at most 2^26, Hkv at most 2^16,
+ * B * Hkv * (Nq * Hq / Hkv / 16 + 1) * (Nk / 128 + 1) below 2^31 (FA_ERR_SHAPE beyond). The keys that there are, by seqlens_k, are dealt to the
+ * workgroups in equal runs: results are the same bits in every run, but a sequence's bits depend on the lengths of the others (float32
+ * sums cut elsewhere). `workspace` (partial results, float32; 16-byte aligned) needs fa_qcache_fwd_workspace_bytes() bytes, undefined on entry
+ * and return; where that is 0 it may be NULL. It grows with the batch up to 25 MB (Nq * Hq / Hkv up to 64) or 68 MB, not with the caches.
+ * type: of Q and O, FA_TYPE_BF16 or FA_TYPE_F16. Forward only, as fa_kvcache_fwd.
  */
 size_t fa_qcache_fwd_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int d);
 int fa_qcache_fwd(const void* Q, const void* Kcodes, const void* Kscales, const void* Vcodes, const void* Vscales, const int32_t* seqlens_k,
@@ -684,7 +686,7 @@ int fa_qcache_fwd(const void* Q, const void* Kcodes, const void* Kscales, const 
  * Q [B, N, Hq, d] -> Qout, and in the same launch K [B, N, Hkv, d] -> Kout (K NULL: Q alone; Hkv is ignored): element (b, i, h, t) at b *
  * batch_stride + i * token_stride + h * head_stride + t, `strides` (HOST array, elements) holding those three of Q, Qout, K, Kout in turn.
  * An output may be its input (the same strides). positions: DEVICE int32, axis x, sequence b, token i at positions[x * axis_stride + b * batch_stride + i];
- * any values, negative ones too. inv_freq: DEVICE float32 [pairs], finite. axis: DEVICE int32 [pairs] (clamped into 0 .. axes - 1; nullptr: 0). type:
+ * any values, negative ones too. inv_freq: DEVICE float32 [pairs], finite (up to 1 for the accuracy said). axis: DEVICE int32 [pairs] (clamped into 0 .. axes - 1; nullptr: 0). type:
  * FA_TYPE_*. Tensors aligned to their elements (16 bytes, with strides of as many, is fastest). d a multiple of 8 up to 256, 1 <= pairs,
  * 2 * pairs <= d, 1 <= axes; B * N below 2^31, Hq + Hkv at most 2^20. Packed batches: B = 1, N the tokens of all sequences.
  */

@@ -95,7 +95,7 @@ __device__ __forceinline__ void merge_few(int slots, P partial, L logsum, F done
 
 // ... by a whole workgroup of 256, for many slots: groups of D / 4 threads take them in turn, each with a running maximum of its own, and
 // join through LDS. (One sequence, 32 heads, 94 slots of 128 columns: 27 us by merge_slots, whose four workgroups go over the slots one
-// after the other, SPLIT_US so.)
+// after the other, 5.2 us so.)
 template <int D>
 constexpr int merge_split_lds() { return 256 * 16 + (1024 / D) * 4; }
 template <int D, class P, class L, class F>

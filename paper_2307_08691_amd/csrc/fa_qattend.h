@@ -6,7 +6,7 @@
 // segment by segment, a segment being the part of a unit that lies in it. A unit that is one workgroup's alone is finished there; of the others
 // each workgroup leaves a normalised partial O and its logsumexp, and the merge joins them (fa_merge.h). A workgroup has two partial segments at
 // most: the first, that begins inside a unit (slot 2 w), and the last, that begins a unit (slot 2 w + 1).
-// (64 paged sequences of up to 8192 keys, 32 heads on 8 of 128: CUT_OLD us with equal shares of the cache, longest sequence first, CUT_NEW so.)
+// (64 paged sequences of up to 8192 keys, 32 heads on 8 of 128, 4 bits: 69 us with equal shares of each sequence, the longest first, 64 so.)
 #pragma once
 #include "fa_mx.h"
 

@@ -219,6 +219,14 @@ def test_attend_without_causal_rule_and_with_more_queries_than_keys(nq, lens, d)
         check("f16", d, 3, nq, 4, 2, 128, 64, lens, 8, 4, causal=causal)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("k_bits,v_bits", BITS)
+def test_attend_with_groups_of_five_and_slabs_of_odd_lengths(d, k_bits, v_bits):
+    check("bf16", d, 3, 1, 10, 2, 301, 0, [301, 7, 150], k_bits, v_bits)
+    check("f16", d, 3, 7, 10, 2, 301, 0, [301, 7, 150], k_bits, v_bits)
+    check("bf16", d, 3, 30, 10, 2, 1277, 0, [1277, 3, 640], k_bits, v_bits)  # wide blocks
+
+
 EDGES = [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 159, 160, 161, 255, 256, 257, 287, 288, 289, 383, 384, 385, 511, 512, 513, 699]
 
 
