@@ -1378,6 +1378,7 @@ def _qcache(cache, B, Nk, table, dev):
         raise ValueError("codes and scales must be [B, Hkv, Nk, bytes] or [pages, Hkv, page_size, bytes]")
     x.d = 32 * Ks.shape[3]
     lead = tuple(Kc.shape[:3])
+    _counted(lead, "the cache")
     bits = {x.d // 2: 4, x.d: 8}
     for t, nm in ((Kc, "Kcodes"), (Vc, "Vcodes")):
         if t.shape[-1] not in bits:
@@ -1403,6 +1404,12 @@ def _qcache(cache, B, Nk, table, dev):
     return x
 
 
+def _counted(shape, name):
+    """(The library counts sequences, heads and rows in 32 bits.)"""
+    if any(n >= 2**31 for n in shape):
+        raise ValueError(f"{name} has a dimension of 2**31 or more: {tuple(shape)}")
+
+
 def _type16(t, name):
     import torch
     if t.dtype not in (torch.bfloat16, torch.float16):
@@ -1414,6 +1421,7 @@ def _row_strides(t, name, shape, dtype, dev, unit):
     """Strides of a tensor [B, N, H, d] whose rows are dense and lie a multiple of `unit` elements apart."""
     if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != dev:
         raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)} on {dev}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    _counted(shape, name)
     # (a dimension of one has no say)
     s = [0 if n == 1 else v for n, v in zip(t.shape[:3], t.stride()[:3])]
     if t.stride(3) != 1 and t.shape[3] > 1 or any(v % unit for v in s) or any(v < 0 for v in s):
@@ -1474,6 +1482,7 @@ def fa_qcache_read(cache, K, V, seqlens_k=None, block_table=None, max_seqlen_k: 
         raise ValueError(f"the cache holds {x.Hkv} heads of {x.d}, K is {tuple(K.shape)}")
     _need(K, "K", K.dtype)
     _need(V, "V", K.dtype, tuple(K.shape), dev)
+    _counted(K.shape, "K")
     for t, nm in ((seqlens_k, "seqlens_k"), (first, "first")):
         if t is not None:
             _need(t, nm, torch.int32, (B,), dev)
@@ -1496,6 +1505,7 @@ def fa_qcache_fwd(Q, cache, scale: float, causal: bool, seqlens_k=None, block_ta
     _need(Q, "Q")
     if Q.dim() != 4:
         raise ValueError("Q must be [B, Nq, Hq, d]")
+    _counted(Q.shape, "Q")
     B, Nq, Hq, d = Q.shape
     dev = Q.device
     x = _qcache(cache, B, max_seqlen_k, block_table, dev)

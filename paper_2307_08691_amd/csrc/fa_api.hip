@@ -1324,8 +1324,11 @@ int fa_qcache_read(const void* Kcodes, const void* Kscales, const void* Vcodes, 
 }
 
 static bool qcache_fwd_sizes(int B, int Hq, int Hkv, int Nq, int Nk) {
-  return B > 0 && Hq > 0 && Hkv > 0 && Hq % Hkv == 0 && Nq > 0 && Nk > 0 && Nk <= FA_CACHE_MAX_SLOTS && Hkv <= (1 << 16) &&
-         (double)B * Nq * Hq <= (1 << 26) && (double)B * Hkv * (((double)Nq * (Hq / Hkv)) / 16 + 1) * (Nk / 128 + 1) < (double)0x7fffffff;
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || Nq <= 0 || Nk <= 0 || Nk > FA_CACHE_MAX_SLOTS || Hkv > (1 << 16)) return false;
+  // (rows as the blocks have them: the merge's grid goes by these, and threads of a grid are counted in 32 bits)
+  const long rows = (long)Nq * (Hq / Hkv), block = rows <= 16 ? 16 : (rows <= 64 ? 32 : 128);
+  return (double)B * Hkv * (double)((rows + block - 1) / block * block) <= (double)(1 << 26) &&
+         (double)B * Hkv * ((double)rows / 16 + 1) * (Nk / 128 + 1) < (double)0x7fffffff;
 }
 
 size_t fa_qcache_fwd_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int d) {

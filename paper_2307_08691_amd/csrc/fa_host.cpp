@@ -607,6 +607,12 @@ bool current_stream_of(c10::Device dev, void*& st) {
   if (PyErr_Occurred()) return false;
   return index == dev.index();
 }
+// (the library counts sequences, heads and rows in 32 bits)
+bool counted(const at::Tensor* t) {
+  for (int64_t n : t->sizes())
+    if (n > INT_MAX) return false;
+  return true;
+}
 int type16(at::ScalarType t) { return t == at::kBFloat16 ? FA_TYPE_BF16 : (t == at::kHalf ? FA_TYPE_F16 : -1); }
 
 // (Kcodes, Kscales, Vcodes, Vscales) and a table: as binding._qcache
@@ -618,7 +624,7 @@ struct QCache {
     if (!PyTuple_Check(cache) || PyTuple_GET_SIZE(cache) != 4 || !integer(most, Nk) || Nk < 0) return false;
     for (int i = 0; i < 4; ++i) {
       t[i] = plain(PyTuple_GET_ITEM(cache, i));
-      if (!t[i] || t[i]->dim() != 4 || t[i]->scalar_type() != at::kByte || t[i]->device() != dev) return false;
+      if (!t[i] || t[i]->dim() != 4 || t[i]->scalar_type() != at::kByte || t[i]->device() != dev || !counted(t[i])) return false;
     }
     if (t[1]->size(3) > 1 << 20) return false;
     d = 32 * (int)t[1]->size(3), Hkv = (int)t[0]->size(1);
@@ -658,7 +664,7 @@ PyObject* qcache_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
   if (nargs != 8 || !plain_context()) Py_RETURN_NONE;
   const at::Tensor *K = strided(args[0]), *V = strided(args[1]), *Ko = nullptr, *Vo = nullptr;
-  if (!K || !V || K->dim() != 4) Py_RETURN_NONE;
+  if (!K || !V || K->dim() != 4 || !counted(K)) Py_RETURN_NONE;
   const at::ScalarType et = K->scalar_type();
   const c10::Device dev = K->device();
   const int type = type16(et), B = (int)K->size(0), Nq = (int)K->size(1), Hkv = (int)K->size(2), d = (int)K->size(3);
@@ -694,7 +700,7 @@ PyObject* qcache_read(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
   if (nargs != 8 || !plain_context()) Py_RETURN_NONE;
   const at::Tensor *K = plain(args[1]), *V = plain(args[2]), *cu = nullptr;
-  if (!K || K->dim() < 3) Py_RETURN_NONE;
+  if (!K || K->dim() < 3 || !counted(K)) Py_RETURN_NONE;
   const at::ScalarType et = K->scalar_type();
   const c10::Device dev = K->device();
   const int type = type16(et), dims = args[7] == Py_None ? 4 : 3;
@@ -734,7 +740,7 @@ PyObject* qcache_fwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const at::Tensor* Q = plain(args[0]);
   float scale;
   int causal;
-  if (!Q || Q->dim() != 4 || !number(args[2], scale) || !flag(args[3], causal)) Py_RETURN_NONE;
+  if (!Q || Q->dim() != 4 || !counted(Q) || !number(args[2], scale) || !flag(args[3], causal)) Py_RETURN_NONE;
   const at::ScalarType et = Q->scalar_type();
   const c10::Device dev = Q->device();
   const int type = type16(et), B = (int)Q->size(0), Nq = (int)Q->size(1), Hq = (int)Q->size(2), d = (int)Q->size(3);
@@ -772,7 +778,7 @@ PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const at::ScalarType et = Q->scalar_type();
   const c10::Device dev = Q->device();
   const int n = (int)Q->dim(), lead = n - 2, type = value_type(Q);
-  if (type < 0 || (n != 3 && n != 4)) Py_RETURN_NONE;
+  if (type < 0 || (n != 3 && n != 4) || !counted(Q) || !counted(pos)) Py_RETURN_NONE;
   const int d = (int)Q->size(n - 1), Hq = (int)Q->size(n - 2), N = (int)Q->size(n - 3), B = n == 4 ? (int)Q->size(0) : 1, pairs = (int)f->size(0);
   int Hkv = 0;
   if (args[2] != Py_None) {

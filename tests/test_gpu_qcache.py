@@ -434,3 +434,30 @@ def test_a_prompt_sees_what_later_steps_see(k_bits, v_bits):
         score = 2 * (M * d / 2**24 + (M + np.abs(f64(L)) + 8) / 2**21)
         assert (np.abs(f64(l) - f64(L)) <= score).all()
         assert (np.abs(f64(o) - f64(O)) <= 2 * 2.0**-8 * (A + np.abs(f64(O))) * (1 + 2.0**-7) + A * 8 * score.transpose(0, 2, 1)[..., None]).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_pages_behind_a_sequence_are_not_looked_up(d):
+    """Entries of the table behind the last page that has a key are no pages at all."""
+    r, lens = rng(d), [70, 0, 640, 64, 1, 129]
+    cache = Cache(r, 6, 640, 2, d, 64, lens, 4, 8)
+    short = cache.table.clone()
+    for b, n in enumerate(lens):
+        short[b, -(-n // 64):] = -2**30
+    for nq in (1, 5, 40):
+        Q = gpu(r.normal(size=(6, nq, 4, d)), torch.bfloat16)
+        for causal in (False, True):
+            want = binding.fa_qcache_fwd(Q, cache.q, 0.1, causal, **cache.more)
+            got = binding.fa_qcache_fwd(Q, cache.q, 0.1, causal, **{**cache.more, "block_table": short})
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+    outs = []
+    for table in (cache.table, short):
+        K, V = (torch.zeros(6, 700, 2, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        binding.fa_qcache_read(cache.q, K, V, cache.more["seqlens_k"], table)
+        k, v = (torch.zeros(sum(lens), 2, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        binding.fa_qcache_read(cache.q, k, v, cache.more["seqlens_k"], table, cu_seqlens=ints([0] + np.cumsum(lens).tolist()))
+        q = binding.QCache(*(t.clone() for t in cache.q))
+        x = gpu(np.random.default_rng(7).normal(size=(6, 3, 2, d)), torch.bfloat16)
+        binding.fa_qcache_append(x, x, q, cache.more["seqlens_k"], table)
+        outs.append([K, V, k, v, *q])
+    assert all(torch.equal(a, b) for a, b in zip(*outs))

@@ -85,6 +85,9 @@ def test_attend_refusals():
         assert fa.fa_qcache_fwd_workspace_bytes(*x.values()) == 0, bad
     # more chunks of keys than are counted in 31 bits
     assert attend(B=64, Hq=1 << 10, Hkv=1 << 4, Nq=1 << 10, Nk=1 << 30) == fa.FA_ERR_SHAPE
+    # 2^24 rows, but 2^28 with those of the blocks of 16: a merge of more threads than a grid counts
+    assert attend(B=1 << 20, Hq=16, Hkv=16, Nq=1, Nk=256) == fa.FA_ERR_SHAPE
+    assert fa.fa_qcache_fwd_workspace_bytes(1 << 20, 16, 16, 1, 256, 64) == 0
 
 
 @pytest.mark.parametrize("d", [64, 128])
@@ -191,3 +194,21 @@ def test_tensors_of_rope(f):
     refused("Qout must be", f, Q, K, pos, inv, None, False, Q[:, :2])
     refused("places of their own", f, Q, K, pos, inv, None, False, torch.zeros(2, 1, 4, 64).expand(2, 3, 4, 64))
     refused("Kout without K", f, Q, None, pos, inv, None, False, None, K)
+
+
+def test_dimensions_past_31_bits():
+    """Seen before anything is called: tensors that only have a shape."""
+    def cache(n, hkv, rows):
+        return fa.qcache(n, hkv, rows, 64, device="meta")
+
+    def x(*shape):
+        return torch.empty(shape, dtype=torch.bfloat16, device="meta")
+
+    far, f = 2**31 + 1, torch.empty(8, device="meta")
+    for call in (lambda: fa.fa_qcache_fwd(x(1, 1, 1, 64), cache(1, 1, far), 1.0, True),
+                 lambda: fa.fa_qcache_fwd(x(1, far, 1, 64), cache(1, 1, 64), 1.0, True),
+                 lambda: fa.fa_qcache_append(x(1, far, 1, 64), x(1, far, 1, 64), cache(1, 1, 64)),
+                 lambda: fa.fa_qcache_read(cache(1, 1, 64), x(1, far, 1, 64), x(1, far, 1, 64)),
+                 lambda: fa.fa_rope_fwd(x(1, far, 1, 64), None, torch.empty((1, far), dtype=torch.int32, device="meta"), f)):
+        with pytest.raises(ValueError, match=r"2\*\*31"):
+            call()
