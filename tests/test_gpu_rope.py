@@ -128,3 +128,17 @@ def test_gradient_of_a_rotation_of_learned_tensors():
                 z[0, i, 0, t] += 0.5
                 d = (w.double() * (binding.fa_rope_fwd(z, None, pos, f, axis, neighbours)[0].double() - y)).sum() / 0.5
                 assert abs(float(d) - float(g[0, i, 0, t])) < 2**-16
+
+
+def test_more_tokens_than_workgroups_and_elements_past_31_bits():
+    """2^20 + 5 packed tokens of 33 heads of 64 in place: as the same tokens by themselves."""
+    T, f = 2**20 + 5, gpu(frequencies(32))
+    X = torch.zeros(T, 33, 64, dtype=torch.bfloat16, device="cuda")
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    at = torch.tensor([0, 1, 7, 2**20 - 1, 2**20, 2**20 + 4], device="cuda")
+    X[at] = gpu(np.random.default_rng(5).normal(size=(6, 33, 64)), torch.bfloat16)
+    want = binding.fa_rope_fwd(X[at], None, pos[at], f)[0]
+    got = binding.fa_rope_fwd(X, None, pos, f, Qout=X)[0]
+    assert got is X and torch.equal(X[at], want)
+    X[at] = 0
+    assert not X.any()
