@@ -663,9 +663,10 @@ int fa_qcache_read(const void* Kcodes, const void* Kscales, const void* Vcodes, 
 /*
  * Forward against such a cache: fa_kvcache_fwd over the values that codes and scales stand for. Q, O [B, Nq, Hq, d], LSE [B, Hq, Nq],
  * lengths, causal rule (query r at position r + seqlens_k[b] - Nq) and rows that see no key (O = 0, LSE = -inf) as there; any Nq. Keys and
- * values that a query does not see do not touch its result, also where their blocks are NaN (e = 255); E4M3's own NaN codes, which
- * fa_qcache_append never writes, and values past half precision's range have to lie in keys that all queries of the sequence see. NaN in a
- * query, in a key that it sees or in that key's value reaches the row's result. d in {64, 128}; Hkv at most 2^16, B * Hkv * R at most 2^26
+ * values that a query does not see do not touch its result, whatever they hold: NaN blocks (e = 255), E4M3's own NaN codes (which
+ * fa_qcache_append never writes), values past the type's range. NaN in a query, in a key that it sees or in that key's value reaches the row's
+ * result; a value past the type's range that a row sees leaves it infinite or NaN in that channel (in bfloat16 also values whose sum reaches
+ * 2^108: the sums are float32, of weights up to 2^20). d in {64, 128}; Hkv at most 2^16, B * Hkv * R at most 2^26
  * with R = Nq * Hq / Hkv rounded up to a multiple of 16 (rows up to 16), 32 (up to 64) or 128,
  * B * Hkv * (Nq * Hq / Hkv / 16 + 1) * (Nk / 128 + 1) below 2^31 (FA_ERR_SHAPE beyond). The keys that there are, by seqlens_k, are dealt to the
  * workgroups in equal runs: results are the same bits in every run, but a sequence's bits depend on the lengths of the others (float32

@@ -12,6 +12,7 @@
 namespace fa {
 
 typedef __attribute__((ext_vector_type(2))) short s16x2;
+typedef __attribute__((ext_vector_type(8))) unsigned short u16x8;
 
 // Row of the codes (and of the scales) in which head g of sequence s keeps slot c
 __device__ __forceinline__ long mx_row(const CacheView& v, int s, int g, int c) {
@@ -48,6 +49,53 @@ __device__ __forceinline__ bf16x8 mx_decode8(uint32_t w0, uint32_t w1, float s) 
     r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, true));
   }
   return __builtin_bit_cast(bf16x8, r);
+}
+
+// ---- Elements that are no finite 16-bit number: blocks of e = 255, E4M3's own NaN codes, and values that round past the type's range. A product
+// with them is NaN also where the weight is zero, so that what hides a key from some rows has to take them out of the product and give them to the
+// rows that do see it.
+
+// Whether a piece of a block may have one
+template <int BITS, bool F16, int N>
+__device__ __forceinline__ bool mx_past_type(const uint32_t (&w)[N], uint32_t e) {
+  // (elements up to 6 and 448; from these scales on 4 and 256 of them are 2^16 or 2^128)
+  bool past = e >= (F16 ? (BITS == 4 ? 141u : 135u) : (BITS == 4 ? 253u : 247u));
+  if constexpr (BITS == 8) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) past |= (((w[j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0u;
+  }
+  return past;
+}
+template <bool F16>
+__device__ __forceinline__ bool not_finite16(bf16x8 y, int t) {
+  const uint32_t mask = F16 ? 0x7c00u : 0x7f80u;
+  return ((uint32_t)__builtin_bit_cast(u16x8, y)[t] & mask) == mask;
+}
+// The piece without them: zeros in their place
+template <int BITS, bool F16, int N>
+__device__ __forceinline__ void mx_drop_past_type(uint32_t (&w)[N], uint32_t& e) {
+#pragma unroll
+  for (int j = 0; j < N * 4 / BITS; ++j) {
+    uint32_t& w0 = w[BITS == 4 ? j : 2 * j];
+    uint32_t& w1 = w[BITS == 4 ? j : 2 * j + 1];
+    const bf16x8 y = mx_decode8<BITS, F16>(w0, BITS == 4 ? 0u : w1, mx_scale(e));
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      const uint32_t code = not_finite16<F16>(y, t) ? (BITS == 4 ? 0xfu : 0xffu) << (BITS * t % 32) : 0u;
+      if (BITS == 4 || t < 4) w0 &= ~code;
+      else w1 &= ~code;
+    }
+  }
+  e = e == 255u ? 127u : e;
+}
+// Of four elements the ones that were taken out; zero for the others
+template <int BITS, bool F16>
+__device__ __forceinline__ f32x4 mx_past_type4(const uint8_t* codes, uint32_t e) {
+  const bf16x8 y = mx_decode8<BITS, F16>(BITS == 4 ? (uint32_t) * (const uint16_t*)codes : *(const uint32_t*)codes, 0u, mx_scale(e));
+  f32x4 x;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) x[t] = not_finite16<F16>(y, t) ? widen<F16>(y, t) : 0.f;
+  return x;
 }
 
 // Eight values over their scale, rounded to the nearest element (halves to even)

@@ -203,22 +203,19 @@ __device__ __forceinline__ void narrow_segment(const QAttendArgs& a, const QAtte
 
   auto compute = [&](int key0) {
     const bool edge = key0 + KT - 1 > lim_least || key0 + KT > it.end;
-    // (Where some rows do not see a key of V that is NaN, its blocks go in as zeros, and the rows that do see it get their NaN below.)
-    unsigned long long none[GROUPS];
+    // (Where some rows do not see a key, elements of V that are not finite go in as zeros, and the rows that do see it get them below.)
+    unsigned long long past[GROUPS];
     uint32_t e[GROUPS];
 #pragma unroll
     for (int v = 0; v < GROUPS; ++v) {
-      none[v] = 0ull;
+      past[v] = 0ull;
       e[v] = (vs[v / HG] >> (8 * (2 * (v % HG) + (lane >> 5)))) & 0xffu;
     }
     if (edge) {
 #pragma unroll
       for (int v = 0; v < GROUPS; ++v) {
-        const bool nan = e[v] == 255u;
-        none[v] = __builtin_amdgcn_ballot_w64(nan);
-        e[v] = nan ? 127u : e[v];
-#pragma unroll
-        for (int j = 0; j < VW; ++j) Vr[v][j] = nan ? 0u : Vr[v][j];
+        past[v] = __builtin_amdgcn_ballot_w64(mx_past_type<VB, F16>(Vr[v], e[v]));
+        if (past[v]) mx_drop_past_type<VB, F16>(Vr[v], e[v]);
       }
     }
     auto put_v = [&](int v) {
@@ -317,13 +314,20 @@ __device__ __forceinline__ void narrow_segment(const QAttendArgs& a, const QAtte
     if (edge) {
 #pragma unroll
       for (int v = 0; v < GROUPS; ++v)
-        for (unsigned long long b = none[v]; b; b &= b - 1) {
+        for (unsigned long long b = past[v]; b; b &= b - 1) {
           const int i = __builtin_ctzll(b), k = key0 + 32 * (v / HG) + (i & 31), blk = 2 * (v % HG) + (i >> 5);
+          if (k >= it.end) continue;  // (the last key once more)
+          const long row = mx_row(cv, it.s, it.g, k);  // (from the cache again: the tile's place is another's by now)
+          const uint32_t ee = a.c.Vs[row * SROW + blk];
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt)
+          for (int c = 0; c < 2; ++c) {
+            const f32x4 x = mx_past_type4<VB, F16>(a.c.Vc + row * VROW + (32 * blk + 16 * c + 4 * l4) * VB / 8, ee);
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
-              if (ct / 2 == blk && k <= lim_row[rt]) O[rt][ct] = (f32x4){NAN, NAN, NAN, NAN};
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+              for (int ct = 0; ct < CT; ++ct)
+                if (ct == 2 * blk + c && k <= lim_row[rt]) O[rt][ct] += x;
+          }
         }
     }
   };

@@ -100,15 +100,14 @@ __device__ __forceinline__ void wide_segment(const QAttendArgs& a, const QAttend
       *(bf16x8*)(smem + to + swz_off<ROWB>(tk, quarter * CHUNKS + j)) = y;
     }
   };
-  // (Where some row does not see a key of the tile, blocks that are NaN go in as zeros, and the rows that see them get their NaN after the product.)
+  // (Where some row does not see a key of the tile, elements that are not finite go in as zeros, and the rows that see them get them after the product.)
   auto put_v = [&](Raw& x, int key0, int stage) {
     const int tk = at.key, quarter = at.quarter;
     if (key0 + BC - 1 > lim_item || key0 + BC > it.end) {
-      const bool none = x.vs == 255u;
-      x.vs = none ? 127u : x.vs;
-#pragma unroll
-      for (int j = 0; j < VW; ++j) x.v[j] = none ? 0u : x.v[j];
-      smem[W::FLAGS_OFF + stage * 4 * BC + 4 * tk + quarter] = none;
+      const bool past = mx_past_type<VB, F16>(x.v, x.vs);
+      const auto [k4, q4] = part();
+      smem[W::FLAGS_OFF + stage * 4 * BC + 4 * k4 + q4] = past;
+      if (past) mx_drop_past_type<VB, F16>(x.v, x.vs);
     }
     const float s = mx_scale(x.vs);
 #pragma unroll
@@ -212,15 +211,26 @@ __device__ __forceinline__ void wide_segment(const QAttendArgs& a, const QAttend
         },
         [&](int i, const bf16x8& v) { O[i >> 2] = mfma32<F16>(v, P[(i >> 1) & 1][i & 1], O[i >> 2]); });
     if (key0 + BC - 1 > lim_item || key0 + BC > it.end) {
-      const uint32_t none = *(const uint32_t*)(smem + W::FLAGS_OFF + buf * 4 * BC + 4 * lane);  // of key `lane` of the tile
-      for (unsigned long long b = __builtin_amdgcn_ballot_w64(none != 0u); b; b &= b - 1) {
+      int ln = lane;  // (hidden from the compiler, as in part())
+      asm volatile("" : "+v"(ln));
+      const uint32_t past = *(const uint32_t*)(smem + W::FLAGS_OFF + buf * 4 * BC + 4 * ln);  // of key `ln` of the tile
+      for (unsigned long long b = __builtin_amdgcn_ballot_w64(past != 0u); b; b &= b - 1) {
         const int k = __builtin_ctzll(b);
-        const uint32_t which = (uint32_t)__builtin_amdgcn_readlane((int)none, k);
+        if (key0 + k >= it.end) break;  // (the last key once more)
+        const uint32_t which = (uint32_t)__builtin_amdgcn_readlane((int)past, k);
+        const long row = mx_row(cv, it.s, it.g, key0 + k);
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-          if ((which >> (8 * (4 / DT) * dt)) & 0xffu && key0 + k <= lim_end)
+        for (int dt = 0; dt < DT; ++dt) {
+          if (!((which >> (8 * (4 / DT) * dt)) & (DT == 4 ? 0xffu : 0xffffu))) continue;
+          const uint32_t ee = a.c.Vs[row * (D / 32) + dt];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) O[dt][r] = NAN;
+          for (int r4 = 0; r4 < 4; ++r4) {
+            const f32x4 x = mx_past_type4<VB, F16>(a.c.Vc + row * (D * VB / 8) + (32 * dt + 8 * r4 + 4 * (ln >> 5)) * VB / 8, ee);
+            if (key0 + k <= lim_end)
+#pragma unroll
+              for (int u = 0; u < 4; ++u) O[dt][4 * r4 + u] += x[u];
+          }
+        }
       }
     }
     if (more) hide(Sn, key0 + BC);

@@ -461,3 +461,104 @@ def test_pages_behind_a_sequence_are_not_looked_up(d):
         binding.fa_qcache_append(x, x, q, cache.more["seqlens_k"], table)
         outs.append([K, V, k, v, *q])
     assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+# ---- values past the type's range among keys that only some rows see
+
+def check_beside(dtype, c, Q, lens, causal, infinite, skip=None):
+    """O of fa_qcache_fwd where c.rows has the keys and values with what is `infinite` (values as the type has them: infinities, NaN; else 0)
+    left out: as if that were zeros in the rows that do not see it, and not finite in those that do (NaN where the key's weight is below the type's
+    least number). skip: rows [B, Nq, Hq] left out of the comparison."""
+    B, nq, hq, d = Q.shape
+    hkv = c.rows[0].shape[2]
+    O, L = (f64(x) for x in binding.fa_qcache_fwd(Q, c.q, d**-0.5, causal, **c.more))
+    none = np.zeros((0, hkv, d))
+    rows = [[x[b][:lens[b]] for b in range(B)] for x in c.rows]
+    eO, eL, A, M = dec.prefix_forward(f64(Q), none, none, *rows, lens, d**-0.5, causal)
+    e = torch.finfo(TYPES[dtype]).eps / 2
+    score = M * d / 2**24 + (M + np.abs(eL) + 8) / 2**21
+    tol = e * (A + np.abs(eO)) * (1 + 2 * e) + A * 4 * score.transpose(0, 2, 1)[..., None]
+    wrong = []
+    for b in range(B):
+        for q in range(nq):
+            seen = max(0, min(lens[b], lens[b] - nq + q + 1)) if causal else lens[b]
+            for h in range(hq):
+                if skip is not None and skip[b, q, h]:
+                    continue
+                g = h * hkv // hq
+                x = infinite[b, :seen, g]
+                with np.errstate(invalid="ignore"):
+                    want = eO[b, q, h] + x.sum(0)
+                # (half precision's P, where it is subnormal, as everywhere above: of the largest value in the channel)
+                small = c.slots * 4.0 / 2**25 * np.abs(c.rows[1][b, :lens[b], g]).max(0) if dtype == "f16" else 0.0
+                finite = np.isfinite(want)
+                ok = np.where(finite, np.abs(O[b, q, h] - np.where(finite, want, 0)) <= tol[b, q, h] + small, ~np.isfinite(O[b, q, h]))
+                # Sums are float32, over weights against a reference that bfloat16's largest score may outgrow by up to 2^20 before it is
+                # advanced: where the values seen sum to 2^128 / 2^20 the sum may pass 2^128 and be infinite (half precision's cannot:
+                # 2^8 times the few hundred values below 2^16 stays below 2^33).
+                if dtype == "bf16":
+                    ok |= ~np.isfinite(O[b, q, h]) & (np.abs(c.rows[1][b, :seen, g]).sum(0) >= 2.0**108)
+                if not ok.all() or not abs(L[b, h, q] - eL[b, h, q]) <= score[b, h, q]:
+                    wrong.append((b, q, h, np.flatnonzero(~ok).tolist()))
+    assert not wrong, wrong[:5]
+
+
+def put_block(c, which, b, slot, g, blk, values):
+    """A block of 32 values into the cache; returns what it stands for."""
+    bits = c.bits[which]
+    codes, scales = orc.quantise(values, bits)
+    row, at = (int(c.order[b, slot // c.page]), slot % c.page) if c.page else (b, slot)
+    packed = orc.packed(codes, bits)
+    n = len(packed)
+    c.q[2 * which][row, g, at, n * blk:n * blk + n] = gpu(packed)
+    c.q[2 * which + 1][row, g, at, blk] = int(scales[0])
+    return orc.values(codes, scales, bits)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("k_bits,v_bits", BITS)
+@pytest.mark.parametrize("nq,page", [(1, 64), (5, 0), (10, 64), (40, 64)])
+def test_what_a_row_does_not_see_may_be_past_the_type(dtype, d, k_bits, v_bits, nq, page):
+    """The type's largest numbers, which quantised come back as infinities, among the newest values: the rows before them are as if they were not
+    there, the others are not finite in that channel and in no other; of an old value every row is. Likewise keys, of which the rows that
+    do see them are left out; and E4M3's own NaN codes, which no block of append's has."""
+    hq, hkv, B, slots, lens = 4, 2, 2, 300, [300, 171]
+    r = rng(nq + d)
+    c = Cache(r, B, slots, hkv, d, page, lens, k_bits, v_bits)
+    for x in c.rows:
+        for b in range(B):
+            x[b, lens[b]:] = 0.0  # (no key's)
+    Q = gpu(r.normal(size=(B, nq, hq, d)), TYPES[dtype])
+    top = torch.finfo(TYPES[dtype]).max
+    infinite, skip = np.zeros((B, slots, hkv, d)), np.zeros((B, nq, hq), bool)
+
+    def spoil(b, slot, g, blk, at, other):
+        x = np.zeros(32)
+        x[at], x[other], x[(at + 2) % 32] = top, -top, top / 4
+        x = put_block(c, 1, b, slot, g, blk, x)
+        held = f64(torch.from_numpy(x).to(TYPES[dtype]))
+        assert np.isinf(held[at]) and np.isinf(held[other]) and np.isfinite(held).sum() == 30
+        here = slice(32 * blk, 32 * blk + 32)
+        infinite[b, slot, g, here] = np.where(np.isfinite(held), 0, held)
+        c.rows[1][b, slot, g, here] = np.where(np.isfinite(held), x, 0)
+
+    spoil(0, 299, 0, 1, 3, 20)
+    spoil(1, 5, 0, 0, 31, 0)
+    if nq > 1:
+        spoil(0, 298, 1, 0, 16, 15)
+        spoil(1, 171 - nq // 2, 1, d // 32 - 1, 8, 7)
+        x = np.zeros(32)
+        x[4] = top
+        put_block(c, 0, 1, 171 - nq // 2, 0, 1, x)
+        skip[1, nq - nq // 2:, :2] = True  # (query q sees keys up to 171 - nq + q)
+    if v_bits == 8:
+        slot, g = 300 - max(1, nq // 3), 1
+        row, at = (int(c.order[0, slot // page]), slot % page) if page else (0, slot)
+        c.q.Vcodes[row, g, at, 35], c.q.Vcodes[row, g, at, 47] = 0x7f, 0xff
+        infinite[0, slot, g, [35, 47]] = np.nan
+        c.rows[1][0, slot, g, [35, 47]] = 0.0
+    check_beside(dtype, c, Q, lens, True, infinite, skip)
+    if nq > 1:  # (without the causal rule every row sees every key: the spoilt key is taken back)
+        c.rows[0][1, 171 - nq // 2, 0, 32:64] = put_block(c, 0, 1, 171 - nq // 2, 0, 1, r.normal(size=32))
+        check_beside(dtype, c, Q, lens, False, infinite)
