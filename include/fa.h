@@ -653,8 +653,9 @@ int fa_qcache_append(const void* Knew, const void* Vnew, void* Kcodes, void* Ksc
  *   cu_seqlens == nullptr: K, V [B, N, Hkv, d]; row i of sequence b is slot first[b] + i (first: DEVICE int32 [B], nullptr: 0).
  *   cu_seqlens != nullptr: K, V [N, Hkv, d] packed; sequence b fills rows cu_seqlens[b] .. cu_seqlens[b + 1] - 1 from its slot 0 on (DEVICE
  *     int32 [B + 1]; first must be nullptr, FA_ERR_SHAPE otherwise), which fa_varlen_cross_fwd can take as they are.
- * Rows whose slot lies outside 0 .. seqlens_k[b] - 1 (nullptr: Nk), and packed rows past N, are left as they were. At most 2^30 rows a head in
- * all (B * Hkv * min(N, Nk), rounded up to 64 rows each; FA_ERR_SHAPE beyond). Everything else as fa_qcache_append.
+ * Rows whose slot lies outside 0 .. seqlens_k[b] - 1 (nullptr: Nk), and packed rows past N, are left as they were. Below 2^30 rows of
+ * all heads: B * Hkv * N, or of packed rows B * Hkv * min(N, Nk), with N or the least rounded up to a multiple of 64 (FA_ERR_SHAPE otherwise).
+ * Everything else as fa_qcache_append.
  */
 int fa_qcache_read(const void* Kcodes, const void* Kscales, const void* Vcodes, const void* Vscales, void* K, void* V,
                    const int32_t* seqlens_k, const int32_t* block_table, const int32_t* first, const int32_t* cu_seqlens, int B, int Hkv, int N,

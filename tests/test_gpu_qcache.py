@@ -158,6 +158,22 @@ def test_read_of_no_lengths_is_all_slots_and_blocks_without_numbers_are_nan():
     assert np.array_equal(f64(K), c.rows[0], equal_nan=True) and np.array_equal(f64(V), c.rows[1], equal_nan=True)
 
 
+def test_read_of_windows_longer_than_the_cache():
+    """Wherever the window begins, the rows that have a slot are found, and no others written."""
+    first = [0, -1, -63, -64, -65, -430, -499, -500, 69, 70, -2**31, 2**31 - 1, 5]
+    lens = [70] * (len(first) - 1) + [0]
+    c = Cache(rng(20), len(first), 70, 2, 64, 0, lens, 4, 8)
+    K, V = (torch.full((len(first), 500, 2, 64), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    binding.fa_qcache_read(c.q, K, V, first=ints(first), **c.more)
+    for got, rows in ((K, c.rows[0]), (V, c.rows[1])):
+        want = np.full(got.shape, 7.0)
+        for b in range(len(first)):
+            lo, hi = max(0, -first[b]), min(500, lens[b] - first[b])
+            if lo < hi:
+                want[b, lo:hi] = rows[b, first[b] + lo:first[b] + hi]
+        assert np.array_equal(f64(got), want)
+
+
 # ---- attention
 
 def check(dtype, d, B, nq, hq, hkv, slots, page, lens, k_bits, v_bits, causal=True, seed=0, scale=None, cache=None, Q=None, call=None):

@@ -2,6 +2,7 @@
 launched, no GPU is touched."""
 import pytest
 
+from launches import launches
 from paper_2307_08691_amd import binding as fa
 
 torch = pytest.importorskip("torch")
@@ -63,6 +64,22 @@ def test_read_refusals():
         assert read(**bad) == fa.FA_ERR_SHAPE, bad
     for bad in PAGES + [dict(d=16), dict(d=260), dict(type=fa.FA_TYPE_F32)]:
         assert read(**bad) == fa.FA_ERR_UNSUPPORTED, bad
+
+
+def test_how_many_rows_read_takes():
+    """Both sides of the limit: below 2^30 rows of all heads in whole workgroups of 64, where packed rows count as many a sequence as its cache has
+    slots at most, and windows (which may begin before slot 0) all of theirs."""
+    def call(cu, B, Hkv, N, Nk):
+        return "fa_qcache_read", [P] * 7 + [0, 0, P if cu else 0, B, Hkv, N, Nk, 64, 4, 8, 0, 0, fa.FA_TYPE_BF16]
+
+    sizes = [(0, 64, 8, 1 << 20, 64, 1 << 23), (1, 64, 8, 1 << 21, 64, 512), (0, 1 << 10, 1 << 8, 65, 1 << 30, 1 << 19),
+             (1, 1 << 10, 1 << 8, 1 << 12, 63 * 64, 63 << 18), (0, 1, 1, (1 << 30) - 64, 1 << 30, (1 << 24) - 1),
+             (1, 1, 1, (1 << 30) - 64, 1 << 30, (1 << 24) - 1)]
+    for (*_, grid), kernels in zip(sizes, launches([call(*x[:-1]) for x in sizes])):
+        assert [(k[0].split("<")[0], *k[1:]) for k in kernels] == [("qread_kernel", grid, 1, 256)]
+    for cu, B, Hkv, N, Nk in ((0, 1, 1, 1 << 30, 1 << 30), (1, 1, 1, 1 << 30, 1 << 30), (0, 1, 1, (1 << 30) - 63, 1 << 30), (0, 64, 8, 1 << 21, 64),
+                              (0, 1 << 10, 1 << 8, 1 << 12, 1 << 12), (1, 1 << 10, 1 << 8, 1 << 13, 1 << 12)):
+        assert read(cu=P if cu else 0, B=B, Hkv=Hkv, N=N, Nk=Nk) == fa.FA_ERR_SHAPE
 
 
 def test_attend_refusals():
