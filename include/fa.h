@@ -672,7 +672,8 @@ int fa_qcache_read(const void* Kcodes, const void* Kscales, const void* Vcodes, 
  * B * Hkv * (Nq * Hq / Hkv / 16 + 1) * (Nk / 128 + 1) below 2^31 (FA_ERR_SHAPE beyond). The keys that there are, by seqlens_k, are dealt to the
  * workgroups in equal runs: results are the same bits in every run, but a sequence's bits depend on the lengths of the others (float32
  * sums cut elsewhere). `workspace` (partial results, float32; 16-byte aligned) needs fa_qcache_fwd_workspace_bytes() bytes, undefined on entry
- * and return; where that is 0 it may be NULL. It grows with the batch up to 25 MB (Nq * Hq / Hkv up to 64) or 68 MB, not with the caches.
+ * and return; where that is 0 it may be NULL. It grows with the batch up to 22 MB (Nq * Hq / Hkv up to 16), 34 MB (up to 64) or
+ * 72 MB, not with the caches.
  * type: of Q and O, FA_TYPE_BF16 or FA_TYPE_F16. Forward only, as fa_kvcache_fwd.
  */
 size_t fa_qcache_fwd_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int d);

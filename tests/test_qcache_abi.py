@@ -119,6 +119,16 @@ def test_workspace_needs(d):
     assert need(64, 8, 200, 1 << 20) <= 2 * 512 * 128 * (d + 1) * 4 + 2 * 64 * 8 * 8 + 256
 
 
+def test_workspace_of_the_largest_batches():
+    """Partial results of all workgroups, and eight bytes for every block of rows of every head: the most that the header says."""
+    for rows, G, groups, blocks, most in ((16, 16, 768, 1, 22), (32, 64, 512, 2, 34), (128, 128, 512, 1, 72)):
+        B = min(1 << 20, (1 << 26) // (rows * blocks))
+        need = fa.fa_qcache_fwd_workspace_bytes(B, G, 1, 1, 256, 128)
+        assert need == 2 * groups * rows * 129 * 4 + 8 * B * blocks <= most * 10**6
+        assert attend(B=B, Hq=G, Hkv=1, Nk=256, d=128, nb=need - 1) == fa.FA_ERR_WORKSPACE
+        assert fa.fa_qcache_fwd_workspace_bytes(B, G, 1, 1, 1 << 20 if B < 1 << 18 else 256, 128) == need
+
+
 @pytest.mark.parametrize("inverse", [False, True])
 def test_rope_refusals(inverse):
     for name in ("Q", "Qo", "Ko", "pos", "f"):
