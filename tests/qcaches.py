@@ -1,4 +1,8 @@
 """Caches in 4 or 8 bits on the GPU beside what they hold in float64, for the tests of the operators on them."""
+import json
+import subprocess
+import sys
+
 import numpy as np
 import torch
 
@@ -67,3 +71,60 @@ class Cache:
                 t = np.stack([np.concatenate([t[p] for p in self.order[b]], 1)[:, :self.slots] for b in range(self.B)])
             out.append(t.transpose(0, 2, 1, 3))
         return out
+
+
+# Batches whose sequences are long and many, so that a workgroup has tens of thousands of keys of one: (d, K's and V's bits, queries, query heads, sequences, page,
+# most slots), 8 key/value heads.
+LONG = [
+    (128, 4, 4, 1, 32, 96, 64, 10240),   # 16 rows, tiles of 32 keys
+    (64, 4, 4, 1, 16, 96, 64, 17536),    # ... of 64
+    (128, 8, 8, 4, 32, 64, 256, 10240),  # 512 workgroups, one tile on its way
+    (128, 4, 4, 5, 32, 64, 64, 10240),   # 32 rows
+    (64, 8, 4, 3, 64, 64, 256, 10240),
+    (128, 4, 4, 40, 32, 32, 64, 10240),  # 128 rows, two blocks
+    (64, 8, 8, 32, 32, 64, 256, 10240),  # ... one
+]
+
+
+def long_lengths(B, slots):
+    return [slots - 37 * (b % 5) for b in range(B)]
+
+
+def longest_segment(lens, nq, group, hkv, rows, chunk, workgroups):
+    """Keys of the longest part of a sequence that one workgroup has: the chunks of all (sequence, head, block of rows) under the causal rule, one
+    after the other, in equal runs."""
+    blocks = -(-nq * group // rows)
+    units = []
+    for n in lens:
+        for _ in range(hkv):
+            for k in range(blocks):
+                last = (min((k + 1) * rows, nq * group) - 1) // group
+                units.append(-(-max(0, min(n, n - nq + last + 1)) // chunk))
+    total = sum(units)
+    run, more = divmod(total, workgroups)
+    cuts = np.cumsum([0] + [run + (w < more) for w in range(workgroups)])
+    ends = np.cumsum([0] + units)
+    points = np.unique(np.concatenate([cuts, ends]))
+    return int(np.diff(points).max()) * chunk
+
+
+GRIDS = """
+import ctypes, json, sys
+sys.path.insert(0, sys.argv[1])
+recorder = ctypes.CDLL(sys.argv[2], mode=ctypes.RTLD_GLOBAL)
+recorder.recorded.restype = ctypes.c_char_p
+from paper_2307_08691_amd import binding
+out = []
+for args in json.load(sys.stdin):
+    assert binding.fa_qcache_fwd_raw(*args) == 0
+    out.append([int(line.split("|")[1]) for line in recorder.recorded().decode().splitlines()])
+json.dump(out, sys.stdout)
+"""
+
+
+def grids(calls):
+    """[arguments of fa_qcache_fwd_raw] -> per call the workgroups of its launches, seen without a GPU (launches.py; the kernels have no names outside)."""
+    import launches
+    r = subprocess.run([sys.executable, "-c", GRIDS, launches.ROOT, launches.recorder()], input=json.dumps(calls), capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
+    return json.loads(r.stdout)

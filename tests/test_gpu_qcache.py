@@ -15,7 +15,7 @@ from paper_2307_08691_amd import binding
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from qcaches import Cache, TYPES, f64, gpu, ints  # noqa: E402
+from qcaches import LONG, Cache, TYPES, f64, gpu, ints, long_lengths  # noqa: E402
 
 BITS = [(4, 4), (8, 4), (4, 8), (8, 8)]
 
@@ -578,3 +578,24 @@ def test_what_a_row_does_not_see_may_be_past_the_type(dtype, d, k_bits, v_bits, 
     if nq > 1:  # (without the causal rule every row sees every key: the spoilt key is taken back)
         c.rows[0][1, 171 - nq // 2, 0, 32:64] = put_block(c, 0, 1, 171 - nq // 2, 0, 1, r.normal(size=32))
         check_beside(dtype, c, Q, lens, False, infinite)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d,k_bits,v_bits,nq,hq,B,page,slots", LONG)
+def test_attend_where_a_workgroup_has_many_tiles_of_a_sequence(dtype, d, k_bits, v_bits, nq, hq, B, page, slots):
+    """More than 64 tiles in a row, for which page numbers are looked up together: they are looked up again. (The sequences' pages, in orders of their own,
+    are from one small pool.)"""
+    r, hkv, pool = rng(slots + d + nq), 8, 48
+    data = [r.normal(size=(pool, page, hkv, d)) for _ in range(2)]
+    tensors, held = [], []
+    for x, bits in zip(data, (k_bits, v_bits)):
+        codes, scales = orc.quantise(x, bits)
+        held.append(orc.values(codes, scales, bits))
+        tensors += [gpu(t.transpose(0, 2, 1, 3)) for t in (orc.packed(codes, bits), scales)]
+    q, lens, order = binding.QCache(*tensors), long_lengths(B, slots), r.integers(0, pool, size=(B, -(-slots // page)))
+    Q = gpu(r.normal(size=(B, nq, hq, d)), TYPES[dtype])
+    O, L = binding.fa_qcache_fwd(Q, q, d**-0.5, True, seqlens_k=ints(lens), block_table=ints(order.tolist()), max_seqlen_k=slots)
+    some = [0, B // 2 + 1, B - 1]
+    c = Cache.__new__(Cache)
+    c.q, c.more, c.rows = q, {}, [np.stack([x[order[b]].reshape(-1, hkv, d) for b in some]) for x in held]
+    check(dtype, d, 3, nq, hq, hkv, slots, page, [lens[b] for b in some], k_bits, v_bits, cache=c, Q=Q[some], call=lambda *a: (O[some], L[some]))

@@ -7,6 +7,8 @@ from paper_2307_08691_amd import binding as fa
 
 torch = pytest.importorskip("torch")
 
+from qcaches import LONG, grids, long_lengths, longest_segment  # noqa: E402
+
 P = 0x10000  # a non-null, 16-byte aligned fake device address; never dereferenced on these paths
 BIG = 1 << 40
 INF, NAN = float("inf"), float("nan")
@@ -127,6 +129,18 @@ def test_workspace_of_the_largest_batches():
         assert need == 2 * groups * rows * 129 * 4 + 8 * B * blocks <= most * 10**6
         assert attend(B=B, Hq=G, Hkv=1, Nk=256, d=128, nb=need - 1) == fa.FA_ERR_WORKSPACE
         assert fa.fa_qcache_fwd_workspace_bytes(B, G, 1, 1, 1 << 20 if B < 1 << 18 else 256, 128) == need
+
+
+def test_the_long_batches_of_the_gpu_tests_are_long():
+    """Page numbers are looked up for 64 tiles at a time: a wavefront has more than that (128 rows: the workgroup)."""
+    calls = [[P] * 10 + [BIG, B, hq, 8, nq, slots, d, kb, vb, page, slots // page, 0.1, True, fa.FA_TYPE_BF16]
+             for d, kb, vb, nq, hq, B, page, slots in LONG]
+    for (d, kb, vb, nq, hq, B, page, slots), launched in zip(LONG, grids(calls)):
+        rows = 16 if nq * hq // 8 <= 16 else (32 if nq * hq // 8 <= 64 else 128)
+        tile = 64 if rows == 128 or (d == 64 and kb + vb == 8) else 32
+        chunk = 256 if rows < 128 and tile == 64 else 128
+        n = longest_segment(long_lengths(B, slots), nq, hq // 8, 8, rows, chunk, launched[0])
+        assert n > 64 * tile * (1 if rows == 128 else 4), (d, kb, vb, nq, n)
 
 
 @pytest.mark.parametrize("inverse", [False, True])
