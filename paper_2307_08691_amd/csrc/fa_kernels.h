@@ -269,7 +269,7 @@ struct QAttendArgs {
 struct QAttendPlan {      // how the work is cut (a function of the sizes alone)
   int rows, blocks;       // packed rows (query * G + head of the group) of a block, blocks of a key/value head
   int chunk_log2;         // keys that are dealt together
-  int groups, least;      // workgroups, and the fewest chunks that one is started for
+  int groups;             // workgroups
   int slots;              // places for partial results
 };
 QAttendPlan qattend_plan(int B, int Hq, int Hkv, int Nq, int Nk, int d, int bits);  // bits: of K and V together (0: room for any)

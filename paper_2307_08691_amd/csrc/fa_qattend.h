@@ -81,10 +81,9 @@ __device__ __forceinline__ void for_segments(const QAttendArgs& a, const QAttend
     all += y;
   }
   all = uniform(all) * Hkv;
-  // As many workgroups as there are, or fewer, so that none has less than p.least chunks; a multiple of the XCDs where it can be. The
-  // first `more` of them have a chunk more than the others.
-  const unsigned most = ((unsigned)all + p.least - 1) / (unsigned)p.least;
-  unsigned n = most < (unsigned)p.groups ? most : (unsigned)p.groups;
+  // As many workgroups as there are, or as there are chunks; a multiple of the XCDs where it can be. The first `more` of them have a
+  // chunk more than the others.
+  unsigned n = (unsigned)all < (unsigned)p.groups ? (unsigned)all : (unsigned)p.groups;
   if (n >= kXcds) n = n / kXcds * kXcds;
   n = (unsigned)uniform((int)n);
   if ((unsigned)b < n) {

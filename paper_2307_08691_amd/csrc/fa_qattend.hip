@@ -456,7 +456,6 @@ QAttendPlan qattend_plan(int B, int Hq, int Hkv, int Nq, int Nk, int d, int bits
   // parts to the merge (us at 512 and 768: 131072 keys of 128, 8 and 4 bits, one sequence, 32 heads on 8: 42.2 and 45.3; 16 sequences of up to
   // 8192, 8 and 8: 35.0 and 35.5; but 64 of up to 8192, 4 and 4: 76.5 and 66.0; 64 of up to 4096 of 64 channels, 8 and 8: 39.3 and 34.7)
   p.groups = p.rows == 16 && !(d == 128 && bits > 8) ? 768 : 512;
-  p.least = 1;
   p.chunk_log2 = p.rows != 128 && bits && narrow_keys(d, bits) == 64 ? 8 : 7;  // (narrow: a tile for each of four wavefronts)
   const double units = (double)B * Hkv * p.blocks;
   if (p.rows != 128 && units <= 512 && Nk <= kWhole)  // (whatever the bits: the workspace is sized without them)
