@@ -629,14 +629,14 @@ int fa_verify_drafts(const int32_t* draft_tokens, const void* draft_probs, const
  * (255: all 32 are NaN); elements are E2M1 (bits = 4: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign; two a byte, the even channel in the low half) or E4M3
  * (bits = 8, as in fa_fp8_fwd). Kcodes [B, Hkv, Nk, d * k_bits / 8] and Kscales [B, Hkv, Nk, d / 32] bytes, the same of V with v_bits (the two
  * may differ); with a block_table (as fa_kvcache_fwd) pools of pages, [pages, Hkv, page_size, ..]: heads before slots, unlike the 16-bit
- * caches. Codes 16-byte aligned, scales 4-byte. k_bits, v_bits in {4, 8} (FA_ERR_UNSUPPORTED otherwise).
+ * caches. Codes 16-byte aligned, scales 4-byte. k_bits, v_bits in {4, 8} (FA_ERR_UNSUPPORTED otherwise). B * Hkv at most 2^20 (FA_ERR_SHAPE beyond).
  *
  * fa_qcache_append: new keys and values, quantised as they are written. Row i of Knew, Vnew goes to slot seqlens_k[b] - Nq + i of sequence
  * b (seqlens_k counts the new keys already; nullptr: Nk); rows whose slot lies outside 0 .. Nk - 1 are dropped. With top the largest
  * magnitude of a block's 32 values, the scale is the smallest power of two, 2^-111 at least, with top <= 1.75 * 2^2 of it (4 bits) or
  * 1.75 * 2^8 (8 bits); every value over its scale is rounded to the nearest element, halves to the one with an even code, what lies
  * above 6 to 6. (Exact but for that rounding, of half a step at most.) A block with an infinity or a NaN becomes NaN (codes 0, e = 255).
- * Element (b, i, g, t) of Knew lies at b * k_batch_stride + i * k_token_stride + g * k_head_stride + t (elements, multiples of 8), of Vnew
+ * Element (b, i, g, t) of Knew lies at b * k_batch_stride + i * k_token_stride + g * k_head_stride + t (elements, multiples of 8, not negative), of Vnew
  * at v_*: both may be slices of a projection's output. Kout, Vout [B, Nq, Hkv, d] (or NULL) receive the values that the new slots now stand
  * for, in the type of Knew: what attention within the new rows has to use to agree with later steps. Kout may be Knew and Vout Vnew,
  * where those are dense. Dropped rows leave Kout, Vout as they were. A value within half a step of the type's range that rounds past it
@@ -688,7 +688,7 @@ int fa_qcache_fwd(const void* Q, const void* Kcodes, const void* Kscales, const 
  * and channels 2 * pairs .. d - 1 pass through. a is the exact product (reduced in float64), sine and cosine are good to float32, the rotation is
  * float32. fa_rope_bwd is the gradient, the same with -a: it takes dQout, dKout and leaves dQ, dK.
  * Q [B, N, Hq, d] -> Qout, and in the same launch K [B, N, Hkv, d] -> Kout (K NULL: Q alone; Hkv is ignored): element (b, i, h, t) at b *
- * batch_stride + i * token_stride + h * head_stride + t, `strides` (HOST array, elements) holding those three of Q, Qout, K, Kout in turn.
+ * batch_stride + i * token_stride + h * head_stride + t, `strides` (HOST array, elements, none negative) holding those three of Q, Qout, K, Kout in turn.
  * An output may be its input (the same strides). positions: DEVICE int32, axis x, sequence b, token i at positions[x * axis_stride + b * batch_stride + i];
  * any values, negative ones too. inv_freq: DEVICE float32 [pairs], finite (up to 1 for the accuracy said). axis: DEVICE int32 [pairs] (clamped into 0 .. axes - 1; nullptr: 0). type:
  * FA_TYPE_*. Tensors aligned to their elements (16 bytes, with strides of as many, is fastest). d a multiple of 8 up to 256, 1 <= pairs,

@@ -450,11 +450,19 @@ constexpr int kWhole = 1024;
 QAttendPlan qattend_plan(int B, int Hq, int Hkv, int Nq, int Nk, int d, int bits) {
   QAttendPlan p;
   const long rows = (long)Nq * (Hq / Hkv);
+  // Rows of a block. us of a pass, 32 heads on 8 of 128, 4 bits, pages of 64, by blocks of 16, 32 and 128:
+  //   rows                             16                  20                   32                   36                  48                   64             128
+  //   16 sequences of up to 4096   27  32  41          35  35  40           39  39  42           50  58  42          53  64  43           65  74  44     -  133  49
+  //   64 of up to 8192             80 104 196         144 110 197          149 120 197          210 195 197         217 206 199          285 219 202     -  416 216
+  // (8 and 8 bits, and 64 channels, rank alike.) Up to 16 rows and from 17 to 32 the choice is the fastest. From 33 to 64 two blocks of 32 read the cache
+  // twice and are mostly slower than one of 128, by up to 1.7 times on few sequences and 9% on many.
   p.rows = rows <= 16 ? 16 : (rows <= 64 ? 32 : 128);
   p.blocks = (int)((rows + p.rows - 1) / p.rows);
   // As many workgroups as fit: three a compute unit, or two. Two stream as fast as three where a tile has 6 KB and more, and leave fewer
   // parts to the merge (us at 512 and 768: 131072 keys of 128, 8 and 4 bits, one sequence, 32 heads on 8: 42.2 and 45.3; 16 sequences of up to
-  // 8192, 8 and 8: 35.0 and 35.5; but 64 of up to 8192, 4 and 4: 76.5 and 66.0; 64 of up to 4096 of 64 channels, 8 and 8: 39.3 and 34.7)
+  // 8192, 8 and 8: 35.0 and 35.5; but 64 of up to 8192, 4 and 4: 76.5 and 66.0; 64 of up to 4096 of 64 channels, 8 and 8: 39.3 and 34.7). Both sides
+  // with LDS and registers for three (Narrow::WAVES), where more than 8 bits of 128 channels have one tile on its way: what two could do with
+  // the room that they have is not measured.
   p.groups = p.rows == 16 && !(d == 128 && bits > 8) ? 768 : 512;
   p.chunk_log2 = p.rows != 128 && bits && narrow_keys(d, bits) == 64 ? 8 : 7;  // (narrow: a tile for each of four wavefronts)
   const double units = (double)B * Hkv * p.blocks;
